@@ -18,6 +18,11 @@
  *                share every projection launch), leaving the prefix cache
  *                as vsr_prefill does.
  *
+ * Context-free calls on the same stages' tensors: vsr_rope_axes and
+ * vsr_qk_norm_rope (positions with several axes, norms of query and key heads),
+ * vsr_pick_tokens (a token per row of logits under rules), vsr_align_select,
+ * vsr_keyframes, vsr_retrieve.
+ *
  * Each candidate sees the prefix plus its own earlier tokens only (the drafts
  * are scored independently, Eq. 6); candidate token j sits at position P + j.
  *
@@ -231,6 +236,169 @@ int vsr_reliability(vsr_ctx *ctx, const int32_t *branch_ids, const int32_t *bran
 int vsr_draft(vsr_ctx *ctx, const int32_t *prompt_ids, const int32_t *prompt_len, int32_t M,
               int32_t Cmax, int32_t n_new, int32_t *tokens);
 
+/* ---- positions with several axes, norms of query and key heads -------------
+ *
+ * A rotary scheme: head dims (i, i + rot/2), rot = 2 * sum of sections, turn by
+ *   pos[a(i)] * base^(-2 i / rot),
+ * a(i) the axis of pair i (e.g. time, height, width of a video row; a text row
+ * has one position on every axis). Dims >= rot pass through.
+ *   interleaved 0: the first sections[0] pairs belong to axis 0, the next
+ *     sections[1] to axis 1, and so on;
+ *   interleaved 1: pair i belongs to axis x = i % n_axes while
+ *     i < n_axes * sections[x], else to axis 0 (axes 1.. must fit that way).
+ * 1 <= n_axes <= VSR_MAX_AXES, sections[x] >= 0 (those past n_axes are ignored),
+ * rot >= 2, base finite and > 0. */
+#define VSR_MAX_AXES 4
+typedef struct vsr_rotary {
+  int32_t n_axes;
+  int32_t sections[VSR_MAX_AXES];
+  int32_t interleaved;
+  float base;
+} vsr_rotary;
+
+/* Heads [tokens][n_heads][head_dim] in device memory, head_dim consecutive,
+ * token and head strides in elements (>= 0): a slice of stacked QKV rows, or a
+ * key cache [n_heads][positions][head_dim] (token_stride head_dim). */
+typedef struct vsr_heads {
+  void *data;
+  int32_t n_heads;
+  int64_t token_stride, head_stride;
+} vsr_heads;
+
+/* Rotates the query heads q_in into q_out and the key heads k_in into k_out.
+ *   pos    : device int32, axis x's position of token t at pos[x pos_stride + t]
+ *            (any int32; angles are exact to about 2^-52 of pos);
+ *   k_rows : device [T] int32 or NULL: token t's key goes to row k_rows[t] of
+ *            k_out (NULL: t), and nowhere if that lies outside [0, k_cap) (e.g.
+ *            -1 for padding). Rows inside it must differ: of two tokens of
+ *            one row either's values, or a mix, remain. Other rows of k_out are
+ *            left as they are. k_cap: rows of k_out (with k_rows NULL: >= T).
+ * All four of one dtype (VSR_F32, VSR_BF16, VSR_F16), element-aligned; 16-byte
+ * aligned pointers and strides, and section sums that are multiples of 8 (fp32:
+ * 4), are fastest. k_in and k_out may both be NULL. q_out may be q_in, and
+ * k_out k_in (with k_rows NULL); other overlaps are refused, but for an output
+ * in columns of stacked rows that the input does not use. Outputs must not
+ * overlap themselves (one stride at least the other's whole extent).
+ * head_dim even, 2 to 256, >= rot; 0 <= T <= 2^30 (0: nothing is done); n_heads 1
+ * to 4096 (a NULL k: none); k_cap < 2^31; no set of heads spans over 2^46 elements. Enqueued on hip_stream, whose device must be the
+ * current one; errors via vsr_last_error(NULL). */
+int vsr_rope_axes(const vsr_rotary *rot, int32_t dtype, int32_t head_dim, int32_t T,
+                  const int32_t *pos, int64_t pos_stride, const vsr_heads *q_in,
+                  const vsr_heads *q_out, const vsr_heads *k_in, const vsr_heads *k_out,
+                  const int32_t *k_rows, int64_t k_cap, void *hip_stream);
+
+/* vsr_rope_axes on normed heads, in the same pass: every query head x becomes
+ * x / sqrt(mean(x^2) + eps) * q_gain (k_gain for keys; over all head_dim dims)
+ * before it is rotated. Statistics in fp32, one rounding at the end.
+ *   q_gain, k_gain : device [head_dim] of gain_dtype (VSR_F32, VSR_BF16 or
+ *                    VSR_F16); k_gain may be NULL with k; eps finite, >= 0. */
+int vsr_qk_norm_rope(const vsr_rotary *rot, int32_t dtype, int32_t head_dim, int32_t T,
+                     const int32_t *pos, int64_t pos_stride, const void *q_gain,
+                     const void *k_gain, int32_t gain_dtype, float eps, const vsr_heads *q_in,
+                     const vsr_heads *q_out, const vsr_heads *k_in, const vsr_heads *k_out,
+                     const int32_t *k_rows, int64_t k_cap, void *hip_stream);
+
+/* Positions of a context's prefix on several axes, for every later prefill or
+ * verify call (whose prefix must have P rows, else VSR_ESTATE): row p of the prefix
+ * sits at pos[x pos_stride + p] on axis x, token j of a candidate or branch at
+ * next + j on every axis (next: usually 1 + the largest prefix position).
+ *   rot : 2 * sum of sections == head_dim, base == the context's rope_base;
+ *         NULL: back to one axis, row p at p (pos, P and next are ignored);
+ *   pos : device, read on the context's stream.
+ * The current prefix is dropped. 1 <= P <= max_prefix. */
+int vsr_set_positions(vsr_ctx *ctx, const vsr_rotary *rot, const int32_t *pos,
+                      int64_t pos_stride, int32_t P, int32_t next);
+
+/* Norms of the query and key heads (vsr_qk_norm_rope's, with the context's
+ * rms_eps) in every layer of every later call: q_norm, k_norm are HOST arrays of
+ * n_layers device pointers to [head_dim] gains in the context's dtype (borrowed,
+ * like the weights; vsr_load_weights leaves them). Both NULL: no norms. The
+ * current prefix is dropped. */
+int vsr_load_qk_norms(vsr_ctx *ctx, const void *const *q_norm, const void *const *k_norm);
+
+/* ---- tokens under rules -----------------------------------------------------
+ *
+ * Rules of a row's pick; device pointers, NULL where a rule is not used. With c
+ * the number of v in the row's output list, "seen": v in its prompt or output:
+ *   l = logit;  seen: l = l > 0 ? l / repetition : l * repetition;
+ *   l = l - (frequency c + presence [c > 0]);  l = l + bias[v];
+ *   mask bit v clear: l = -inf,
+ * in fp32 in this order (no multiply-add fused).
+ *   repetition, presence, frequency : [rows] float; repetition > 0;
+ *   bias : float rows of vocab, bias_stride apart (0: one row for all);
+ *   mask : rows of ceil(vocab / 32) words, mask_stride words apart (0: one row
+ *          for all): bit v % 32 of word v / 32 set allows token v. */
+typedef struct vsr_token_rules {
+  const float *repetition, *presence, *frequency;
+  const float *bias;
+  int64_t bias_stride;
+  const uint32_t *mask;
+  int64_t mask_stride;
+} vsr_token_rules;
+
+/* Token lists of the rows: row r's prompt is prompt[r prompt_stride + i], i <
+ * prompt_len[r] (device [rows]; NULL: n_prompt for each; clamped to [0,
+ * n_prompt]); likewise its output (the tokens picked so far). Ids outside [0,
+ * vocab) are ignored. prompt and output may be NULL. */
+typedef struct vsr_token_lists {
+  const int32_t *prompt;
+  int64_t prompt_stride;
+  int32_t n_prompt;
+  const int32_t *prompt_len;
+  const int32_t *output;
+  int64_t output_stride;
+  int32_t n_output;
+  const int32_t *output_len;
+} vsr_token_lists;
+
+/* Bytes of device workspace vsr_pick_tokens needs (0 for invalid sizes). */
+size_t vsr_pick_workspace_size(int32_t rows, int32_t vocab);
+
+/* The greedy pick of each row of logits under the rules.
+ *   logits    : device [rows][vocab] of dtype (VSR_F32, VSR_BF16, VSR_F16), rows
+ *               stride elements apart (>= vocab);
+ *   lists, rules : HOST structs, or NULL;
+ *   processed : device float [rows][vocab] out, rows processed_stride apart: the
+ *               logits after the rules; NULL: not kept. May be logits itself
+ *               (fp32, the same stride);
+ *   token     : device [rows] int32 out, the lowest index of the largest logit
+ *               after the rules; -1 where every one is -inf (a mask that allows
+ *               nothing);
+ *   logprob   : device [rows] float out or NULL, log softmax of the logits after
+ *               the rules at that token; -inf where the token is -1. What a mask
+ *               forbids is not looked at. An allowed NaN is never picked and makes
+ *               the logprob NaN, as an allowed +inf does;
+ *   workspace : device, >= vsr_pick_workspace_size(rows, vocab) bytes, 16-byte
+ *               aligned, caller-owned; calls that overlap in time need their own.
+ * 0 <= rows <= 65535 (0: nothing is done), 1 <= vocab <= 2^24. 16-byte aligned
+ * rows are fastest. Enqueued on hip_stream, whose device must be the current
+ * one; errors via vsr_last_error(NULL). */
+int vsr_pick_tokens(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,
+                    int64_t stride, const vsr_token_lists *lists, const vsr_token_rules *rules,
+                    float *processed, int64_t processed_stride, int32_t *token, float *logprob,
+                    void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* Bytes of device workspace vsr_draft_ruled needs for M branches (0 for an
+ * invalid config or M). */
+size_t vsr_draft_ruled_workspace_size(const vsr_config *cfg, int32_t M);
+
+/* vsr_draft with every token picked by vsr_pick_tokens' rules: row m of the
+ * rules is branch m, its prompt list the branch's prompt_ids (the shared prefix
+ * is not in it), its output list the tokens it was given so far.
+ *   rules      : HOST struct or NULL; the mask of step s starts mask_step s
+ *                words past that of step 0 (0: one mask for all steps), the
+ *                other rules hold for every step;
+ *   tokens     : device [M][n_new] int32 out; a step whose mask allows nothing
+ *                gives -1, and the branch goes on from id 0;
+ *   logprobs   : device [M][n_new] float out or NULL;
+ *   workspace  : device, >= vsr_draft_ruled_workspace_size(cfg, M) bytes, 256-byte
+ *                aligned, caller-owned.
+ * Other arguments, checks and effects as vsr_draft. */
+int vsr_draft_ruled(vsr_ctx *ctx, const int32_t *prompt_ids, const int32_t *prompt_len,
+                    int32_t M, int32_t Cmax, int32_t n_new, const vsr_token_rules *rules,
+                    int64_t mask_step, int32_t *tokens, float *logprobs, void *workspace,
+                    size_t ws_bytes);
+
 /* Stage 2 and the final choice (Section 3.2, Eq. 14-15; Algorithm 1; the
  * strategies compared in Table 3). No context: the inputs are CLIP
  * embeddings, not verifier state.
@@ -257,7 +425,8 @@ int vsr_align_select(const float *ent, const float *frames, int32_t M, int32_t N
 /* Message of the last failed call on this context ("" if none). With
  * ctx == NULL: message of the last failed context-free call on this thread
  * (vsr_create, vsr_align_select, vsr_weights_to_f16, vsr_keyframes,
- * vsr_retrieve, vsr_retrieve_static). */
+ * vsr_retrieve, vsr_retrieve_static, vsr_rope_axes, vsr_qk_norm_rope,
+ * vsr_pick_tokens). */
 const char *vsr_last_error(const vsr_ctx *ctx);
 
 /* Keyframes of a video (Section 3.1, Eq. 1). Each frame is compared with the
@@ -328,7 +497,7 @@ int vsr_retrieve_static(const float *frame_emb, const int32_t *key_idx, const in
 int vsr_weights_to_f16(const void *src, void *dst, size_t n, void *hip_stream);
 
 /* Call validator, off by default. With checks set, every later vsr_prefill,
- * vsr_score, vsr_verify, vsr_reliability and vsr_draft call on the context
+ * vsr_score, vsr_verify, vsr_reliability, vsr_draft and vsr_draft_ruled call on the context
  * clears a status word in the workspace before its launches, then waits for
  * its stream and reads the word once after them (the call becomes
  * synchronous), and returns
@@ -361,7 +530,7 @@ void vsr_destroy(vsr_ctx *ctx);
  * 3 VSR_STAGE_KINDS + s (there kind 3 is the prefix rows' attention, kind 15
  * the candidate rows'; fp32 contexts do both in kind 3 and apply the norms in
  * kinds 2, 6 and 9);
- * kinds: 0 embedding, 1 RMSNorm, 2 QKV projection + rotary + cache write,
+ * kinds: 0 embedding, 1 RMSNorm (of query and key heads too), 2 QKV projection + rotary + cache write,
  * 3 attention, 4 attention merge, 5 output projection, 6 gate/up + SwiGLU,
  * 7 down projection, 8 LM-head inputs, 9 LM head + chunk LSE,
  * 10 LSE merge + target gather, 11 sum + argmax, 12 row tables, 13 copy,

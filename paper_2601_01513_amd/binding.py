@@ -24,7 +24,9 @@ VSR_RETRIEVE_STATIC_BYTES = 32 << 20
 EXPORTS = ["vsr_workspace_size", "vsr_create", "vsr_load_weights", "vsr_prefill",
            "vsr_score", "vsr_verify", "vsr_reliability", "vsr_draft", "vsr_align_select", "vsr_weights_to_f16",
            "vsr_keyframes", "vsr_retrieve_workspace_size", "vsr_retrieve", "vsr_retrieve_static",
-           "vsr_last_error",
+           "vsr_rope_axes", "vsr_qk_norm_rope", "vsr_set_positions", "vsr_load_qk_norms",
+           "vsr_pick_workspace_size", "vsr_pick_tokens", "vsr_draft_ruled_workspace_size",
+           "vsr_draft_ruled", "vsr_last_error",
            "vsr_destroy", "vsr_set_checks", "vsr_profile_enable", "vsr_profile_read"]
 
 VSR_SELECT_TWO_STAGE, VSR_SELECT_ADDITION, VSR_SELECT_INVERT = 0, 1, 2
@@ -60,6 +62,33 @@ class VsrWeights(ctypes.Structure):
     _fields_ = [("embed", ctypes.c_void_p), ("lm_head", ctypes.c_void_p),
                 ("final_norm", ctypes.c_void_p), ("attn_norm", _PP), ("wqkv", _PP),
                 ("wo", _PP), ("ffn_norm", _PP), ("wgu", _PP), ("wdown", _PP)]
+
+
+VSR_MAX_AXES = 4
+
+
+class VsrRotary(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * VSR_MAX_AXES),
+                ("interleaved", ctypes.c_int32), ("base", ctypes.c_float)]
+
+
+class VsrHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n_heads", ctypes.c_int32),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class VsrTokenRules(ctypes.Structure):
+    _fields_ = [("repetition", ctypes.c_void_p), ("presence", ctypes.c_void_p),
+                ("frequency", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("bias_stride", ctypes.c_int64), ("mask", ctypes.c_void_p),
+                ("mask_stride", ctypes.c_int64)]
+
+
+class VsrTokenLists(ctypes.Structure):
+    _fields_ = [("prompt", ctypes.c_void_p), ("prompt_stride", ctypes.c_int64),
+                ("n_prompt", ctypes.c_int32), ("prompt_len", ctypes.c_void_p),
+                ("output", ctypes.c_void_p), ("output_stride", ctypes.c_int64),
+                ("n_output", ctypes.c_int32), ("output_len", ctypes.c_void_p)]
 
 
 class VsrError(RuntimeError):
@@ -139,6 +168,30 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
     lib.vsr_retrieve_static.restype = ctypes.c_int
+    heads = [ctypes.POINTER(VsrHeads)] * 4
+    i32, i64, ptr = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
+    lib.vsr_rope_axes.argtypes = [ctypes.POINTER(VsrRotary), i32, i32, i32, ptr, i64, *heads,
+                                  ptr, i64, ptr]
+    lib.vsr_rope_axes.restype = ctypes.c_int
+    lib.vsr_qk_norm_rope.argtypes = [ctypes.POINTER(VsrRotary), i32, i32, i32, ptr, i64, ptr,
+                                     ptr, i32, ctypes.c_float, *heads, ptr, i64, ptr]
+    lib.vsr_qk_norm_rope.restype = ctypes.c_int
+    lib.vsr_set_positions.argtypes = [ptr, ctypes.POINTER(VsrRotary), ptr, i64, i32, i32]
+    lib.vsr_set_positions.restype = ctypes.c_int
+    lib.vsr_load_qk_norms.argtypes = [ptr, _PP, _PP]
+    lib.vsr_load_qk_norms.restype = ctypes.c_int
+    lib.vsr_pick_workspace_size.argtypes = [i32, i32]
+    lib.vsr_pick_workspace_size.restype = ctypes.c_size_t
+    lib.vsr_pick_tokens.argtypes = [ptr, i32, i32, i32, i64, ctypes.POINTER(VsrTokenLists),
+                                    ctypes.POINTER(VsrTokenRules), ptr, i64, ptr, ptr, ptr,
+                                    ctypes.c_size_t, ptr]
+    lib.vsr_pick_tokens.restype = ctypes.c_int
+    lib.vsr_draft_ruled_workspace_size.argtypes = [ctypes.POINTER(VsrConfig), i32]
+    lib.vsr_draft_ruled_workspace_size.restype = ctypes.c_size_t
+    lib.vsr_draft_ruled.argtypes = [ptr, ptr, ctypes.POINTER(i32), i32, i32, i32,
+                                    ctypes.POINTER(VsrTokenRules), i64, ptr, ptr, ptr,
+                                    ctypes.c_size_t]
+    lib.vsr_draft_ruled.restype = ctypes.c_int
     lib.vsr_last_error.argtypes = [ctypes.c_void_p]
     lib.vsr_last_error.restype = ctypes.c_char_p
     lib.vsr_destroy.argtypes = [ctypes.c_void_p]
@@ -226,6 +279,7 @@ class Verifier:
         if rc != VSR_OK:
             raise VsrError(rc, self.lib.vsr_last_error(None).decode())
         self.h = h
+        self._has_qk_norm = False
         self.load_weights(weights)
 
     def _check(self, rc: int):
@@ -248,6 +302,34 @@ class Verifier:
                         *[ctypes.cast(arrs[k], _PP) for k in
                           ("attn_norm", "wqkv", "wo", "ffn_norm", "wgu", "wdown")])
         self._check(self.lib.vsr_load_weights(self.h, ctypes.byref(cw)))
+        # Decoders with query/key norms carry their gains as q_norm and k_norm.
+        self._qk_norm = [[lw.get(k) for lw in w["layers"]] for k in ("q_norm", "k_norm")]
+        given = [t is not None for ts in self._qk_norm for t in ts]
+        if any(given) != all(given):
+            raise VsrError(VSR_EINVAL, "q_norm and k_norm must be given in every layer or none")
+        for t in (t for ts in self._qk_norm for t in ts if t is not None):
+            if t.numel() != self.cfg.head_dim or not t.is_contiguous() or \
+                    t.dtype != w["final_norm"].dtype:
+                raise VsrError(VSR_EINVAL, "q_norm, k_norm: contiguous [head_dim] gains in the "
+                                           "model's dtype expected")
+        if any(given) or self._has_qk_norm:
+            arrs = [(ctypes.c_void_p * L)(*map(_ptr, ts)) if any(given) else None
+                    for ts in self._qk_norm]
+            self._check(self.lib.vsr_load_qk_norms(self.h, *[ctypes.cast(a, _PP) for a in arrs]))
+        self._has_qk_norm = any(given)
+
+    def set_positions(self, rot=None, pos=None, next: int = 0):
+        """Positions of the prefix on several axes (vsr_set_positions) for the
+        next prefills: rot a rotary() scheme; pos device int32 [n_axes][P], its
+        last dim contiguous; token j after the prefix sits at next + j on every
+        axis. rot None: back to one axis, row p at p. Drops the current prefix."""
+        if rot is None:
+            self._check(self.lib.vsr_set_positions(self.h, None, None, 0, 0, 0))
+            return
+        _check_pos(rot, pos, int(pos.shape[-1]))
+        self._pos = pos
+        self._check(self.lib.vsr_set_positions(self.h, ctypes.byref(rot), _ptr(pos),
+                                               pos.stride(0), int(pos.shape[1]), int(next)))
 
     def prefill(self, visual, ids):
         """visual: device [Pv][d] (config dtype) or None; ids: device int32 [Pt] or None."""
@@ -329,6 +411,38 @@ class Verifier:
                                        _ptr(out)))
         return out
 
+    def draft_ruled(self, prompt_ids, prompt_len: Sequence[int], n_new: int, repetition=None,
+                    presence=None, frequency=None, bias=None, mask=None, out=None,
+                    workspace=None):
+        """draft() with every token picked under pick_tokens' rules (row m is
+        branch m; its prompt list is the branch's prompt, its output list the
+        tokens it got so far). mask: int32 words [1 or M][ceil(vocab/32)], or
+        [n_new][1 or M][...] with one mask a step. out: (tokens [M][n_new] int32,
+        logprobs [M][n_new] f32 or None). Returns (tokens, logprobs)."""
+        torch = self._torch
+        M, cmax = int(prompt_ids.shape[0]), int(prompt_ids.shape[1])
+        lens = (ctypes.c_int32 * M)(*[int(x) for x in prompt_len])
+        step = 0
+        if mask is not None and mask.dim() == 3:
+            if int(mask.shape[0]) != int(n_new):
+                raise VsrError(VSR_EINVAL, "mask: one row of masks a step expected")
+            step = mask.stride(0)
+            rules = _token_rules(M, self.cfg.vocab, repetition, presence, frequency, bias, mask[0])
+        else:
+            rules = _token_rules(M, self.cfg.vocab, repetition, presence, frequency, bias, mask)
+        if out is None:
+            out = (torch.empty((M, int(n_new)), dtype=torch.int32, device=self.device),
+                   torch.empty((M, int(n_new)), dtype=torch.float32, device=self.device))
+        if workspace is None:
+            size = self.lib.vsr_draft_ruled_workspace_size(ctypes.byref(self.c), M)
+            with torch.cuda.stream(self.stream):  # (reused in that stream's order)
+                workspace = torch.empty(max(size, 256), dtype=torch.uint8, device=self.device)
+        tokens, logprobs = out
+        self._check(self.lib.vsr_draft_ruled(
+            self.h, _ptr(prompt_ids), lens, M, cmax, int(n_new), ctypes.byref(rules), step,
+            _ptr(tokens), _ptr(logprobs), _ptr(workspace), workspace.numel()))
+        return tokens, logprobs
+
     def set_checks(self, ids: bool = True, finite: bool = True):
         """Call validator (vsr_set_checks): later calls wait for their stream
         and raise VsrError with code VSR_EID / VSR_ENONFINITE on a bad id or a
@@ -376,6 +490,211 @@ def weights_to_f16(t, stream=None):
     if rc != VSR_OK:
         raise VsrError(rc, lib.vsr_last_error(None).decode())
     return out
+
+
+def rotary(sections: Sequence[int], base: float, interleaved: bool = False) -> VsrRotary:
+    """A rotary scheme (vsr_rotary): sections[x] pairs of a head turn with the
+    position of axis x, in consecutive runs or with the axes in turn."""
+    n = len(sections)
+    if not 1 <= n <= VSR_MAX_AXES:
+        raise VsrError(VSR_EINVAL, "rotary: 1 to 4 sections expected")
+    return VsrRotary(n, (ctypes.c_int32 * VSR_MAX_AXES)(*sections), bool(interleaved), base)
+
+
+def _dtypes():
+    import torch
+    return {torch.float32: VSR_F32, torch.bfloat16: VSR_BF16, torch.float16: VSR_F16}
+
+
+def _check_pos(rot, pos, T):
+    import torch
+    if pos.dtype != torch.int32 or pos.dim() != 2 or int(pos.shape[0]) != rot.n_axes or \
+            int(pos.shape[1]) != T or (T > 1 and pos.stride(1) != 1):
+        raise VsrError(VSR_EINVAL, "pos: int32 [n_axes][tokens], tokens contiguous, expected")
+
+
+def _heads(t, like, n_heads, rows=None):
+    """vsr_heads of [tokens][n_heads][head_dim] on like's device, in its dtype."""
+    shape = t.shape
+    if len(shape) != 3 or t.dtype != like.dtype or t.device != like.device or \
+            shape[1] != n_heads or shape[2] != like.shape[2] or \
+            (rows is not None and shape[0] != rows):
+        raise VsrError(VSR_EINVAL, "heads: [tokens][n_heads][head_dim] tensors of one dtype, "
+                                   "device and size expected")
+    ts, hs, ds = t.stride()
+    if ds != 1:
+        raise VsrError(VSR_EINVAL, "heads: head_dim must be contiguous")
+    return VsrHeads(t.data_ptr(), n_heads, ts, hs)
+
+
+def _on_device(t, stream, call):
+    """call(stream handle) with t's device current, on `stream` or its current
+    stream."""
+    import torch
+    if not t.is_cuda:
+        raise VsrError(VSR_EINVAL, "device tensors expected")
+    st = stream if stream is not None else torch.cuda.current_stream(t.device)
+    if t.device.index == torch.cuda.current_device():
+        rc = call(st.cuda_stream)
+    else:
+        with torch.cuda.device(t.device):
+            rc = call(st.cuda_stream)
+    if rc != VSR_OK:
+        raise VsrError(rc, load_library().vsr_last_error(None).decode())
+
+
+def _rotate(rot, pos, q, k, gains, eps, q_out, k_out, k_rows, stream):
+    import torch
+    lib = load_library()
+    if q.dim() != 3 or q.dtype not in _dtypes():
+        raise VsrError(VSR_EINVAL, "heads: [tokens][n_heads][head_dim] float tensors expected")
+    T, nq, hd = q.shape
+    _check_pos(rot, pos, T)
+    if q_out is None:
+        q_out = torch.empty((T, nq, hd), dtype=q.dtype, device=q.device)
+    qi, qo = _heads(q, q, nq, T), _heads(q_out, q, nq, T)
+    ki = ko = None
+    cap = 0
+    if k is not None:
+        nk = k.shape[1] if k.dim() == 3 else 0
+        if k_out is None:
+            if k_rows is not None:
+                raise VsrError(VSR_EINVAL, "k_rows needs k_out")
+            k_out = torch.empty((T, nk, hd), dtype=k.dtype, device=k.device)
+        ki, ko = _heads(k, q, nk, T), _heads(k_out, q, nk)
+        cap = int(k_out.shape[0])
+        if k_rows is not None and (k_rows.dtype != torch.int32 or not k_rows.is_contiguous()
+                                   or k_rows.numel() != T or k_rows.device != q.device):
+            raise VsrError(VSR_EINVAL, "k_rows: contiguous int32 [tokens] expected")
+    elif k_out is not None or k_rows is not None:
+        raise VsrError(VSR_EINVAL, "k_out and k_rows need k")
+    if pos.device != q.device:
+        raise VsrError(VSR_EINVAL, "pos lies on another device")
+    dtype = _dtypes()[q.dtype]
+    tail = (ctypes.byref(qi), ctypes.byref(qo), ctypes.byref(ki) if ki else None,
+            ctypes.byref(ko) if ko else None, _ptr(k_rows), cap)
+    if gains is None:
+        _on_device(q, stream, lambda st: lib.vsr_rope_axes(
+            ctypes.byref(rot), dtype, hd, T, pos.data_ptr(), pos.stride(0), *tail, st))
+    else:
+        gq, gk = gains
+        for g in (gq, gk) if k is not None else (gq,):
+            if g is None or g.dtype != gq.dtype or g.dtype not in _dtypes() or \
+                    g.numel() != hd or not g.is_contiguous() or g.device != q.device:
+                raise VsrError(VSR_EINVAL, "gains: contiguous [head_dim] tensors of one float "
+                                           "dtype expected")
+        _on_device(q, stream, lambda st: lib.vsr_qk_norm_rope(
+            ctypes.byref(rot), dtype, hd, T, pos.data_ptr(), pos.stride(0), gq.data_ptr(),
+            _ptr(gk), _dtypes()[gq.dtype], float(eps), *tail, st))
+    return q_out, k_out
+
+
+def rope_axes(rot, pos, q, k=None, q_out=None, k_out=None, k_rows=None, stream=None):
+    """Rotary positions with several axes (vsr_rope_axes). rot: rotary(...); pos:
+    device int32 [n_axes][T]; q: [T][Hq][hd] and k: [T][Hk][hd], any token and head
+    strides (slices of stacked QKV rows). q_out, k_out: new tensors, or given ones
+    (q itself for in place; a key cache [Hk][positions][hd] as its transpose(0, 1),
+    with k_rows [T] int32 its positions, -1 to leave a key out). Returns (q_out,
+    k_out), valid once the stream is synchronised."""
+    return _rotate(rot, pos, q, k, None, 0.0, q_out, k_out, k_rows, stream)
+
+
+def qk_norm_rope(rot, pos, q, k, q_gain, k_gain, eps: float, q_out=None, k_out=None, k_rows=None,
+                 stream=None):
+    """rope_axes() on normed heads, in the same pass (vsr_qk_norm_rope): every
+    head x becomes x / sqrt(mean(x^2) + eps) * gain first. q_gain, k_gain: [hd]
+    in any float dtype."""
+    return _rotate(rot, pos, q, k, (q_gain, k_gain), eps, q_out, k_out, k_rows, stream)
+
+
+def _rows_of(t, rows, width, dtype, what):
+    """(pointer, row stride) of [1 or rows][>= width] rows; stride 0: one for all."""
+    if t is None:
+        return 0, 0
+    if t.dtype != dtype or t.dim() != 2 or t.shape[0] not in (1, rows) or \
+            t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+        raise VsrError(VSR_EINVAL, f"{what}: {dtype} [1 or {rows}][{width}] rows expected")
+    return t.data_ptr(), 0 if t.shape[0] == 1 else t.stride(0)
+
+
+def _token_rules(rows, vocab, repetition, presence, frequency, bias, mask):
+    import torch
+    for t in (repetition, presence, frequency):
+        if t is not None and (t.dtype != torch.float32 or t.numel() != rows or
+                              not t.is_contiguous()):
+            raise VsrError(VSR_EINVAL, f"penalties: contiguous float32 [{rows}] expected")
+    b, bs = _rows_of(bias, rows, vocab, torch.float32, "bias")
+    m, ms = _rows_of(mask, rows, (vocab + 31) // 32, torch.int32, "mask")
+    return VsrTokenRules(_ptr(repetition), _ptr(presence), _ptr(frequency), b, bs, m, ms)
+
+
+def _token_list(ids, length, rows, what):
+    import torch
+    if ids is None:
+        return 0, 0, 0, 0
+    if ids.dtype != torch.int32 or ids.dim() != 2 or ids.shape[0] != rows or \
+            (ids.shape[1] > 1 and ids.stride(1) != 1):
+        raise VsrError(VSR_EINVAL, f"{what}: int32 [{rows}][n] rows expected")
+    if length is not None and (length.dtype != torch.int32 or length.numel() != rows or
+                               not length.is_contiguous()):
+        raise VsrError(VSR_EINVAL, f"{what}_len: contiguous int32 [{rows}] expected")
+    return ids.data_ptr(), ids.stride(0), ids.shape[1], _ptr(length)
+
+
+def pick_tokens(logits, prompt=None, prompt_len=None, output=None, output_len=None,
+                repetition=None, presence=None, frequency=None, bias=None, mask=None,
+                processed=None, out=None, workspace=None, stream=None):
+    """The greedy pick of each row of logits under rules (vsr_pick_tokens).
+
+    logits: device [rows][vocab], float32, bfloat16 or float16, rows at any stride;
+    prompt, output: int32 [rows][n] token lists, *_len int32 [rows] (all n if None);
+    repetition, presence, frequency: float32 [rows]; bias: float32 [1 or rows][vocab];
+    mask: int32 words [1 or rows][ceil(vocab / 32)], a set bit allows its token;
+    processed: float32 [rows][vocab] to keep the logits after the rules (may be
+    logits). Returns (token [rows] int32, logprob [rows] f32), or `out`, whose
+    logprob may be None; valid once the stream is synchronised. token -1, logprob
+    -inf: no token was allowed."""
+    import torch
+    lib = load_library()
+    if logits.dim() != 2 or logits.dtype not in _dtypes() or \
+            (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise VsrError(VSR_EINVAL, "logits: float rows [rows][vocab] expected")
+    rows, vocab = logits.shape
+    dev = logits.device
+    rules = _token_rules(rows, vocab, repetition, presence, frequency, bias, mask)
+    lists = VsrTokenLists(*_token_list(prompt, prompt_len, rows, "prompt"),
+                          *_token_list(output, output_len, rows, "output"))
+    if processed is not None and (processed.dtype != torch.float32 or
+                                  processed.shape != logits.shape or
+                                  (vocab > 1 and processed.stride(1) != 1)):
+        raise VsrError(VSR_EINVAL, "processed: float32 rows of the logits' shape expected")
+    if out is None:
+        out = (torch.empty(rows, dtype=torch.int32, device=dev),
+               torch.empty(rows, dtype=torch.float32, device=dev))
+    token, logprob = out
+    if token.dtype != torch.int32 or token.numel() != rows or not token.is_contiguous() or \
+            (logprob is not None and (logprob.dtype != torch.float32 or logprob.numel() != rows
+                                      or not logprob.is_contiguous())):
+        raise VsrError(VSR_EINVAL, "out: contiguous int32 [rows] and float32 [rows] expected")
+    for t in (prompt, prompt_len, output, output_len, repetition, presence, frequency, bias,
+              mask, processed, token, logprob, workspace):
+        if t is not None and t.device != dev:
+            raise VsrError(VSR_EINVAL, "pick_tokens: tensors on different devices")
+    if workspace is None:
+        size = max(lib.vsr_pick_workspace_size(rows, vocab), 16)
+        if stream is not None:  # (reused in that stream's order)
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        else:
+            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+    # (A single row's stride is not looked at.)
+    stride = logits.stride(0) if rows > 1 else vocab
+    p_stride = processed.stride(0) if processed is not None and rows > 1 else vocab
+    _on_device(logits, stream, lambda st: lib.vsr_pick_tokens(
+        logits.data_ptr(), _dtypes()[logits.dtype], rows, vocab, stride,
+        ctypes.byref(lists), ctypes.byref(rules), _ptr(processed), p_stride, _ptr(token),
+        _ptr(logprob), _ptr(workspace), workspace.numel(), st))
+    return token, logprob
 
 
 def align_select(ent, frames, rel, delta: float, strategy: str = "two_stage", out=None,

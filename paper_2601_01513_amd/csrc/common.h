@@ -157,6 +157,85 @@ hipError_t launch_align_select(const float *ent, const float *frames, int M, int
                                const float *rel, float delta, int strategy, float *align,
                                int32_t *choice, hipStream_t s);
 
+// Rotary positions with several axes (kernels_rotary.hip): pair i < rot / 2
+// turns with the position of its axis; sections[x] pairs to axis x, in
+// consecutive runs or in turn (pair i to axis i % n_axes while it has pairs
+// left, else to axis 0).
+constexpr int kMaxAxes = 4;
+struct RotaryAxes {
+  int rot, n_axes;
+  int sections[kMaxAxes];
+  int interleaved;
+};
+// Heads [tokens][n][head_dim] in and out (may be one and the same), strides in
+// elements; lo planes: fp16 remainders (NULL: none).
+struct HeadSet {
+  const void *in, *in_lo;
+  void *out, *out_lo;
+  long in_ts, in_hs, out_ts, out_hs;
+  int n;
+  const void *gain;
+};
+struct RotateArgs {
+  HeadSet q, k;
+  int T, hd;
+  RotaryAxes axes;
+  double log2_step, step;  // angle ratio of neighbouring pairs: 2^-log2_step = step
+  const int32_t *pos;      // [n_axes] rows pos_stride apart
+  long pos_stride;
+  float eps;
+  int gain_dtype;          // VSR_* dtype of the gains
+  // Token t's key goes to row k_rows[t] of k.out (NULL: t), nowhere if that lies
+  // outside [0, k_cap); k_rows_in: it is read from that row too.
+  const int32_t *k_rows;
+  long k_cap;
+  int k_rows_in;
+  // Contexts: angles from rotary-table row row_pos[t] (NULL: t); queries are
+  // multiplied by q_scale.
+  const float2 *table;
+  const int32_t *row_pos;
+  float q_scale;
+  int lph, nsplit;  // set by the launchers
+};
+// dtype: a VSR_* value, of every tensor but the gains; norm: RMSNorm first.
+hipError_t launch_rotate_heads(const RotateArgs &a, int dtype, bool norm, hipStream_t s);
+// The norm form on a context's query rows and key cache, angles from its table
+// (fp16, with remainder planes where given, or fp32).
+hipError_t launch_norm_cached(const RotateArgs &a, bool f32, hipStream_t s);
+// Rotary table whose rows p < P hold the angles of pos[axis][p], the others those
+// of position next + p - P.
+hipError_t launch_rope_axes_table(float2 *cs, int npos, const RotaryAxes &axes, float base,
+                                  const int32_t *pos, long pos_stride, int P, int next,
+                                  hipStream_t s);
+
+// Positions 0 for n rows and one rotary-table row of no turn (half pairs): the
+// QKV epilogues given these store unrotated heads.
+hipError_t launch_no_turn(int32_t *zero_pos, long n, float2 *row, int half, hipStream_t s);
+
+// Greedy pick under rules (kernels_pick.hip): the fields of vsr_pick_tokens.
+struct PickArgs {
+  const void *logits;
+  long stride;
+  int rows, vocab;
+  const int32_t *prompt, *prompt_len, *output, *output_len;
+  long prompt_stride, output_stride;
+  int n_prompt, n_output;
+  const float *repetition, *presence, *frequency, *bias;
+  long bias_stride;
+  const uint32_t *mask;
+  long mask_stride;
+  float *processed;
+  long processed_stride;
+  int32_t *token;  // rows token_stride apart, logprob too
+  float *logprob;
+  long token_stride;
+  int32_t *next_ids;  // not NULL: [rows], the token, 0 for -1
+};
+size_t pick_workspace_bytes(int rows, int vocab);
+hipError_t launch_pick(const PickArgs &a, int dtype, void *ws, hipStream_t s);
+// len[m] = length of branch m.
+hipError_t launch_branch_lengths(const Branches &br, int32_t *len, hipStream_t s);
+
 // Retrieval stage (Eq. 1-3): histograms + keyframes, then per-keyframe top-k
 // and the merged top-K (kernels_retrieval.hip).
 hipError_t launch_keyframes(const uint8_t *frames, int NF, int H, int W, float theta,
@@ -353,6 +432,9 @@ int lmhead_chunks(int vocab);
 // its vocabulary index as int bits; the lowest index on ties).
 hipError_t gemm_lmargmax(const f16 *A, const void *W, bool w_f16, int rows, int vocab, int K,
                          float2 *part, hipStream_t s);
+// LM head that keeps the logits: logits[rows][vocab], fp32.
+hipError_t gemm_lmlogits(const f16 *A, const void *W, bool w_f16, int rows, int vocab, int K,
+                         float *logits, hipStream_t s);
 // Few-row products (rows <= kSkinnyMaxRows; N a multiple of 64, K of 32): the
 // same operands and epilogues as the GEMMs above, computed as a weight stream
 // (K split over up to kSkinnyMaxSplit slices, fp32 partials of
@@ -377,6 +459,9 @@ hipError_t skinny_qkv_rope(const f16 *A, int rows, int asplit, const void *W, bo
 int skinny_lm_chunks(int vocab);
 hipError_t skinny_lmargmax(const f16 *A, int rows, const void *W, bool w_f16, int vocab, int K,
                            float2 *part, hipStream_t s);
+// The logits themselves, [rows][vocab] (vocab a multiple of 64).
+hipError_t skinny_lmlogits(const f16 *A, int rows, const void *W, bool w_f16, int vocab, int K,
+                           float *logits, hipStream_t s);
 // Projections of at most 8 rows as one launch each, the first two with the
 // RMSNorm (gain g) of the residual rows x; for the sizes few_ok takes (att =
 // n_heads * head_dim).
@@ -463,6 +548,8 @@ hipError_t f32_lmhead(const float *A, const float *g, float eps, const int32_t *
                       const int32_t *lm_tgt, float2 *part, float *tgt_logit, hipStream_t s);
 // Greedy LM head: as gemm_lmargmax, in chunks of 64 entries.
 hipError_t f32_lmargmax(const float *A, const float *W, int rows, int vocab, int K, float2 *part,
+                        hipStream_t s);
+hipError_t f32_lmlogits(const float *A, const float *W, int rows, int vocab, int K, float *logits,
                         hipStream_t s);
 // Attention of query tokens t0 .. T-1: tokens below `split` are prefix rows
 // (causal over k / vt), the others (branch row b = t - split) see prefix keys

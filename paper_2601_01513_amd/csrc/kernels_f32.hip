@@ -55,7 +55,7 @@ __device__ __forceinline__ f32x4 ld4(const float *p, int k, int n) {
 // The tiny model's QKV projection (384 prefix + candidate rows, K 256, 768
 // columns): 9.7 us; with one thread per output and separate norms and passes
 // it took 196 + 57 + 9 us. Its whole verify pass: 2889 -> 101 us.
-enum { EPI_QKV, EPI_RESIDUAL, EPI_SWIGLU, EPI_LSE, EPI_ARGMAX };
+enum { EPI_QKV, EPI_RESIDUAL, EPI_SWIGLU, EPI_LSE, EPI_ARGMAX, EPI_LOGITS };
 
 struct F32Gemm {
   const float *A, *W;
@@ -67,7 +67,7 @@ struct F32Gemm {
   const float *h_last;
   int n_heads, n_kv, hd;  // QKV
   QKVOut<float> o;
-  float *y;  // residual stream (added to) or FFN hidden
+  float *y;  // residual stream (added to), FFN hidden or logits
   const int32_t *tgt;
   float2 *part;
   float *tgt_logit;
@@ -241,6 +241,12 @@ __global__ __launch_bounds__(256) void k_f32_gemm(F32Gemm a) {
       for (int j = 0; j < NG; ++j) {
         const int col = u0 + 16 * j + c16;
         if (row < a.rows && col < a.n) a.y[(long)row * a.n + col] += v[j];
+      }
+    } else if constexpr (EPI == EPI_LOGITS) {
+#pragma unroll
+      for (int j = 0; j < NG; ++j) {
+        const int col = u0 + 16 * j + c16;
+        if (row < a.rows && col < a.n) a.y[(long)row * a.n + col] = v[j];
       }
     } else if constexpr (EPI == EPI_LSE) {
       // The 16 lanes of a row hold its 16 NG logits of this chunk.
@@ -581,6 +587,18 @@ hipError_t f32_lmargmax(const float *A, const float *W, int rows, int vocab, int
   a.n = vocab;
   a.part = part;
   return launch_f32<EPI_ARGMAX, false>(a, s);
+}
+
+hipError_t f32_lmlogits(const float *A, const float *W, int rows, int vocab, int K, float *logits,
+                        hipStream_t s) {
+  F32Gemm a{};
+  a.A = A;
+  a.W = W;
+  a.rows = rows;
+  a.K = K;
+  a.n = vocab;
+  a.y = logits;
+  return launch_f32<EPI_LOGITS, false>(a, s);
 }
 
 hipError_t f32_attn(const F32AttnArgs &a, hipStream_t s) {

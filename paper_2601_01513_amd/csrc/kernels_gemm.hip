@@ -1429,6 +1429,38 @@ __global__ __launch_bounds__(256) void k_gemm_lmhead_4w(const f16 *__restrict__ 
   }
 }
 
+// LM head that keeps the logits (drafts under rules): the greedy variant's
+// products, stored as logits[token][vocab]. A lane holds 4 neighbouring
+// vocabulary entries of a token at a time.
+template <class TL, bool WCVT>
+__global__ __launch_bounds__(NT) void k_gemm_lmlogits(const f16 *__restrict__ Hn,
+                                                      const uint16_t *__restrict__ Wlm, int T,
+                                                      int vocab, int K, Launch ln,
+                                                      float *__restrict__ logits) {
+  __shared__ u32x4 lds[2 * TL::STAGE];
+  const Work wk = block_work(ln);
+  const int m0 = wk.tm * TL::BM, n0 = wk.tn * TL::BN;
+  f32x16 acc[TL::FM][TL::FN];
+  mainloop<TL, WCVT, false>(
+      Wlm, [=](int r) { return min(m0 + r, vocab - 1); }, Hn,
+      [=](int r) { return min(n0 + r, T - 1); }, K, 1, 0, K / BK, lds, acc);
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int wm = w / TL::WN, wn = w % TL::WN;
+#pragma unroll
+  for (int fn = 0; fn < TL::FN; ++fn) {
+    const int t = n0 + wn * TL::TN + fn * 32 + (lane & 31);
+    if (t >= T) continue;
+    float *row_t = logits + (long)t * vocab;
+#pragma unroll
+    for (int fm = 0; fm < TL::FM; ++fm)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = m0 + acc_row<TL>(wm, fm, r, lane);
+        if (row < vocab) row_t[row] = acc[fm][fn][r];
+      }
+  }
+}
+
 // Greedy variant of the LM head: per (vocab tile, token) the largest logit and
 // its vocabulary index (the lowest on ties), part[c][t] = (max, index bits).
 template <class TL, bool WCVT>
@@ -1688,6 +1720,16 @@ hipError_t gemm_lmargmax(const f16 *A, const void *W, bool w_f16, int rows, int 
   const int nm = lmhead_chunks(vocab), nn = (rows + TL::BN - 1) / TL::BN;
   const Launch ln{nm, nn, 1, nm * nn, 0, 1};
   VSR_WLAUNCH(k_gemm_lmargmax, ln.blocks(), A, W16, rows, vocab, K, ln, part);
+  return hipGetLastError();
+}
+
+hipError_t gemm_lmlogits(const f16 *A, const void *W, bool w_f16, int rows, int vocab, int K,
+                         float *logits, hipStream_t s) {
+  if (rows == 0) return hipSuccess;
+  typedef TileStd TL;
+  const int nm = lmhead_chunks(vocab), nn = (rows + TL::BN - 1) / TL::BN;
+  const Launch ln{nm, nn, 1, nm * nn, 0, 1};
+  VSR_WLAUNCH(k_gemm_lmlogits, ln.blocks(), A, W16, rows, vocab, K, ln, logits);
   return hipGetLastError();
 }
 

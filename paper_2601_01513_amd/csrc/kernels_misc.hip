@@ -115,6 +115,16 @@ hipError_t launch_draft_step(const Branches &br, int P, int S, int step, int32_t
   return hipGetLastError();
 }
 
+__global__ void k_branch_lengths(Branches br, int32_t *len) {
+  const int m = blockIdx.x * blockDim.x + threadIdx.x;
+  if (m < br.M) len[m] = br.cu[m + 1] - br.cu[m];
+}
+
+hipError_t launch_branch_lengths(const Branches &br, int32_t *len, hipStream_t s) {
+  k_branch_lengths<<<(br.M + 63) / 64, 64, 0, s>>>(br, len);
+  return hipGetLastError();
+}
+
 // Greedy pick per row from the LM-head partials (chunks in vocabulary order,
 // each holding its lowest best index): tokens[m][step] and the next inputs.
 // Block per row: threads stride over the chunks, then waves and blocks keep

@@ -687,6 +687,14 @@ hipError_t skinny_lmargmax(const f16 *A, int rows, const void *W, bool w_f16, in
   return launch_lm<SK_ARGMAX>(A, rows, W, w_f16, vocab, K, part, s, nullptr, nullptr);
 }
 
+hipError_t skinny_lmlogits(const f16 *A, int rows, const void *W, bool w_f16, int vocab, int K,
+                           float *logits, hipStream_t s) {
+  if (rows == 0) return hipSuccess;
+  if (!skinny_args_ok(rows, vocab, K, 1)) return hipErrorInvalidValue;
+  // One K slice: its partials are the products, in skinny_lmargmax's order.
+  return launch(A, rows, 1, W, w_f16, vocab, K, 1, logits, s);
+}
+
 hipError_t skinny_lmhead(const f16 *A, int rows, const void *W, bool w_f16, int vocab, int K,
                          const int32_t *lm_tgt, float2 *part, float *tgt_logit, hipStream_t s) {
   if (rows == 0) return hipSuccess;

@@ -48,7 +48,7 @@ struct Plan {
   int lm_rows;  // LM-head rows: candidate rows, or 2 per branch (reliability)
   size_t x, xn, q, q_lo, attn, h, kc, vtc, kc_lo, vtc_lo, bk, bvt, bk_lo, bvt_lo, kd, vtd,
       kd_lo, vtd_lo, part_acc, part_ml, lm_part, tgt, row_lo, row_pos, cache_row, dec_ids,
-      lm_tgt, rope, h_last, gemm_part, flags, total;
+      lm_tgt, rope, h_last, gemm_part, flags, zero_pos, no_turn, total;
 };
 
 // Returns an empty message if cfg is supported.
@@ -195,6 +195,10 @@ Plan make_plan(const vsr_config &c) {
   p.h_last = take(d * 4);
   p.gemm_part = take(gemm_part * 4);
   p.flags = take(64);
+  // Contexts with query/key norms: what makes the QKV epilogues store their
+  // heads unrotated (position 0 for every row, one table row of no turn).
+  p.zero_pos = take(R * 4);
+  p.no_turn = take((hd / 2) * 8);
   p.total = off;
   return p;
 }
@@ -213,6 +217,8 @@ struct vsr_ctx {
   int P = 0;
   const void *embed = nullptr, *lm_head = nullptr, *final_norm = nullptr;
   std::vector<const void *> attn_norm, wqkv, wo, ffn_norm, wgu, wdown;
+  std::vector<const void *> q_norm, k_norm;  // empty: no query/key norms
+  int pos_P = 0;  // prefix length of vsr_set_positions (0: one axis)
   std::string err;
 
   // Stage timing (vsr_profile_*): event pairs recorded around each launch.
@@ -373,6 +379,133 @@ extern "C" int vsr_load_weights(vsr_ctx *ctx, const vsr_weights *w) {
 
 namespace {
 
+int set_device(vsr_ctx *c) {
+  int cur = -1;
+  if (hipGetDevice(&cur) == hipSuccess && cur == c->device) return VSR_OK;
+  HIPCHECK(c, "hipSetDevice", hipSetDevice(c->device));
+  return VSR_OK;
+}
+
+// The scheme's message if it is not one, else NULL; its axes.
+const char *rotary_axes(const vsr_rotary *r, int head_dim, RotaryAxes *out) {
+  if (!r) return "rotary scheme is NULL";
+  if (r->n_axes < 1 || r->n_axes > VSR_MAX_AXES) return "n_axes must lie in [1, VSR_MAX_AXES]";
+  if (!(r->base > 0.f) || !std::isfinite(r->base)) return "base must be finite and > 0";
+  int half = 0;
+  for (int x = 0; x < r->n_axes; ++x) {
+    if (r->sections[x] < 0 || r->sections[x] > 128) return "sections must lie in [0, 128]";
+    out->sections[x] = r->sections[x];
+    half += r->sections[x];
+  }
+  if (half < 1) return "the sections hold no pair";
+  if (2 * half > head_dim) return "2 * sum of sections exceeds head_dim";
+  if (r->interleaved)
+    for (int x = 1; x < r->n_axes; ++x)
+      if (r->sections[x] > 0 && x + r->n_axes * (r->sections[x] - 1) >= half)
+        return "interleaved: an axis has more pairs than its turns";
+  out->rot = 2 * half;
+  out->n_axes = r->n_axes;
+  out->interleaved = r->interleaved != 0;
+  return nullptr;
+}
+
+}  // namespace
+
+extern "C" int vsr_set_positions(vsr_ctx *ctx, const vsr_rotary *rot, const int32_t *pos,
+                                 int64_t pos_stride, int32_t P, int32_t next) {
+  if (!ctx) return VSR_EINVAL;
+  const vsr_config &cf = ctx->cfg;
+  RotaryAxes axes{};
+  if (rot) {
+    if (const char *msg = rotary_axes(rot, cf.head_dim, &axes))
+      return ctx->fail(VSR_EINVAL, "%s", msg);
+    if (axes.rot != cf.head_dim)
+      return ctx->fail(VSR_EINVAL, "2 * sum of sections must equal head_dim");
+    if (rot->base != cf.rope_base)
+      return ctx->fail(VSR_EINVAL, "base differs from the context's rope_base");
+    if (P < 1) return ctx->fail(VSR_EINVAL, "P must be >= 1");
+    if (P > cf.max_prefix)
+      return ctx->fail(VSR_ERANGE, "P = %d exceeds max_prefix %d", P, cf.max_prefix);
+    if (!pos || (reinterpret_cast<uintptr_t>(pos) & 3))
+      return ctx->fail(VSR_EINVAL, "pos must be non-NULL and 4-byte aligned");
+    if (pos_stride < 0 || (rot->n_axes > 1 && pos_stride > 0 && pos_stride < P))
+      return ctx->fail(VSR_EINVAL, "pos_stride must be 0 or at least P");
+  }
+  if (const int rc = set_device(ctx)) return rc;
+  ctx->prefilled = false;
+  float2 *table = ctx->at<float2>(ctx->plan.rope);
+  HIPCHECK(ctx, "rotary table",
+           rot ? launch_rope_axes_table(table, ctx->plan.rope_npos, axes, cf.rope_base, pos,
+                                        pos_stride, P, next, ctx->stream)
+               : launch_rope_table(table, ctx->plan.rope_npos, cf.head_dim, cf.rope_base,
+                                   ctx->stream));
+  ctx->pos_P = rot ? P : 0;
+  return VSR_OK;
+}
+
+extern "C" int vsr_load_qk_norms(vsr_ctx *ctx, const void *const *q_norm,
+                                 const void *const *k_norm) {
+  if (!ctx) return VSR_EINVAL;
+  if (!q_norm != !k_norm)
+    return ctx->fail(VSR_EINVAL, "q_norm and k_norm must both be given or both be NULL");
+  const int L = q_norm ? ctx->cfg.n_layers : 0;
+  for (int l = 0; l < L; ++l)
+    if (!q_norm[l] || !k_norm[l])
+      return ctx->fail(VSR_EINVAL, "query/key norms: layer %d has a NULL tensor", l);
+  if (const int rc = set_device(ctx)) return rc;
+  ctx->prefilled = false;
+  if (L > 0)
+    HIPCHECK(ctx, "query/key norms",
+             launch_no_turn(ctx->at<int32_t>(ctx->plan.zero_pos), ctx->plan.rows_max,
+                            ctx->at<float2>(ctx->plan.no_turn), ctx->cfg.head_dim / 2,
+                            ctx->stream));
+  ctx->q_norm.assign(q_norm, q_norm + L);
+  ctx->k_norm.assign(k_norm, k_norm + L);
+  return VSR_OK;
+}
+
+namespace {
+
+// Query/key norms of layer l in place: the QKV epilogue stored query rows
+// row0 .. row0 + n - 1 and their keys (cache k, its remainders k_lo, capacity
+// npos) unrotated; this norms and rotates both. row_pos, cache_row as in
+// QKVOut, for these rows.
+template <typename TA>
+hipError_t norm_heads(vsr_ctx *c, int l, bool precise, int row0, int n, TA *k, TA *k_lo, int npos,
+                      const int32_t *row_pos, const int32_t *cache_row) {
+  constexpr bool kMfma = std::is_same<TA, f16>::value;
+  const vsr_config &cf = c->cfg;
+  const size_t q0 = (size_t)row0 * cf.n_heads * cf.head_dim;
+  RotateArgs a{};
+  a.q.in = a.q.out = c->at<TA>(c->plan.q) + q0;
+  a.k.in = a.k.out = k;
+  if (precise) {
+    a.q.in_lo = a.q.out_lo = c->at<TA>(c->plan.q_lo) + q0;
+    a.k.in_lo = a.k.out_lo = k_lo;
+  }
+  a.q.in_ts = a.q.out_ts = (long)cf.n_heads * cf.head_dim;
+  a.q.in_hs = a.q.out_hs = cf.head_dim;
+  a.q.n = cf.n_heads;
+  a.q.gain = c->q_norm[l];
+  a.k.in_ts = a.k.out_ts = cf.head_dim;
+  a.k.in_hs = a.k.out_hs = (long)npos * cf.head_dim;
+  a.k.n = cf.n_kv_heads;
+  a.k.gain = c->k_norm[l];
+  a.T = n;
+  a.hd = cf.head_dim;
+  a.axes.rot = cf.head_dim;
+  a.eps = cf.rms_eps;
+  a.gain_dtype = cf.dtype;
+  a.k_rows = cache_row;
+  a.k_cap = npos;
+  a.k_rows_in = cache_row != nullptr;
+  a.table = c->at<float2>(c->plan.rope);
+  a.row_pos = row_pos;
+  // The fast attention kernels take the queries pre-scaled (log2 units).
+  a.q_scale = kMfma && !precise ? 1.4426950408889634f / std::sqrt((float)cf.head_dim) : 1.f;
+  return launch_norm_cached(a, !kMfma, c->stream);
+}
+
 // One decoder block over `rows` rows whose residual stream is x. `mode` 0 is
 // the prefix (causal, caches of layer l), 1 the candidates (cascade).
 // TW is the weight type, TA the activation type (bf16 / fp16 on the MFMA
@@ -476,6 +609,13 @@ int run_layers(vsr_ctx *c, int rows, int mode, const Split &split) {
         qo.vt2_lo = bvt_lo;
       }
     }
+    const bool qk_norm = !c->q_norm.empty();
+    const int32_t *row_pos = qo.row_pos, *row_pos2 = qo.row_pos2;
+    if (qk_norm) {  // the rotation follows the norm, in a pass of its own
+      qo.rope = c->at<float2>(p.no_turn);
+      qo.row_pos = qo.row_pos2 = c->at<int32_t>(p.zero_pos);
+      qo.q_scale = 1.f;
+    }
     if constexpr (kMfma) {
       if (few_qkv)
         STAGE(c, K_QKV, "qkv projection",
@@ -489,6 +629,16 @@ int run_layers(vsr_ctx *c, int rows, int mode, const Split &split) {
     } else {
       STAGE(c, K_QKV, "qkv projection",
             f32_qkv_rope(x, attn_g, cf.rms_eps, wqkv, rows, d, Hq, Hkv, hd, qo, s));
+    }
+    if (qk_norm) {
+      const int first = fused ? P : rows;
+      STAGE(c, K_NORM, "query/key norms",
+            norm_heads<TA>(c, l, precise, 0, first, qo.k, qo.k_lo, qo.kv_npos, row_pos,
+                           cache_row));
+      if (fused)
+        STAGE(c, K_NORM, "candidate query/key norms",
+              norm_heads<TA>(c, l, precise, P, rows - P, qo.k2, qo.k2_lo, qo.kv_npos2, row_pos2,
+                             nullptr));
     }
     // The prefix's last layer only feeds the last prefix row (the hidden state
     // that predicts candidate token 0): its keys/values are needed for every
@@ -813,8 +963,19 @@ int reliability_impl(vsr_ctx *c, const Branches &br, const int32_t *ids, int yes
 // values kept in the draft cache), then n_new steps of one row per branch.
 // Each step's LM head picks the next token on the device and feeds it to the
 // next step's embedding, so the loop never waits for the host.
+// `ruled` not NULL: the head keeps its logits and the tokens are picked from them
+// under the rules.
+struct RuledDraft {
+  PickArgs pick;    // rules, prompt lists, the first step's outputs and mask
+  long mask_step;   // words from one step's mask to the next
+  float *logits;    // [M][vocab]
+  int32_t *prompt_len;
+  void *ws;         // of the pick
+};
+
 template <typename TW, typename TA>
-int draft_impl(vsr_ctx *c, const Branches &br, const int32_t *ids, int n_new, int32_t *tokens) {
+int draft_impl(vsr_ctx *c, const Branches &br, const int32_t *ids, int n_new, int32_t *tokens,
+               const RuledDraft *ruled) {
   constexpr bool kMfma = std::is_same<TA, f16>::value;
   const vsr_config &cf = c->cfg;
   const Plan &p = c->plan;
@@ -831,6 +992,31 @@ int draft_impl(vsr_ctx *c, const Branches &br, const int32_t *ids, int n_new, in
   const bool skinny_lm = kMfma && M <= kSkinnyMaxRows && skinny_lm_chunks(cf.vocab) > 0;
   const int chunks = skinny_lm ? skinny_lm_chunks(cf.vocab) : p.lm_chunks;
   auto pick = [&](int step) -> int {
+    if (ruled) {
+      if constexpr (kMfma) {
+        STAGE(c, K_LMHEAD, "draft lm head",
+              skinny_lm ? skinny_lmlogits(lm_in, M, c->lm_head, wf16, cf.vocab, cf.d_model,
+                                          ruled->logits, s)
+                        : gemm_lmlogits(lm_in, c->lm_head, wf16, M, cf.vocab, cf.d_model,
+                                        ruled->logits, s));
+      } else {
+        STAGE(c, K_LMHEAD, "draft lm head",
+              f32_lmlogits(lm_in, static_cast<const TW *>(c->lm_head), M, cf.vocab, cf.d_model,
+                           ruled->logits, s));
+      }
+      PickArgs a = ruled->pick;
+      if (step > 0 && (a.repetition || a.presence || a.frequency)) {
+        a.output = tokens;
+        a.output_stride = n_new;
+        a.n_output = step;
+      }
+      a.token = tokens + step;
+      if (a.logprob) a.logprob += step;
+      if (a.mask) a.mask += step * ruled->mask_step;
+      a.next_ids = next_ids;
+      STAGE(c, K_SELECT, "draft pick", launch_pick(a, VSR_F32, ruled->ws, s));
+      return VSR_OK;
+    }
     if constexpr (kMfma) {
       if (skinny_lm)
         STAGE(c, K_LMHEAD, "draft lm head",
@@ -847,6 +1033,8 @@ int draft_impl(vsr_ctx *c, const Branches &br, const int32_t *ids, int n_new, in
           launch_argmax_merge(part, chunks, M, n_new, step, tokens, next_ids, s));
     return VSR_OK;
   };
+  if (ruled && ruled->pick.prompt)
+    STAGE(c, K_ROWS, "draft prompt lengths", launch_branch_lengths(br, ruled->prompt_len, s));
   STAGE(c, K_ROWS, "draft rows",
         launch_draft_rows(br, c->P, p.dec_S, ids, cf.vocab, c->at<int32_t>(p.flags), row_lo,
                           row_pos, cache_row, lm_tgt, s));
@@ -878,13 +1066,6 @@ int draft_impl(vsr_ctx *c, const Branches &br, const int32_t *ids, int n_new, in
     rc = pick(step);
     if (rc) return rc;
   }
-  return VSR_OK;
-}
-
-int set_device(vsr_ctx *c) {
-  int cur = -1;
-  if (hipGetDevice(&cur) == hipSuccess && cur == c->device) return VSR_OK;
-  HIPCHECK(c, "hipSetDevice", hipSetDevice(c->device));
   return VSR_OK;
 }
 
@@ -927,6 +1108,9 @@ extern "C" int vsr_prefill(vsr_ctx *ctx, const void *visual, int32_t n_visual,
                      ctx->cfg.max_prefix);
   if (n_visual > 0 && !visual) return ctx->fail(VSR_EINVAL, "visual is NULL");
   if (n_text > 0 && !ids) return ctx->fail(VSR_EINVAL, "ids is NULL");
+  if (ctx->pos_P && P != ctx->pos_P)
+    return ctx->fail(VSR_ESTATE, "prefix length %lld, but vsr_set_positions gave %d positions", P,
+                     ctx->pos_P);
   int rc = set_device(ctx);
   if (rc) return rc;
   ctx->prefilled = false;
@@ -987,6 +1171,9 @@ extern "C" int vsr_verify(vsr_ctx *ctx, const void *visual, int32_t n_visual,
                      ctx->cfg.max_prefix);
   if (n_visual > 0 && !visual) return ctx->fail(VSR_EINVAL, "visual is NULL");
   if (n_text > 0 && !ids) return ctx->fail(VSR_EINVAL, "ids is NULL");
+  if (ctx->pos_P && P != ctx->pos_P)
+    return ctx->fail(VSR_ESTATE, "prefix length %lld, but vsr_set_positions gave %d positions", P,
+                     ctx->pos_P);
   if (M < 1 || Cmax < 1) return ctx->fail(VSR_EINVAL, "M and Cmax must be >= 1");
   if (M > ctx->cfg.max_cands)
     return ctx->fail(VSR_ERANGE, "M = %d exceeds max_cands %d", M, ctx->cfg.max_cands);
@@ -1072,9 +1259,12 @@ extern "C" int vsr_reliability(vsr_ctx *ctx, const int32_t *branch_ids,
   return checks_end(ctx, rc, lp_yes_no, 2L * M);
 }
 
-extern "C" int vsr_draft(vsr_ctx *ctx, const int32_t *prompt_ids, const int32_t *prompt_len,
-                         int32_t M, int32_t Cmax, int32_t n_new, int32_t *tokens) {
-  if (!ctx) return VSR_EINVAL;
+namespace {
+
+// vsr_draft and vsr_draft_ruled: `ruled` (NULL: greedy over the logits) is
+// complete but for its prompt lists and branch lengths.
+int draft_call(vsr_ctx *ctx, const int32_t *prompt_ids, const int32_t *prompt_len, int32_t M,
+               int32_t Cmax, int32_t n_new, int32_t *tokens, RuledDraft *ruled) {
   if (!ctx->prefilled) return ctx->fail(VSR_ESTATE, "draft before a successful prefill");
   if (ctx->cfg.max_new < 1) return ctx->fail(VSR_ESTATE, "context created with max_new = 0");
   if (M < 1 || Cmax < 1) return ctx->fail(VSR_EINVAL, "M and Cmax must be >= 1");
@@ -1101,9 +1291,99 @@ extern "C" int vsr_draft(vsr_ctx *ctx, const int32_t *prompt_ids, const int32_t 
   ctx->phase = 2;
   rc = checks_begin(ctx);
   if (rc) return rc;
-  rc = ctx->cfg.dtype == VSR_BF16 ? draft_impl<bf16, f16>(ctx, br, prompt_ids, n_new, tokens)
-                                  : draft_impl<float, float>(ctx, br, prompt_ids, n_new, tokens);
+  rc = ctx->cfg.dtype == VSR_BF16
+           ? draft_impl<bf16, f16>(ctx, br, prompt_ids, n_new, tokens, ruled)
+           : draft_impl<float, float>(ctx, br, prompt_ids, n_new, tokens, ruled);
   return checks_end(ctx, rc, nullptr, 0);
+}
+
+// Parts of a ruled draft's workspace: logits, branch lengths, the pick's partials.
+struct RuledPlan {
+  size_t prompt_len, pick, total;
+};
+RuledPlan ruled_plan(const vsr_config &c, int M) {
+  RuledPlan p;
+  p.prompt_len = align_up((size_t)M * c.vocab * 4, 256);
+  p.pick = p.prompt_len + align_up((size_t)M * 4, 256);
+  p.total = align_up(p.pick + pick_workspace_bytes(M, c.vocab), 256);
+  return p;
+}
+
+// The rules' part of PickArgs; an error message or NULL.
+const char *rules_to_pick(const vsr_token_rules *r, int vocab, PickArgs *a) {
+  if (!r) return nullptr;
+  const uintptr_t any = reinterpret_cast<uintptr_t>(r->repetition) |
+                        reinterpret_cast<uintptr_t>(r->presence) |
+                        reinterpret_cast<uintptr_t>(r->frequency) |
+                        reinterpret_cast<uintptr_t>(r->bias) | reinterpret_cast<uintptr_t>(r->mask);
+  if (any & 3) return "rules must be 4-byte aligned";
+  if (r->bias && r->bias_stride != 0 && r->bias_stride < vocab)
+    return "bias_stride must be 0 or at least vocab";
+  if (r->mask && r->mask_stride != 0 && r->mask_stride < (vocab + 31) / 32)
+    return "mask_stride must be 0 or at least ceil(vocab / 32)";
+  a->repetition = r->repetition;
+  a->presence = r->presence;
+  a->frequency = r->frequency;
+  a->bias = r->bias;
+  a->bias_stride = r->bias_stride;
+  a->mask = r->mask;
+  a->mask_stride = r->mask_stride;
+  return nullptr;
+}
+
+constexpr int kMaxPickVocab = 1 << 24, kMaxPickRows = 65535;
+
+}  // namespace
+
+extern "C" int vsr_draft(vsr_ctx *ctx, const int32_t *prompt_ids, const int32_t *prompt_len,
+                         int32_t M, int32_t Cmax, int32_t n_new, int32_t *tokens) {
+  if (!ctx) return VSR_EINVAL;
+  return draft_call(ctx, prompt_ids, prompt_len, M, Cmax, n_new, tokens, nullptr);
+}
+
+extern "C" size_t vsr_draft_ruled_workspace_size(const vsr_config *cfg, int32_t M) {
+  if (!check_config(cfg).empty() || M < 1 || M > cfg->max_cands || cfg->vocab > kMaxPickVocab)
+    return 0;
+  return ruled_plan(*cfg, M).total;
+}
+
+extern "C" int vsr_draft_ruled(vsr_ctx *ctx, const int32_t *prompt_ids,
+                               const int32_t *prompt_len, int32_t M, int32_t Cmax, int32_t n_new,
+                               const vsr_token_rules *rules, int64_t mask_step, int32_t *tokens,
+                               float *logprobs, void *workspace, size_t ws_bytes) {
+  if (!ctx) return VSR_EINVAL;
+  const vsr_config &cf = ctx->cfg;
+  if (M < 1) return ctx->fail(VSR_EINVAL, "M and Cmax must be >= 1");
+  if (M > cf.max_cands)
+    return ctx->fail(VSR_ERANGE, "M = %d exceeds max_cands %d", M, cf.max_cands);
+  if (cf.vocab > kMaxPickVocab) return ctx->fail(VSR_ERANGE, "vocab exceeds 2^24");
+  const RuledPlan p = ruled_plan(cf, M);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))
+    return ctx->fail(VSR_EINVAL, "workspace must be a non-NULL, 256-byte aligned device pointer");
+  if (ws_bytes < p.total)
+    return ctx->fail(VSR_ENOMEM, "workspace smaller than vsr_draft_ruled_workspace_size");
+  RuledDraft r{};
+  if (const char *msg = rules_to_pick(rules, cf.vocab, &r.pick))
+    return ctx->fail(VSR_EINVAL, "%s", msg);
+  if (mask_step < 0) return ctx->fail(VSR_EINVAL, "mask_step must be >= 0");
+  char *ws = static_cast<char *>(workspace);
+  r.mask_step = mask_step;
+  r.logits = reinterpret_cast<float *>(ws);
+  r.prompt_len = reinterpret_cast<int32_t *>(ws + p.prompt_len);
+  r.ws = ws + p.pick;
+  r.pick.logits = r.logits;
+  r.pick.stride = cf.vocab;
+  r.pick.rows = M;
+  r.pick.vocab = cf.vocab;
+  // Only the penalties look at the lists.
+  if (r.pick.repetition) {
+    r.pick.prompt = prompt_ids;
+    r.pick.prompt_stride = r.pick.n_prompt = Cmax;
+    r.pick.prompt_len = r.prompt_len;
+  }
+  r.pick.logprob = logprobs;
+  r.pick.token_stride = n_new;
+  return draft_call(ctx, prompt_ids, prompt_len, M, Cmax, n_new, tokens, &r);
 }
 
 extern "C" int vsr_align_select(const float *ent, const float *frames, int32_t M, int32_t NF,
@@ -1263,6 +1543,238 @@ extern "C" int vsr_weights_to_f16(const void *src, void *dst, size_t n, void *hi
                                            static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) {
     g_create_error = std::string("HIP error in weights_to_f16: ") + hipGetErrorString(e);
+    return VSR_EHIP;
+  }
+  return VSR_OK;
+}
+
+namespace {
+
+// One set of heads as the call gives it: its message if it is wrong, else NULL.
+const char *heads_error(const vsr_heads *h, size_t esize, bool out, int head_dim, long rows) {
+  if (!h->data || reinterpret_cast<uintptr_t>(h->data) % esize)
+    return "heads must be non-NULL and aligned to their element";
+  if (h->n_heads < 1 || h->n_heads > 4096) return "n_heads must lie in [1, 4096]";
+  if (h->token_stride < 0 || h->head_stride < 0) return "head strides must be >= 0";
+  if ((double)rows * h->token_stride + (double)h->n_heads * h->head_stride > 0x1p46)
+    return "heads span more than 2^46 elements";
+  if (!out) return nullptr;
+  // Token-major or head-major, nothing written twice.
+  const bool ts = rows == 1 || h->token_stride >= (h->n_heads - 1) * h->head_stride + head_dim;
+  const bool hs = h->n_heads == 1 || h->head_stride >= (rows - 1) * h->token_stride + head_dim;
+  const bool t1 = rows == 1 || h->token_stride >= head_dim;
+  const bool h1 = h->n_heads == 1 || h->head_stride >= head_dim;
+  return (ts && h1) || (hs && t1) ? nullptr : "output heads overlap themselves";
+}
+
+// Whether writing `o` (orows rows) can change what `i` (irows rows) holds.
+bool heads_clash(const vsr_heads *o, long orows, const vsr_heads *i, long irows, int head_dim,
+                 size_t esize) {
+  const auto extent = [&](const vsr_heads *h, long rows) {
+    return (size_t)((rows - 1) * h->token_stride + (h->n_heads - 1) * h->head_stride + head_dim) *
+           esize;
+  };
+  const uintptr_t a = reinterpret_cast<uintptr_t>(o->data), b = reinterpret_cast<uintptr_t>(i->data);
+  if (a + extent(o, orows) <= b || b + extent(i, irows) <= a) return false;
+  // Columns of the same stacked rows.
+  const size_t row = (size_t)o->token_stride * esize;
+  const size_t wo = extent(o, 1), wi = extent(i, 1);
+  if (o->token_stride != i->token_stride || wo > row || wi > row) return true;
+  const size_t off = a >= b ? (a - b) % row : (row - (b - a) % row) % row;
+  return !(off >= wi && off + wo <= row);
+}
+
+bool same_heads(const vsr_heads *a, const vsr_heads *b) {
+  return a->data == b->data && a->n_heads == b->n_heads && a->token_stride == b->token_stride &&
+         a->head_stride == b->head_stride;
+}
+
+void set_heads(HeadSet *s, const vsr_heads *in, const vsr_heads *out, const void *gain) {
+  s->in = in->data;
+  s->out = out->data;
+  s->in_ts = in->token_stride;
+  s->in_hs = in->head_stride;
+  s->out_ts = out->token_stride;
+  s->out_hs = out->head_stride;
+  s->n = in->n_heads;
+  s->gain = gain;
+}
+
+int rotate_call(const char *name, const vsr_rotary *rot, int32_t dtype, int32_t head_dim, int32_t T,
+                const int32_t *pos, int64_t pos_stride, bool norm, const void *q_gain,
+                const void *k_gain, int32_t gain_dtype, float eps, const vsr_heads *q_in,
+                const vsr_heads *q_out, const vsr_heads *k_in, const vsr_heads *k_out,
+                const int32_t *k_rows, int64_t k_cap, void *hip_stream) {
+  g_create_error.clear();
+  RotateArgs a{};
+  const size_t esize = dtype == VSR_F32 ? 4 : 2;
+  const auto type_ok = [](int d) { return d == VSR_F32 || d == VSR_BF16 || d == VSR_F16; };
+  const auto check = [&]() -> const char * {
+    if (!type_ok(dtype)) return "dtype must be VSR_F32, VSR_BF16 or VSR_F16";
+    if (head_dim < 2 || head_dim > 256 || head_dim % 2) return "head_dim must be even, 2 to 256";
+    if (const char *m = rotary_axes(rot, head_dim, &a.axes)) return m;
+    if (T < 0 || T > 1 << 30) return "T must lie in [0, 2^30]";
+    if (!q_in || !q_out || !k_in != !k_out) return "q_in and q_out, and k_in and k_out, go together";
+    if (norm) {
+      if (!type_ok(gain_dtype)) return "gain_dtype must be VSR_F32, VSR_BF16 or VSR_F16";
+      const uintptr_t low = gain_dtype == VSR_F32 ? 3 : 1;
+      if (!q_gain || (k_in && !k_gain) || (reinterpret_cast<uintptr_t>(q_gain) & low) ||
+          (reinterpret_cast<uintptr_t>(k_gain) & low))
+        return "gains must be non-NULL and aligned to their element";
+      if (!(eps >= 0.f) || !std::isfinite(eps)) return "eps must be finite and >= 0";
+    }
+    if (T == 0) return nullptr;
+    if (!pos || (reinterpret_cast<uintptr_t>(pos) & 3)) return "pos must be non-NULL and 4-byte aligned";
+    if (pos_stride < 0) return "pos_stride must be >= 0";
+    if (const char *m = heads_error(q_in, esize, false, head_dim, T)) return m;
+    if (const char *m = heads_error(q_out, esize, true, head_dim, T)) return m;
+    if (q_in->n_heads != q_out->n_heads) return "q_in and q_out differ in n_heads";
+    if (!same_heads(q_in, q_out) && heads_clash(q_out, T, q_in, T, head_dim, esize))
+      return "q_out overlaps q_in";
+    if (!k_in) return nullptr;
+    if (reinterpret_cast<uintptr_t>(k_rows) & 3) return "k_rows must be 4-byte aligned";
+    if (k_cap < 1 || k_cap > INT32_MAX || (!k_rows && k_cap < T))
+      return "k_cap must lie in [1, 2^31), and be >= T without k_rows";
+    const long rows = k_rows ? k_cap : T;
+    if (const char *m = heads_error(k_in, esize, false, head_dim, T)) return m;
+    if (const char *m = heads_error(k_out, esize, true, head_dim, rows)) return m;
+    if (k_in->n_heads != k_out->n_heads) return "k_in and k_out differ in n_heads";
+    if (!(same_heads(k_in, k_out) && !k_rows) &&
+        heads_clash(k_out, rows, k_in, T, head_dim, esize))
+      return "k_out overlaps k_in";
+    if (heads_clash(q_out, T, k_in, T, head_dim, esize)) return "q_out overlaps k_in";
+    if (heads_clash(k_out, rows, q_in, T, head_dim, esize)) return "k_out overlaps q_in";
+    if (heads_clash(k_out, rows, q_out, T, head_dim, esize)) return "k_out overlaps q_out";
+    return nullptr;
+  };
+  if (const char *msg = check()) {
+    g_create_error = std::string(name) + ": " + msg;
+    return VSR_EINVAL;
+  }
+  if (T == 0) return VSR_OK;
+  set_heads(&a.q, q_in, q_out, q_gain);
+  if (k_in) set_heads(&a.k, k_in, k_out, k_gain);
+  a.T = T;
+  a.hd = head_dim;
+  a.pos = pos;
+  a.pos_stride = pos_stride;
+  a.log2_step = 2.0 / a.axes.rot * std::log2((double)rot->base);
+  a.step = std::exp2(-a.log2_step);
+  a.eps = eps;
+  a.gain_dtype = gain_dtype;
+  a.k_rows = k_rows;
+  a.k_cap = k_cap;
+  a.q_scale = 1.f;
+  const hipError_t e =
+      launch_rotate_heads(a, dtype, norm, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) {
+    g_create_error = std::string("HIP error in ") + name + ": " + hipGetErrorString(e);
+    return VSR_EHIP;
+  }
+  return VSR_OK;
+}
+
+}  // namespace
+
+extern "C" int vsr_rope_axes(const vsr_rotary *rot, int32_t dtype, int32_t head_dim, int32_t T,
+                             const int32_t *pos, int64_t pos_stride, const vsr_heads *q_in,
+                             const vsr_heads *q_out, const vsr_heads *k_in,
+                             const vsr_heads *k_out, const int32_t *k_rows, int64_t k_cap,
+                             void *hip_stream) {
+  return rotate_call("rope_axes", rot, dtype, head_dim, T, pos, pos_stride, false, nullptr, nullptr,
+                     VSR_F32, 0.f, q_in, q_out, k_in, k_out, k_rows, k_cap, hip_stream);
+}
+
+extern "C" int vsr_qk_norm_rope(const vsr_rotary *rot, int32_t dtype, int32_t head_dim, int32_t T,
+                                const int32_t *pos, int64_t pos_stride, const void *q_gain,
+                                const void *k_gain, int32_t gain_dtype, float eps,
+                                const vsr_heads *q_in, const vsr_heads *q_out,
+                                const vsr_heads *k_in, const vsr_heads *k_out,
+                                const int32_t *k_rows, int64_t k_cap, void *hip_stream) {
+  return rotate_call("qk_norm_rope", rot, dtype, head_dim, T, pos, pos_stride, true, q_gain, k_gain,
+                     gain_dtype, eps, q_in, q_out, k_in, k_out, k_rows, k_cap, hip_stream);
+}
+
+extern "C" size_t vsr_pick_workspace_size(int32_t rows, int32_t vocab) {
+  if (rows < 1 || rows > kMaxPickRows || vocab < 1 || vocab > kMaxPickVocab) return 0;
+  return pick_workspace_bytes(rows, vocab);
+}
+
+extern "C" int vsr_pick_tokens(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,
+                               int64_t stride, const vsr_token_lists *lists,
+                               const vsr_token_rules *rules, float *processed,
+                               int64_t processed_stride, int32_t *token, float *logprob,
+                               void *workspace, size_t ws_bytes, void *hip_stream) {
+  g_create_error.clear();
+  PickArgs a{};
+  const auto check = [&]() -> const char * {
+    if (dtype != VSR_F32 && dtype != VSR_BF16 && dtype != VSR_F16)
+      return "dtype must be VSR_F32, VSR_BF16 or VSR_F16";
+    if (rows < 0 || rows > kMaxPickRows) return "rows must lie in [0, 65535]";
+    if (vocab < 1 || vocab > kMaxPickVocab) return "vocab must lie in [1, 2^24]";
+    if (rows == 0) return nullptr;
+    const uintptr_t esize = dtype == VSR_F32 ? 4 : 2;
+    if (!logits || !token || !workspace) return "NULL argument";
+    if (reinterpret_cast<uintptr_t>(logits) % esize) return "logits must be aligned to their element";
+    if ((reinterpret_cast<uintptr_t>(token) | reinterpret_cast<uintptr_t>(logprob) |
+         reinterpret_cast<uintptr_t>(processed)) & 3)
+      return "outputs must be 4-byte aligned";
+    if (stride < vocab || stride > (1LL << 40)) return "stride must be at least vocab";
+    if (const char *m = rules_to_pick(rules, vocab, &a)) return m;
+    if (processed) {
+      if (processed_stride < vocab || processed_stride > (1LL << 40))
+        return "processed_stride must be at least vocab";
+      const uintptr_t p = reinterpret_cast<uintptr_t>(processed),
+                      l = reinterpret_cast<uintptr_t>(logits);
+      const size_t pn = ((size_t)(rows - 1) * processed_stride + vocab) * 4,
+                   ln = ((size_t)(rows - 1) * stride + vocab) * esize;
+      if (p < l + ln && l < p + pn && !(p == l && dtype == VSR_F32 && processed_stride == stride))
+        return "processed overlaps logits";
+    }
+    if (lists) {
+      if (lists->n_prompt < 0 || lists->n_output < 0 || lists->prompt_stride < 0 ||
+          lists->output_stride < 0)
+        return "list sizes and strides must be >= 0";
+      if ((reinterpret_cast<uintptr_t>(lists->prompt) | reinterpret_cast<uintptr_t>(lists->output) |
+           reinterpret_cast<uintptr_t>(lists->prompt_len) |
+           reinterpret_cast<uintptr_t>(lists->output_len)) & 3)
+        return "lists must be 4-byte aligned";
+    }
+    if (reinterpret_cast<uintptr_t>(workspace) & 15) return "workspace must be 16-byte aligned";
+    if (ws_bytes < pick_workspace_bytes(rows, vocab))
+      return "workspace smaller than vsr_pick_workspace_size";
+    return nullptr;
+  };
+  if (const char *msg = check()) {
+    g_create_error = std::string("pick_tokens: ") + msg;
+    return VSR_EINVAL;
+  }
+  if (rows == 0) return VSR_OK;
+  a.logits = logits;
+  a.stride = stride;
+  a.rows = rows;
+  a.vocab = vocab;
+  // The lists only matter to penalties, the prompt's only to repetition.
+  if (lists && a.repetition) {
+    a.prompt = lists->n_prompt > 0 ? lists->prompt : nullptr;
+    a.prompt_stride = lists->prompt_stride;
+    a.n_prompt = lists->n_prompt;
+    a.prompt_len = lists->prompt_len;
+  }
+  if (lists && (a.repetition || a.presence || a.frequency)) {
+    a.output = lists->n_output > 0 ? lists->output : nullptr;
+    a.output_stride = lists->output_stride;
+    a.n_output = lists->n_output;
+    a.output_len = lists->output_len;
+  }
+  a.processed = processed;
+  a.processed_stride = processed_stride;
+  a.token = token;
+  a.logprob = logprob;
+  a.token_stride = 1;
+  const hipError_t e = launch_pick(a, dtype, workspace, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) {
+    g_create_error = std::string("HIP error in pick_tokens: ") + hipGetErrorString(e);
     return VSR_EHIP;
   }
   return VSR_OK;

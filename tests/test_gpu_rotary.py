@@ -1,0 +1,236 @@
+"""vsr_rope_axes and vsr_qk_norm_rope against float64: types, head sizes, axes,
+strides, slots, in place, far positions, values that pass through.
+
+Bounds, for a pair of (normed) values of length h: the output's rounding, half a
+step of its value (eps/2), plus, in units of 2^-24 h, the fp32 steps before it:
+the turn's fraction and sine (16-bit types: the vector unit's sine, 2^-20
+absolute = 16; fp32: 4), three roundings of the rotation (3) and, normed, the sum
+of squares (at most 16 terms in a lane and 6 steps over lanes, halved by the
+square root: 11), division, root and products (5); 40 covers them all. The angle
+itself is off by at most |pos| 2^-49 (products of fp64 values)."""
+import numpy as np
+import pytest
+
+from plain_decoder import axis_of_pair, rope
+
+pytestmark = pytest.mark.gpu
+
+EPS = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+
+def _torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch
+
+
+def _dt(name):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[name]
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _normed(x, gain, eps):
+    if gain is None:
+        return x
+    return x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * _np(gain)
+
+
+def _check(got, x, pos, sections, interleaved, base, dtype, gain=None, eps=1e-6):
+    y = _normed(_np(x), gain, eps)
+    axis = axis_of_pair(sections, interleaved)
+    want, half = rope(y, pos, axis, base), len(axis)
+    h = np.abs(y).copy()
+    h[..., :half] = h[..., half:2 * half] = np.hypot(y[..., :half], y[..., half:2 * half])
+    far = np.abs(pos.astype(np.float64)).max() * 2.0 ** -49
+    # (Below fp16's smallest normal number, 2^-14, its step is 2^-24.)
+    least = 2.0 ** -25 if dtype == "f16" else 0.0
+    bound = EPS[dtype] * np.abs(want) + (40 * 2.0 ** -24 + far) * h * (1 + EPS[dtype]) + least
+    off = np.abs(_np(got) - want)
+    assert got.shape == x.shape
+    assert np.all(off <= bound), (float((off / np.maximum(bound, 1e-300)).max()),)
+
+
+# T, Hq, Hk, head_dim, sections, interleaved, dtype
+CASES = [
+    (1, 1, 1, 2, (1,), False, "f32"),
+    (1, 28, 4, 128, (16, 24, 24), False, "bf16"),
+    (3, 16, 2, 128, (24, 20, 20), True, "f16"),
+    (65, 5, 5, 64, (12, 10, 10), True, "bf16"),
+    (33, 3, 1, 80, (10, 10), False, "f16"),     # a partial rotation, narrow tail
+    (17, 4, 2, 36, (5, 4), True, "f32"),        # 9 pairs and a tail of 9: element by element
+    (9, 2, 2, 6, (1, 1, 1), False, "bf16"),
+    (130, 8, 2, 256, (16, 16), False, "f32"),
+    (21, 7, 1, 256, (56, 24, 24, 24), True, "f16"),
+    (40, 2, 1, 250, (60, 65), False, "f16"),    # 125 pairs: two chunks a lane
+    (700, 14, 2, 128, (64,), False, "bf16"),
+    (5000, 6, 2, 64, (10, 0, 22), False, "f16"),  # an axis without pairs, waves of many tokens
+]
+
+
+@pytest.mark.parametrize("norm", [False, True], ids=["rope", "norm"])
+@pytest.mark.parametrize("T,hq,hk,hd,sections,interleaved,dtype", CASES)
+def test_against_float64(T, hq, hk, hd, sections, interleaved, dtype, norm):
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    g = torch.Generator(device="cuda").manual_seed(T * 7 + hd)
+    n = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    qkv = (n(T, hq + 2 * hk, hd) * 3).to(_dt(dtype))
+    q, k = qkv[:, :hq], qkv[:, hq:hq + hk]
+    pos = torch.randint(0, 40000, (len(sections), T), generator=g, device="cuda",
+                        dtype=torch.int32)
+    rot = B.rotary(sections, 1e6, interleaved)
+    if norm:
+        gq, gk = ((1 + 0.3 * n(hd)).to(_dt(dtype)) for _ in range(2))
+        qo, ko = B.qk_norm_rope(rot, pos, q, k, gq, gk, 1e-6)
+    else:
+        gq = gk = None
+        qo, ko = B.rope_axes(rot, pos, q, k)
+    p = pos.cpu().numpy()
+    _check(qo, q, p, sections, interleaved, 1e6, dtype, gq)
+    _check(ko, k, p, sections, interleaved, 1e6, dtype, gk)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_keys_into_cache_slots(dtype):
+    """Permuted slots, keys left out (-1 and past the end), other slots as they
+    were; gains in a type of their own; every layout gives the same values."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    T, hq, hk, hd, cap = 50, 12, 2, 128, 96
+    g = torch.Generator(device="cuda").manual_seed(3)
+    n = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    dt = _dt(dtype)
+    qkv = n(T, hq + 2 * hk, hd).to(dt)
+    q, k = qkv[:, :hq], qkv[:, hq:hq + hk]
+    pos = torch.randint(-5, 5000, (3, T), generator=g, device="cuda", dtype=torch.int32)
+    slots = torch.randperm(cap, generator=g, device="cuda")[:T].to(torch.int32)
+    slots[7], slots[20], slots[21] = -1, cap, 2 ** 31 - 1
+    gq, gk = (1 + 0.3 * n(hd)).to(torch.bfloat16), (1 + 0.3 * n(hd)).to(torch.bfloat16)
+    rot = B.rotary((16, 24, 24), 1e4)
+    cache = n(hk, cap, hd).to(dt)
+    before = cache.clone()
+    q1, _ = B.qk_norm_rope(rot, pos, q, k, gq, gk, 1e-5, k_out=cache.transpose(0, 1), k_rows=slots)
+    q2, k2 = B.qk_norm_rope(rot, pos, q, k, gq, gk, 1e-5)
+    torch.cuda.synchronize()
+    assert torch.equal(q1, q2)
+    _check(k2, k, pos.cpu().numpy(), (16, 24, 24), False, 1e4, dtype, gk, 1e-5)
+    kept = [t for t in range(T) if t not in (7, 20, 21)]
+    at = slots[kept].long()
+    assert torch.equal(cache[:, at], k2[kept].transpose(0, 1))
+    others = torch.ones(cap, dtype=torch.bool, device="cuda")
+    others[at] = False
+    assert torch.equal(cache[:, others], before[:, others])
+
+
+@pytest.mark.parametrize("hd,shift", [(128, 0), (128, 1), (64, 4), (36, 2)])
+def test_layouts_in_place_and_unaligned(hd, shift):
+    """In place within stacked rows, an odd element offset, padded rows, heads of
+    several strides: the values of the contiguous call, bit for bit."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    T, hq, hk = 30, 6, 2
+    g = torch.Generator(device="cuda").manual_seed(hd + shift)
+    width = (hq + 2 * hk) * hd + 24
+    flat = torch.randn(T * width + 8, generator=g, device="cuda").to(torch.bfloat16)
+    rows = flat[shift:shift + T * width].view(T, width)
+    q = rows[:, :hq * hd].view(T, hq, hd)
+    k = rows[:, hq * hd:(hq + hk) * hd].view(T, hk, hd)
+    v = rows[:, (hq + hk) * hd:].clone()
+    pos = torch.randint(0, 9000, (2, T), generator=g, device="cuda", dtype=torch.int32)
+    rot = B.rotary((hd // 4, hd // 4), 1e4, True)
+    ones = torch.ones(hd, device="cuda")
+    want_q, want_k = B.qk_norm_rope(rot, pos, q.contiguous(), k.contiguous(), ones, ones, 1e-6)
+    head_major = torch.empty((hq, T, hd), dtype=q.dtype, device="cuda").transpose(0, 1)
+    got_q, got_k = B.qk_norm_rope(rot, pos, q, k, ones, ones, 1e-6, q_out=head_major)
+    torch.cuda.synchronize()
+    # (Lanes sum a head's squares in another order where the width of a load differs.)
+    aligned = shift * 2 % 16 == 0 and hd == 128
+    same = torch.equal if aligned else \
+        lambda a, b: torch.allclose(a.float(), b.float(), rtol=2.0 ** -7, atol=0)
+    assert same(got_q, want_q) and same(got_k, want_k)
+    B.qk_norm_rope(rot, pos, q, k, ones, ones, 1e-6, q_out=q, k_out=k)
+    torch.cuda.synchronize()
+    assert torch.equal(q, got_q) and torch.equal(k, got_k)
+    assert torch.equal(rows[:, (hq + hk) * hd:], v)
+
+
+def test_far_positions_and_one_token():
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    far = [2 ** 31 - 1, -2 ** 31, 2 ** 24 + 1, 16777259, 131072, -1, 0]
+    pos = torch.tensor([far, far[::-1]], dtype=torch.int32, device="cuda")
+    q = torch.randn((len(far), 3, 64), generator=torch.Generator("cuda").manual_seed(1),
+                    device="cuda")
+    for base in (1e4, 1e6):
+        qo, none = B.rope_axes(B.rotary((16, 16), base), pos, q)
+        assert none is None
+        _check(qo, q, pos.cpu().numpy(), (16, 16), False, base, "f32")
+    one, _ = B.rope_axes(B.rotary((16, 16), 1e4), pos[:, 2:3], q[2:3])
+    _check(one, q[2:3], pos[:, 2:3].cpu().numpy(), (16, 16), False, 1e4, "f32")
+
+
+def test_nothing_to_do_and_what_passes_through():
+    """No tokens; position 0; dims past the rotation: exact values, infinities and
+    NaNs of one pair or head touching no other."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    rot = B.rotary((8, 8), 1e4)
+    empty = torch.empty((0, 4, 64), dtype=torch.float16, device="cuda")
+    out, _ = B.rope_axes(rot, torch.empty((2, 0), dtype=torch.int32, device="cuda"), empty)
+    assert out.shape == (0, 4, 64)
+    x = torch.randn((6, 4, 64), generator=torch.Generator("cuda").manual_seed(2),
+                    device="cuda").half()
+    zero = torch.zeros((2, 6), dtype=torch.int32, device="cuda")
+    out, _ = B.rope_axes(rot, zero, x)
+    assert torch.equal(out, x)
+    bad = x.clone()
+    bad[1, 2, 3] = float("inf")    # pair (3, 19)
+    bad[2, 1, 40] = float("inf")   # past the rotation
+    bad[3, 0, 63] = float("nan")
+    pos = torch.arange(12, dtype=torch.int32, device="cuda").view(2, 6) + 1
+    got, _ = B.rope_axes(rot, pos, bad)
+    ref, _ = B.rope_axes(rot, pos, x)
+    touched = torch.zeros_like(x, dtype=torch.bool)
+    touched[1, 2, 3] = touched[1, 2, 19] = touched[2, 1, 40] = touched[3, 0, 63] = True
+    assert torch.equal(got[~touched], ref[~touched])
+    assert torch.isinf(got[2, 1, 40]) and torch.isnan(got[3, 0, 63])
+    assert not torch.isfinite(got[1, 2, 3]) and not torch.isfinite(got[1, 2, 19])
+    # A head of zeros stays zero under the norm; one with an infinity is its own.
+    bad[4, 1] = 0
+    ones = torch.ones(64, device="cuda")
+    normed, _ = B.qk_norm_rope(rot, pos, bad, None, ones, None, 1e-6)
+    assert torch.equal(normed[4, 1], torch.zeros_like(normed[4, 1]))
+    assert torch.isfinite(normed[0]).all() and torch.isnan(normed[3, 0]).all()
+
+
+def test_another_stream_and_a_captured_call():
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q = torch.randn((64, 8, 128), generator=g, device="cuda").half()
+    k = torch.randn((64, 2, 128), generator=g, device="cuda").half()
+    pos = torch.arange(64, dtype=torch.int32, device="cuda").view(1, 64)
+    rot = B.rotary((64,), 1e6)
+    ones = torch.ones(128, device="cuda")
+    want = B.qk_norm_rope(rot, pos, q, k, ones, ones, 1e-6)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    outs = torch.empty_like(q), torch.empty_like(k)
+    torch.cuda.synchronize()
+    B.qk_norm_rope(rot, pos, q, k, ones, ones, 1e-6, q_out=outs[0], k_out=outs[1], stream=side)
+    side.synchronize()
+    assert all(map(torch.equal, outs, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.qk_norm_rope(rot, pos, q, k, ones, ones, 1e-6, q_out=outs[0], k_out=outs[1])
+    for _ in range(3):
+        q.copy_(torch.randn(q.shape, generator=g, device="cuda"))
+        k.copy_(torch.randn(k.shape, generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(map(torch.equal, outs, B.qk_norm_rope(rot, pos, q, k, ones, ones, 1e-6)))

@@ -1,0 +1,256 @@
+"""The three operators together, as a context uses them: prefixes with positions
+on several axes, decoders with query/key norms, drafts under rules, against the
+float64 decoder of plain_decoder.py. Per-token bounds as in the other context
+tests: 2e-2 for bf16 contexts, 1e-4 for fp32."""
+import numpy as np
+import pytest
+
+import plain_decoder as PD
+from paper_2601_01513_amd import workload as W
+
+pytestmark = pytest.mark.gpu
+
+SMALL_BF16 = W.VerifierConfig(
+    name="small bf16 L2 d256 G2 F320 V1000", n_layers=2, d_model=256, n_heads=4,
+    n_kv_heads=2, head_dim=128, d_ff=320, vocab=1000, rope_base=1e6, dtype=W.BF16,
+    n_prefix=90, n_visual=60, n_cands=5, cand_len=20)
+SMALL_F32 = W.VerifierConfig(
+    name="small fp32 L2 d64 hd32 V700", n_layers=2, d_model=64, n_heads=4, n_kv_heads=2,
+    head_dim=32, d_ff=96, vocab=700, rope_base=1e4, dtype=W.F32, n_prefix=50, n_visual=30,
+    n_cands=4, cand_len=12)
+ODD_F32 = SMALL_F32.replace(name="odd fp32 hd18", d_model=60, head_dim=18, vocab=333)
+SECTIONS = {128: (24, 20, 20), 32: (8, 4, 4), 18: (3, 3, 3)}
+
+
+def _torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch
+
+
+def _positions(cfg):
+    """Video rows on a time x 3 x 4 grid, then text on all axes: [3][P], next."""
+    t = np.arange(cfg.n_visual)
+    video = np.stack([t // 12, t // 4 % 3, t % 4])
+    first = int(video.max()) + 1
+    text = np.tile(first + np.arange(cfg.n_text), (3, 1))
+    pos = np.concatenate([video, text], 1).astype(np.int32)
+    return pos, int(pos.max()) + 1
+
+
+def _case(cfg, seed, norms, max_new=0, **kw):
+    torch = _torch()
+    from paper_2601_01513_amd.binding import Verifier
+    wl = W.make_workload(cfg, seed, device="cuda")
+    if norms:
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        for lw in wl.weights["layers"]:
+            for key in ("q_norm", "k_norm"):
+                lw[key] = (1 + 0.2 * torch.randn(cfg.head_dim, generator=g, device="cuda")).to(
+                    W.torch_dtype(cfg))
+    v = Verifier(cfg, wl.weights, device="cuda", max_new=max_new, **kw)
+    return wl, v
+
+
+def _ids(a):
+    import torch
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")
+
+
+def _place(cfg, v, interleaved):
+    from paper_2601_01513_amd import binding as B
+    pos, nxt = _positions(cfg)
+    sections = SECTIONS[cfg.head_dim]
+    v.set_positions(B.rotary(sections, cfg.rope_base, interleaved), _ids(pos), nxt)
+    return pos, nxt, PD.axis_of_pair(sections, interleaved)
+
+
+def _log_softmax(x):
+    m = x.max(-1, keepdims=True)
+    return x - m - np.log(np.exp(x - m).sum(-1, keepdims=True))
+
+
+def _candidates(cfg, wl):
+    lens = np.array([cfg.cand_len, 1, 0, cfg.cand_len // 2, 3][:cfg.n_cands])
+    return wl.cand_ids, lens
+
+
+@pytest.mark.parametrize("norms,interleaved", [(False, False), (True, True)])
+@pytest.mark.parametrize("cfg,split", [(SMALL_BF16, 0), (SMALL_BF16, 1), (SMALL_F32, None),
+                                       (ODD_F32, None)], ids=lambda x: getattr(x, "name", x))
+def test_scoring(cfg, split, norms, interleaved):
+    """prefill + score and the fused verify pass."""
+    torch = _torch()
+    wl, v = _case(cfg, 3, norms, split_layers=split)
+    pos, nxt, axis = _place(cfg, v, interleaved)
+    cand, lens = _candidates(cfg, wl)
+    hw, vis = W.host_weights(wl.weights), W.to_host_f32(wl.visual)
+    v.prefill(wl.visual, _ids(wl.prefix_ids))
+    two = [t.clone() for t in v.score(_ids(cand), lens)]
+    one = v.verify(wl.visual, _ids(wl.prefix_ids), _ids(cand), lens)
+    torch.cuda.synchronize()
+    tol = 1e-4 if cfg.dtype == W.F32 else 2e-2
+    for m in range(cfg.n_cands):
+        ids = cand[m, :lens[m]]
+        lp = _log_softmax(PD.logits_after(cfg, hw, vis, wl.prefix_ids, ids, pos, nxt, axis))
+        want = lp[np.arange(len(ids)), ids]
+        for got in (two[0], one[0]):
+            got = got[m].cpu().numpy()
+            assert np.all(got[lens[m]:] == 0)
+            assert np.all(np.abs(got[:lens[m]] - want) <= tol), np.abs(got[:lens[m]] - want).max()
+
+
+@pytest.mark.parametrize("cfg", [SMALL_BF16, SMALL_F32], ids=lambda c: c.name)
+def test_one_axis_is_what_it_was(cfg):
+    """Every axis counting rows, and one axis restored, give the plain results bit
+    for bit; so does a context whose norms were taken off again."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    wl, v = _case(cfg, 1, False)
+    cand, lens = _candidates(cfg, wl)
+    run = lambda: [t.clone() for t in v.verify(wl.visual, _ids(wl.prefix_ids), _ids(cand), lens)]  # noqa: E731
+    want = run()
+    rows = np.tile(np.arange(cfg.n_prefix), (3, 1))
+    v.set_positions(B.rotary(SECTIONS[cfg.head_dim], cfg.rope_base), _ids(rows), cfg.n_prefix)
+    assert all(map(torch.equal, run(), want))
+    _place(cfg, v, True)
+    assert not torch.equal(run()[0], want[0])
+    v.set_positions()
+    assert all(map(torch.equal, run(), want))
+    normed = dict(wl.weights, layers=[
+        dict(lw, q_norm=torch.ones(cfg.head_dim, device="cuda", dtype=W.torch_dtype(cfg)),
+             k_norm=torch.ones(cfg.head_dim, device="cuda", dtype=W.torch_dtype(cfg)))
+        for lw in wl.weights["layers"]])
+    v.load_weights(normed)
+    assert not torch.equal(run()[0], want[0])
+    v.load_weights(wl.weights)
+    assert all(map(torch.equal, run(), want))
+
+
+def test_states_and_refusals():
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    cfg = SMALL_BF16
+    wl, v = _case(cfg, 2, False, max_new=4)
+    cand, lens = _candidates(cfg, wl)
+    ids = _ids(wl.prefix_ids)
+    v.prefill(wl.visual, ids)
+    pos, nxt, _ = _place(cfg, v, False)
+    code = lambda f: pytest.raises(B.VsrError, match=f)  # noqa: E731
+    with code("prefill"):                       # the prefix was dropped
+        v.score(_ids(cand), lens)
+    with code("89"):                            # another prefix length
+        v.prefill(wl.visual, ids[:-1])
+    with code("89"):
+        v.verify(wl.visual, ids[:-1], _ids(cand), lens)
+    good = B.rotary((24, 20, 20), cfg.rope_base)
+    for rot, p in ((B.rotary((24, 20), cfg.rope_base), pos[:2]), (B.rotary((24, 20, 20), 1e4), pos),
+                   (B.rotary((10, 10, 44), cfg.rope_base, True), pos)):
+        with pytest.raises(B.VsrError):
+            v.set_positions(rot, _ids(p), nxt)
+    with code("max_prefix"):
+        v.set_positions(good, _ids(np.tile(pos, (1, 2))), nxt)
+    v.prefill(wl.visual, ids)                   # refusals changed nothing
+    prompts, plens = _ids(cand), [3] * cfg.n_cands
+    ws = torch.empty(256, dtype=torch.uint8, device="cuda")
+    with code("workspace"):
+        v.draft_ruled(prompts, plens, 2, workspace=ws)
+    with code("max_new"):
+        v.draft_ruled(prompts, plens, 5)
+    with pytest.raises(B.VsrError):
+        v.draft_ruled(prompts, plens, 2, mask=torch.zeros((3, 1, 32), dtype=torch.int32, device="cuda"))
+    # No norms, the default precise layers: as draft().
+    a = v.draft(prompts, plens, 4)
+    b, _ = v.draft_ruled(prompts, plens, 4)
+    torch.cuda.synchronize()
+    assert torch.equal(a, b)
+
+
+# Few branches at a vocabulary of whole 64s (streamed head), other vocabularies and
+# more branches (tiles), fp32.
+DRAFTS = [SMALL_BF16, SMALL_BF16.replace(name="bf16 V1024", vocab=1024),
+          SMALL_BF16.replace(name="bf16 40 branches V1024", vocab=1024, n_cands=40, cand_len=4),
+          SMALL_F32, ODD_F32]
+
+
+@pytest.mark.parametrize("cfg", DRAFTS, ids=lambda c: c.name)
+def test_without_rules_as_vsr_draft(cfg):
+    torch = _torch()
+    wl, v = _case(cfg, 5, True, max_new=6)
+    _place(cfg, v, True)
+    v.prefill(wl.visual, _ids(wl.prefix_ids))
+    lens = 1 + np.arange(cfg.n_cands) % cfg.cand_len
+    want = v.draft(_ids(wl.cand_ids), lens, 6)
+    got, _ = v.draft_ruled(_ids(wl.cand_ids), lens, 6)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("cfg", DRAFTS[:2] + DRAFTS[3:], ids=lambda c: c.name)
+def test_drafts_under_rules(cfg):
+    """Each token of the GPU's own drafts within twice the bound of the best after
+    the rules, its log-probability within the bound; masks by step, one of them
+    empty."""
+    torch = _torch()
+    n_new, M, V = 6, cfg.n_cands, cfg.vocab
+    wl, v = _case(cfg, 7, True, max_new=n_new)
+    pos, nxt, axis = _place(cfg, v, True)
+    v.prefill(wl.visual, _ids(wl.prefix_ids))
+    rng = np.random.default_rng(7)
+    lens = 1 + np.arange(M) % cfg.cand_len
+    mask = rng.integers(0, 2 ** 32, size=(n_new, M, (V + 31) // 32), dtype=np.uint32)
+    mask[2, 1] = 0
+    mask[4, 0] = 0
+    mask[4, 0, 3] = 1 << 5      # a single token
+    bias = (rng.normal(size=(M, V)) * (rng.random((M, V)) < 0.2)).astype(np.float32)
+    rep, pres, freq = (rng.uniform(a, b, M).astype(np.float32)
+                       for a, b in ((1.0, 1.5), (0, 0.5), (0, 0.3)))
+    dev = lambda a: torch.tensor(a, device="cuda")  # noqa: E731
+    tokens, logprobs = v.draft_ruled(
+        _ids(wl.cand_ids), lens, n_new, repetition=dev(rep), presence=dev(pres),
+        frequency=dev(freq), bias=dev(bias), mask=dev(mask.view(np.int32)))
+    torch.cuda.synchronize()
+    tokens, logprobs = tokens.cpu().numpy(), logprobs.cpu().numpy()
+    assert tokens[1, 2] == -1 and logprobs[1, 2] == -np.inf
+    assert tokens[0, 4] == 3 * 32 + 5 and logprobs[0, 4] == 0
+    hw, vis = W.host_weights(wl.weights), W.to_host_f32(wl.visual)
+    tol = 1e-4 if cfg.dtype == W.F32 else 2e-2
+    # (A logit within tol of the decoder's is within tol times the repetition
+    # penalty after it.)
+    tol = tol * 1.5
+    for m in range(M):
+        prompt = wl.cand_ids[m, :lens[m]]
+        x = PD.logits_after(cfg, hw, vis, wl.prefix_ids,
+                            np.concatenate([prompt, np.maximum(tokens[m, :-1], 0)]), pos, nxt,
+                            axis)[lens[m]:]
+        for s in range(n_new):
+            if m == 1 and s == 2:
+                continue
+            y = PD.apply_rules(x[s], prompt, tokens[m, :s], rep[m], pres[m], freq[m], bias[m],
+                               mask[s, m])
+            assert y.max() - y[tokens[m, s]] <= 2 * tol, (m, s)
+            assert abs(logprobs[m, s] - _log_softmax(y)[tokens[m, s]]) <= 2 * tol, (m, s)
+
+
+def test_a_shared_mask_and_prefix_calls_between():
+    """One mask for all steps and branches; scoring and reliability between drafts
+    leave them as they are."""
+    torch = _torch()
+    cfg = SMALL_BF16
+    wl, v = _case(cfg, 9, True, max_new=5)
+    _place(cfg, v, False)
+    v.prefill(wl.visual, _ids(wl.prefix_ids))
+    allowed = np.zeros(32, np.uint32)
+    allowed[[3, 10, 31]] = 0x00F0
+    mask = torch.tensor(allowed.view(np.int32), device="cuda").view(1, 32)
+    lens = [4] * cfg.n_cands
+    rep = torch.full((cfg.n_cands,), 1.2, device="cuda")
+    first = [t.clone() for t in v.draft_ruled(_ids(wl.cand_ids), lens, 5, repetition=rep, mask=mask)]
+    v.score(_ids(wl.cand_ids), [cfg.cand_len] * cfg.n_cands)
+    v.reliability(_ids(wl.cand_ids), [2] * cfg.n_cands, 1, 2, 0.05)
+    again = v.draft_ruled(_ids(wl.cand_ids), lens, 5, repetition=rep, mask=mask)
+    torch.cuda.synchronize()
+    assert all(map(torch.equal, first, again))
+    t = first[0].cpu().numpy()
+    assert np.all((allowed[t // 32] >> (t % 32).astype(np.uint32)) & 1 == 1)
