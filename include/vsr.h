@@ -273,9 +273,8 @@ typedef struct vsr_heads {
  *            -1 for padding). Rows inside it must differ: of two tokens of
  *            one row either's values, or a mix, remain. Other rows of k_out are
  *            left as they are. k_cap: rows of k_out (with k_rows NULL: >= T).
- * All four of one dtype (VSR_F32, VSR_BF16, VSR_F16), element-aligned; 16-byte
- * aligned pointers and strides, and section sums that are multiples of 8 (fp32:
- * 4), are fastest. k_in and k_out may both be NULL. q_out may be q_in, and
+ * All four of one dtype (VSR_F32, VSR_BF16, VSR_F16), element-aligned; rot / 2 and
+ * (head_dim - rot) / 2 that are multiples of 8 (fp32: 4) are fastest. k_in and k_out may both be NULL. q_out may be q_in, and
  * k_out k_in (with k_rows NULL); other overlaps are refused, but for an output
  * in columns of stacked rows that the input does not use. Outputs must not
  * overlap themselves (one stride at least the other's whole extent).
@@ -370,9 +369,9 @@ size_t vsr_pick_workspace_size(int32_t rows, int32_t vocab);
  *               the logprob NaN, as an allowed +inf does;
  *   workspace : device, >= vsr_pick_workspace_size(rows, vocab) bytes, 16-byte
  *               aligned, caller-owned; calls that overlap in time need their own.
- * 0 <= rows <= 65535 (0: nothing is done), 1 <= vocab <= 2^24. 16-byte aligned
- * rows are fastest. Enqueued on hip_stream, whose device must be the current
- * one; errors via vsr_last_error(NULL). */
+ * 0 <= rows <= 65535 (0: nothing is done), 1 <= vocab <= 2^24.
+ * Enqueued on hip_stream, whose device must be the current one; errors via
+ * vsr_last_error(NULL). */
 int vsr_pick_tokens(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,
                     int64_t stride, const vsr_token_lists *lists, const vsr_token_rules *rules,
                     float *processed, int64_t processed_stride, int32_t *token, float *logprob,

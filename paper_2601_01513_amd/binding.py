@@ -326,7 +326,7 @@ class Verifier:
         if rot is None:
             self._check(self.lib.vsr_set_positions(self.h, None, None, 0, 0, 0))
             return
-        _check_pos(rot, pos, int(pos.shape[-1]))
+        _check_pos(_torch_names(), rot, pos, int(pos.shape[-1]), pos.get_device())
         self._pos = pos
         self._check(self.lib.vsr_set_positions(self.h, ctypes.byref(rot), _ptr(pos),
                                                pos.stride(0), int(pos.shape[1]), int(next)))
@@ -422,21 +422,22 @@ class Verifier:
         torch = self._torch
         M, cmax = int(prompt_ids.shape[0]), int(prompt_ids.shape[1])
         lens = (ctypes.c_int32 * M)(*[int(x) for x in prompt_len])
-        step = 0
+        step, dev = 0, prompt_ids.get_device()
         if mask is not None and mask.dim() == 3:
             if int(mask.shape[0]) != int(n_new):
                 raise VsrError(VSR_EINVAL, "mask: one row of masks a step expected")
             step = mask.stride(0)
-            rules = _token_rules(M, self.cfg.vocab, repetition, presence, frequency, bias, mask[0])
+            rules = _token_rules(torch, M, self.cfg.vocab, dev, repetition, presence, frequency,
+                                 bias, mask[0])
         else:
-            rules = _token_rules(M, self.cfg.vocab, repetition, presence, frequency, bias, mask)
+            rules = _token_rules(torch, M, self.cfg.vocab, dev, repetition, presence, frequency,
+                                 bias, mask)
         if out is None:
             out = (torch.empty((M, int(n_new)), dtype=torch.int32, device=self.device),
                    torch.empty((M, int(n_new)), dtype=torch.float32, device=self.device))
         if workspace is None:
             size = self.lib.vsr_draft_ruled_workspace_size(ctypes.byref(self.c), M)
-            with torch.cuda.stream(self.stream):  # (reused in that stream's order)
-                workspace = torch.empty(max(size, 256), dtype=torch.uint8, device=self.device)
+            workspace = _empty(torch, max(size, 256), torch.uint8, self.device, self.stream)
         tokens, logprobs = out
         self._check(self.lib.vsr_draft_ruled(
             self.h, _ptr(prompt_ids), lens, M, cmax, int(n_new), ctypes.byref(rules), step,
@@ -501,92 +502,111 @@ def rotary(sections: Sequence[int], base: float, interleaved: bool = False) -> V
     return VsrRotary(n, (ctypes.c_int32 * VSR_MAX_AXES)(*sections), bool(interleaved), base)
 
 
-def _dtypes():
+_float_types = None  # torch float dtype -> VSR_*
+_raw_stream = None   # device index -> its current stream's handle
+
+
+def _torch_names():
+    """torch (imported on first use), with the library and the two names above set."""
+    global _float_types, _raw_stream
     import torch
-    return {torch.float32: VSR_F32, torch.bfloat16: VSR_BF16, torch.float16: VSR_F16}
+    if _float_types is None:
+        load_library()
+        _float_types = {torch.float32: VSR_F32, torch.bfloat16: VSR_BF16, torch.float16: VSR_F16}
+        # (A Stream object takes longer to make than a call's whole argument list.)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return torch
 
 
-def _check_pos(rot, pos, T):
-    import torch
-    if pos.dtype != torch.int32 or pos.dim() != 2 or int(pos.shape[0]) != rot.n_axes or \
-            int(pos.shape[1]) != T or (T > 1 and pos.stride(1) != 1):
-        raise VsrError(VSR_EINVAL, "pos: int32 [n_axes][tokens], tokens contiguous, expected")
-
-
-def _heads(t, like, n_heads, rows=None):
-    """vsr_heads of [tokens][n_heads][head_dim] on like's device, in its dtype."""
-    shape = t.shape
-    if len(shape) != 3 or t.dtype != like.dtype or t.device != like.device or \
-            shape[1] != n_heads or shape[2] != like.shape[2] or \
-            (rows is not None and shape[0] != rows):
-        raise VsrError(VSR_EINVAL, "heads: [tokens][n_heads][head_dim] tensors of one dtype, "
-                                   "device and size expected")
-    ts, hs, ds = t.stride()
-    if ds != 1:
-        raise VsrError(VSR_EINVAL, "heads: head_dim must be contiguous")
-    return VsrHeads(t.data_ptr(), n_heads, ts, hs)
-
-
-def _on_device(t, stream, call):
-    """call(stream handle) with t's device current, on `stream` or its current
-    stream."""
-    import torch
-    if not t.is_cuda:
+def _call(torch, dev, stream, f, args):
+    """f(*args, stream handle) with device index dev current, on `stream` or dev's
+    current stream."""
+    if dev < 0:
         raise VsrError(VSR_EINVAL, "device tensors expected")
-    st = stream if stream is not None else torch.cuda.current_stream(t.device)
-    if t.device.index == torch.cuda.current_device():
-        rc = call(st.cuda_stream)
+    st = stream.cuda_stream if stream is not None else _raw_stream(dev)
+    if dev == torch.cuda.current_device():
+        rc = f(*args, st)
     else:
-        with torch.cuda.device(t.device):
-            rc = call(st.cuda_stream)
+        with torch.cuda.device(dev):
+            rc = f(*args, st)
     if rc != VSR_OK:
         raise VsrError(rc, load_library().vsr_last_error(None).decode())
 
 
+def _check_pos(torch, rot, pos, T, dev):
+    """pos's axis stride."""
+    if pos.dim() == 2 and pos.dtype is torch.int32 and pos.get_device() == dev:
+        n, t = pos.shape
+        axis, token = pos.stride()
+        if n == rot.n_axes and t == T and (token == 1 or T <= 1):
+            return axis
+    raise VsrError(VSR_EINVAL, "pos: int32 [n_axes][tokens] on the heads' device, tokens "
+                               "contiguous, expected")
+
+
+def _heads(t, dtype, hd, dev, rows):
+    """vsr_heads of t, [rows][n_heads][hd] (rows < 0: any) of dtype on device dev."""
+    if t.dim() == 3 and t.dtype is dtype and t.get_device() == dev:
+        n, heads, d = t.shape
+        ts, hs, ds = t.stride()
+        if d == hd and ds == 1 and (n == rows or rows < 0):
+            return VsrHeads(t.data_ptr(), heads, ts, hs)
+    raise VsrError(VSR_EINVAL, "heads: [tokens][n_heads][head_dim] tensors of one dtype, device "
+                               "and size, head_dim contiguous, expected")
+
+
 def _rotate(rot, pos, q, k, gains, eps, q_out, k_out, k_rows, stream):
-    import torch
-    lib = load_library()
-    if q.dim() != 3 or q.dtype not in _dtypes():
+    torch = _torch_names()
+    dtype, dev = q.dtype, q.get_device()
+    vsr_dtype = _float_types.get(dtype)
+    if vsr_dtype is None or q.dim() != 3:
         raise VsrError(VSR_EINVAL, "heads: [tokens][n_heads][head_dim] float tensors expected")
     T, nq, hd = q.shape
-    _check_pos(rot, pos, T)
+    pos_stride = _check_pos(torch, rot, pos, T, dev)
     if q_out is None:
-        q_out = torch.empty((T, nq, hd), dtype=q.dtype, device=q.device)
-    qi, qo = _heads(q, q, nq, T), _heads(q_out, q, nq, T)
-    ki = ko = None
+        q_out = _empty(torch, (T, nq, hd), dtype, q.device, stream)
+    qi, qo = _heads(q, dtype, hd, dev, T), _heads(q_out, dtype, hd, dev, T)
+    ki = ko = rows = None
     cap = 0
     if k is not None:
-        nk = k.shape[1] if k.dim() == 3 else 0
         if k_out is None:
             if k_rows is not None:
                 raise VsrError(VSR_EINVAL, "k_rows needs k_out")
-            k_out = torch.empty((T, nk, hd), dtype=k.dtype, device=k.device)
-        ki, ko = _heads(k, q, nk, T), _heads(k_out, q, nk)
-        cap = int(k_out.shape[0])
-        if k_rows is not None and (k_rows.dtype != torch.int32 or not k_rows.is_contiguous()
-                                   or k_rows.numel() != T or k_rows.device != q.device):
-            raise VsrError(VSR_EINVAL, "k_rows: contiguous int32 [tokens] expected")
+            k_out = _empty(torch, k.shape, k.dtype, k.device, stream)
+        ki = ctypes.byref(_heads(k, dtype, hd, dev, T))
+        ko = ctypes.byref(_heads(k_out, dtype, hd, dev, -1))
+        cap = k_out.size(0)
+        if k_rows is not None:
+            if k_rows.dtype is not torch.int32 or k_rows.numel() != T or \
+                    not k_rows.is_contiguous() or k_rows.get_device() != dev:
+                raise VsrError(VSR_EINVAL, "k_rows: contiguous int32 [tokens] expected")
+            rows = k_rows.data_ptr()
     elif k_out is not None or k_rows is not None:
         raise VsrError(VSR_EINVAL, "k_out and k_rows need k")
-    if pos.device != q.device:
-        raise VsrError(VSR_EINVAL, "pos lies on another device")
-    dtype = _dtypes()[q.dtype]
-    tail = (ctypes.byref(qi), ctypes.byref(qo), ctypes.byref(ki) if ki else None,
-            ctypes.byref(ko) if ko else None, _ptr(k_rows), cap)
+    head = (ctypes.byref(rot), vsr_dtype, hd, T, pos.data_ptr(), pos_stride)
+    tail = (ctypes.byref(qi), ctypes.byref(qo), ki, ko, rows, cap)
     if gains is None:
-        _on_device(q, stream, lambda st: lib.vsr_rope_axes(
-            ctypes.byref(rot), dtype, hd, T, pos.data_ptr(), pos.stride(0), *tail, st))
-    else:
-        gq, gk = gains
-        for g in (gq, gk) if k is not None else (gq,):
-            if g is None or g.dtype != gq.dtype or g.dtype not in _dtypes() or \
-                    g.numel() != hd or not g.is_contiguous() or g.device != q.device:
-                raise VsrError(VSR_EINVAL, "gains: contiguous [head_dim] tensors of one float "
-                                           "dtype expected")
-        _on_device(q, stream, lambda st: lib.vsr_qk_norm_rope(
-            ctypes.byref(rot), dtype, hd, T, pos.data_ptr(), pos.stride(0), gq.data_ptr(),
-            _ptr(gk), _dtypes()[gq.dtype], float(eps), *tail, st))
+        _call(torch, dev, stream, _lib.vsr_rope_axes, head + tail)
+        return q_out, k_out
+    gq, gk = gains
+    for g in gains if k is not None else gains[:1]:
+        if g is None or g.dtype is not gq.dtype or g.numel() != hd or \
+                not g.is_contiguous() or g.get_device() != dev:
+            raise VsrError(VSR_EINVAL, "gains: contiguous [head_dim] tensors of one float dtype "
+                                       "expected")
+    _call(torch, dev, stream, _lib.vsr_qk_norm_rope,
+          head + (gq.data_ptr(), _ptr(gk), _float_types.get(gq.dtype, -1), eps) + tail)
     return q_out, k_out
+
+
+def _empty(torch, shape, dtype, device, stream):
+    """torch.empty whose memory is reused in `stream`'s order (None: the current
+    stream's)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def rope_axes(rot, pos, q, k=None, q_out=None, k_out=None, k_rows=None, stream=None):
@@ -607,38 +627,51 @@ def qk_norm_rope(rot, pos, q, k, q_gain, k_gain, eps: float, q_out=None, k_out=N
     return _rotate(rot, pos, q, k, (q_gain, k_gain), eps, q_out, k_out, k_rows, stream)
 
 
-def _rows_of(t, rows, width, dtype, what):
-    """(pointer, row stride) of [1 or rows][>= width] rows; stride 0: one for all."""
+def _rows_of(t, rows, width, dtype, dev, what):
+    """(pointer, row stride) of [1 or rows][width] rows; stride 0: one for all."""
     if t is None:
-        return 0, 0
-    if t.dtype != dtype or t.dim() != 2 or t.shape[0] not in (1, rows) or \
-            t.shape[1] != width or (width > 1 and t.stride(1) != 1):
-        raise VsrError(VSR_EINVAL, f"{what}: {dtype} [1 or {rows}][{width}] rows expected")
-    return t.data_ptr(), 0 if t.shape[0] == 1 else t.stride(0)
+        return None, 0
+    if t.dim() == 2 and t.dtype is dtype and t.get_device() == dev:
+        n, w = t.shape
+        stride, step = t.stride()
+        if w == width and (step == 1 or width == 1) and (n == rows or n == 1):
+            return t.data_ptr(), 0 if n == 1 else stride
+    raise VsrError(VSR_EINVAL, f"{what}: {dtype} [1 or {rows}][{width}] rows on the logits' device "
+                               "expected")
 
 
-def _token_rules(rows, vocab, repetition, presence, frequency, bias, mask):
-    import torch
-    for t in (repetition, presence, frequency):
-        if t is not None and (t.dtype != torch.float32 or t.numel() != rows or
-                              not t.is_contiguous()):
-            raise VsrError(VSR_EINVAL, f"penalties: contiguous float32 [{rows}] expected")
-    b, bs = _rows_of(bias, rows, vocab, torch.float32, "bias")
-    m, ms = _rows_of(mask, rows, (vocab + 31) // 32, torch.int32, "mask")
-    return VsrTokenRules(_ptr(repetition), _ptr(presence), _ptr(frequency), b, bs, m, ms)
+def _penalty(t, rows, dtype, dev):
+    if t is None:
+        return None
+    if t.dtype is dtype and t.numel() == rows and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
+    raise VsrError(VSR_EINVAL, f"penalties: contiguous float32 [{rows}] on the logits' device "
+                               "expected")
 
 
-def _token_list(ids, length, rows, what):
-    import torch
+def _token_rules(torch, rows, vocab, dev, repetition, presence, frequency, bias, mask):
+    f32 = torch.float32
+    return VsrTokenRules(_penalty(repetition, rows, f32, dev), _penalty(presence, rows, f32, dev),
+                         _penalty(frequency, rows, f32, dev),
+                         *_rows_of(bias, rows, vocab, f32, dev, "bias"),
+                         *_rows_of(mask, rows, (vocab + 31) // 32, torch.int32, dev, "mask"))
+
+
+def _token_list(torch, ids, length, rows, dev, what):
     if ids is None:
-        return 0, 0, 0, 0
-    if ids.dtype != torch.int32 or ids.dim() != 2 or ids.shape[0] != rows or \
-            (ids.shape[1] > 1 and ids.stride(1) != 1):
-        raise VsrError(VSR_EINVAL, f"{what}: int32 [{rows}][n] rows expected")
-    if length is not None and (length.dtype != torch.int32 or length.numel() != rows or
-                               not length.is_contiguous()):
-        raise VsrError(VSR_EINVAL, f"{what}_len: contiguous int32 [{rows}] expected")
-    return ids.data_ptr(), ids.stride(0), ids.shape[1], _ptr(length)
+        return None, 0, 0, None
+    i32 = torch.int32
+    if ids.dim() == 2 and ids.dtype is i32 and ids.get_device() == dev:
+        r, n = ids.shape
+        stride, step = ids.stride()
+        if r == rows and (step == 1 or n <= 1):
+            if length is None:
+                return ids.data_ptr(), stride, n, None
+            if length.dtype is i32 and length.numel() == rows and length.is_contiguous() and \
+                    length.get_device() == dev:
+                return ids.data_ptr(), stride, n, length.data_ptr()
+    raise VsrError(VSR_EINVAL, f"{what}: int32 [{rows}][n] rows, {what}_len contiguous int32 "
+                               f"[{rows}], on the logits' device, expected")
 
 
 def pick_tokens(logits, prompt=None, prompt_len=None, output=None, output_len=None,
@@ -654,46 +687,50 @@ def pick_tokens(logits, prompt=None, prompt_len=None, output=None, output_len=No
     logits). Returns (token [rows] int32, logprob [rows] f32), or `out`, whose
     logprob may be None; valid once the stream is synchronised. token -1, logprob
     -inf: no token was allowed."""
-    import torch
-    lib = load_library()
-    if logits.dim() != 2 or logits.dtype not in _dtypes() or \
-            (logits.shape[1] > 1 and logits.stride(1) != 1):
+    torch = _torch_names()
+    lib = _lib
+    dtype = _float_types.get(logits.dtype)
+    if dtype is None or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise VsrError(VSR_EINVAL, "logits: float rows [rows][vocab] expected")
     rows, vocab = logits.shape
-    dev = logits.device
-    rules = _token_rules(rows, vocab, repetition, presence, frequency, bias, mask)
-    lists = VsrTokenLists(*_token_list(prompt, prompt_len, rows, "prompt"),
-                          *_token_list(output, output_len, rows, "output"))
-    if processed is not None and (processed.dtype != torch.float32 or
-                                  processed.shape != logits.shape or
-                                  (vocab > 1 and processed.stride(1) != 1)):
-        raise VsrError(VSR_EINVAL, "processed: float32 rows of the logits' shape expected")
-    if out is None:
-        out = (torch.empty(rows, dtype=torch.int32, device=dev),
-               torch.empty(rows, dtype=torch.float32, device=dev))
-    token, logprob = out
-    if token.dtype != torch.int32 or token.numel() != rows or not token.is_contiguous() or \
-            (logprob is not None and (logprob.dtype != torch.float32 or logprob.numel() != rows
-                                      or not logprob.is_contiguous())):
-        raise VsrError(VSR_EINVAL, "out: contiguous int32 [rows] and float32 [rows] expected")
-    for t in (prompt, prompt_len, output, output_len, repetition, presence, frequency, bias,
-              mask, processed, token, logprob, workspace):
-        if t is not None and t.device != dev:
-            raise VsrError(VSR_EINVAL, "pick_tokens: tensors on different devices")
-    if workspace is None:
-        size = max(lib.vsr_pick_workspace_size(rows, vocab), 16)
-        if stream is not None:  # (reused in that stream's order)
-            with torch.cuda.stream(stream):
-                workspace = torch.empty(size, dtype=torch.uint8, device=dev)
-        else:
-            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+    dev = logits.get_device()
+    rules = lists = None
+    if not (repetition is presence is frequency is bias is mask is None):
+        rules = ctypes.byref(_token_rules(torch, rows, vocab, dev, repetition, presence,
+                                          frequency, bias, mask))
+    if not (prompt is output is None):
+        lists = ctypes.byref(VsrTokenLists(
+            *_token_list(torch, prompt, prompt_len, rows, dev, "prompt"),
+            *_token_list(torch, output, output_len, rows, dev, "output")))
     # (A single row's stride is not looked at.)
     stride = logits.stride(0) if rows > 1 else vocab
-    p_stride = processed.stride(0) if processed is not None and rows > 1 else vocab
-    _on_device(logits, stream, lambda st: lib.vsr_pick_tokens(
-        logits.data_ptr(), _dtypes()[logits.dtype], rows, vocab, stride,
-        ctypes.byref(lists), ctypes.byref(rules), _ptr(processed), p_stride, _ptr(token),
-        _ptr(logprob), _ptr(workspace), workspace.numel(), st))
+    kept, kept_stride = None, 0
+    if processed is not None:
+        if processed.dtype is not torch.float32 or processed.shape != logits.shape or \
+                (vocab > 1 and processed.stride(1) != 1) or processed.get_device() != dev:
+            raise VsrError(VSR_EINVAL, "processed: float32 rows of the logits' shape and device "
+                                       "expected")
+        kept, kept_stride = processed.data_ptr(), processed.stride(0) if rows > 1 else vocab
+    if out is None:
+        out = (_empty(torch, rows, torch.int32, logits.device, stream),
+               _empty(torch, rows, torch.float32, logits.device, stream))
+    token, logprob = out
+    if token.dtype is not torch.int32 or token.numel() != rows or not token.is_contiguous() or \
+            token.get_device() != dev or \
+            (logprob is not None and (logprob.dtype is not torch.float32 or
+                                      logprob.numel() != rows or not logprob.is_contiguous() or
+                                      logprob.get_device() != dev)):
+        raise VsrError(VSR_EINVAL, "out: contiguous int32 [rows] and float32 [rows] on the logits' "
+                                   "device expected")
+    if workspace is None:
+        workspace = _empty(torch, max(lib.vsr_pick_workspace_size(rows, vocab), 16), torch.uint8,
+                           logits.device, stream)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise VsrError(VSR_EINVAL, "workspace: contiguous tensor on the logits' device expected")
+    _call(torch, dev, stream, lib.vsr_pick_tokens,
+          (logits.data_ptr(), dtype, rows, vocab, stride, lists, rules, kept, kept_stride,
+           token.data_ptr(), _ptr(logprob), workspace.data_ptr(),
+           workspace.numel() * workspace.element_size()))
     return token, logprob
 
 

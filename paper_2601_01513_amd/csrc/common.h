@@ -157,15 +157,17 @@ hipError_t launch_align_select(const float *ent, const float *frames, int M, int
                                const float *rel, float delta, int strategy, float *align,
                                int32_t *choice, hipStream_t s);
 
+// Outputs above this many bytes are gone from the caches (32 MB of L2) before
+// their reader comes.
+constexpr long kCachedBytes = 64L << 20;
+
 // Rotary positions with several axes (kernels_rotary.hip): pair i < rot / 2
-// turns with the position of its axis; sections[x] pairs to axis x, in
-// consecutive runs or in turn (pair i to axis i % n_axes while it has pairs
-// left, else to axis 0).
+// turns with the position of its axis, 2 bits of a map (16 pairs a word).
 constexpr int kMaxAxes = 4;
+constexpr int kAxisWords = 8;  // head_dim <= 256: up to 128 pairs
 struct RotaryAxes {
   int rot, n_axes;
-  int sections[kMaxAxes];
-  int interleaved;
+  uint32_t map[kAxisWords];
 };
 // Heads [tokens][n][head_dim] in and out (may be one and the same), strides in
 // elements; lo planes: fp16 remainders (NULL: none).
@@ -176,26 +178,30 @@ struct HeadSet {
   int n;
   const void *gain;
 };
+constexpr int kStepBits = 7;  // (of a pair's index)
 struct RotateArgs {
   HeadSet q, k;
   int T, hd;
   RotaryAxes axes;
-  double log2_step, step;  // angle ratio of neighbouring pairs: 2^-log2_step = step
+  double log2_step;        // angle ratio of neighbouring pairs: 2^-log2_step
   const int32_t *pos;      // [n_axes] rows pos_stride apart
   long pos_stride;
   float eps;
   int gain_dtype;          // VSR_* dtype of the gains
   // Token t's key goes to row k_rows[t] of k.out (NULL: t), nowhere if that lies
-  // outside [0, k_cap); k_rows_in: it is read from that row too.
+  // outside [0, k_cap). Contexts read it from that row too.
   const int32_t *k_rows;
   long k_cap;
-  int k_rows_in;
   // Contexts: angles from rotary-table row row_pos[t] (NULL: t); queries are
   // multiplied by q_scale.
   const float2 *table;
   const int32_t *row_pos;
   float q_scale;
-  int lph, nsplit;  // set by the launchers
+  // Set by the launchers: lanes a head, steps over a token's heads, a wave's
+  // stride over tokens and steps, whether outputs are written past the caches, the
+  // angle ratio of pairs 2^b apart.
+  int lph, steps, next_t, next_step, past_caches;
+  double pair_step[kStepBits];
 };
 // dtype: a VSR_* value, of every tensor but the gains; norm: RMSNorm first.
 hipError_t launch_rotate_heads(const RotateArgs &a, int dtype, bool norm, hipStream_t s);
@@ -230,9 +236,10 @@ struct PickArgs {
   float *logprob;
   long token_stride;
   int32_t *next_ids;  // not NULL: [rows], the token, 0 for -1
+  int past_caches;    // set by the launcher: processed is written past the caches
 };
 size_t pick_workspace_bytes(int rows, int vocab);
-hipError_t launch_pick(const PickArgs &a, int dtype, void *ws, hipStream_t s);
+hipError_t launch_pick(PickArgs a, int dtype, void *ws, hipStream_t s);
 // len[m] = length of branch m.
 hipError_t launch_branch_lengths(const Branches &br, int32_t *len, hipStream_t s);
 

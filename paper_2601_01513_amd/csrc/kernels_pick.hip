@@ -69,10 +69,14 @@ __device__ __forceinline__ Best block_best(Best b, Best *red) {
   return b;
 }
 
+// VEC neighbours, at any element's address (the hardware's 16-byte loads and
+// stores take any).
 template <typename T, int VEC>
-struct alignas(sizeof(T) * VEC) Pack {
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
   T v[VEC];
 };
+
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
 // Rounded as written (no fused multiply-add): the same values as the same
 // steps in any fp32 arithmetic, so that equal logits stay equal.
@@ -86,31 +90,56 @@ __device__ __forceinline__ float penalised(float l, uint32_t c, float rep, float
   return l - p;
 }
 
-// Grid (chunks, rows), NT threads, NV packs of VEC entries a thread. VEC > 1:
-// every row of logits, bias and processed starts at 16 bytes. cnt: the chunk's
-// table where the row has lists.
-template <typename T, int VEC, int NV, int NT>
-__global__ __launch_bounds__(NT) void k_pick_chunks(PickArgs a, int chunks, Best *part) {
+// A row's outputs, by one thread.
+__device__ __forceinline__ void finish_row(const PickArgs &a, int r, const Best &b) {
+  const bool none = b.i == INT32_MAX;
+  const int token = none ? -1 : b.i;
+  a.token[r * a.token_stride] = token;
+  // b.m is +inf only where a logit was: the sum is then no number either.
+  if (a.logprob)
+    a.logprob[r * a.token_stride] = none ? (b.s != b.s ? b.s : -INFINITY)
+                                         : (b.m == INFINITY ? NAN : -log1pf(b.s));
+  if (a.next_ids) a.next_ids[r] = none ? 0 : token;
+}
+
+// Grid (chunks, rows), NT threads, NV packs of VEC entries (16 bytes of logits) a
+// thread; cnt: the chunk's table where the row has lists.
+template <typename T, int NV, int NT>
+__global__ __launch_bounds__(NT) void k_pick_chunks(PickArgs a, Best *part) {
   extern __shared__ uint32_t cnt[];
   __shared__ Best red[NT / 64];
-  constexpr int C = NT * NV * VEC;
+  constexpr int VEC = 16 / sizeof(T), C = NT * NV * VEC;
+  typedef Pack<T, VEC> P;
+  typedef Pack<float, 4> P4;
   const int tid = threadIdx.x, r = blockIdx.y;
   const int v0 = blockIdx.x * C;
   const T *logits = static_cast<const T *>(a.logits) + r * a.stride;
+  const float *bias = a.bias ? a.bias + r * a.bias_stride : nullptr;
+  const uint32_t *mask = a.mask ? a.mask + r * a.mask_stride : nullptr;
 
-  // The chunk's logits are on their way while the lists are counted.
-  float x[NV][VEC];
+  // Everything the chunk reads is on its way before the lists are counted. Loads
+  // past the row's end are moved back inside it (the pack the end cuts through is
+  // read again below, the rest is not used).
+  const auto at = [&](int k) { return v0 + (k * NT + tid) * VEC; };
+  const auto inside = [&](int k) { return min(at(k), a.vocab - VEC); };
+  P raw[NV];
+  P4 add[NV][VEC / 4];
+  uint32_t bits[NV];
+  const bool wide = a.vocab >= VEC;
+  if (wide) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = v0 + (k * NT + tid) * VEC;
-    if (v + VEC <= a.vocab) {
-      const Pack<T, VEC> p = *reinterpret_cast<const Pack<T, VEC> *>(logits + v);
+    for (int k = 0; k < NV; ++k) raw[k] = *reinterpret_cast<const P *>(logits + inside(k));
+    if (bias) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) x[k][j] = to_f32(p.v[j]);
-    } else {
+      for (int k = 0; k < NV; ++k)
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) x[k][j] = v + j < a.vocab ? to_f32(logits[v + j]) : 0.f;
+        for (int j = 0; j < VEC / 4; ++j)
+          add[k][j] = *reinterpret_cast<const P4 *>(bias + inside(k) + 4 * j);
     }
+  }
+  if (mask) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) bits[k] = mask[min(at(k), a.vocab - 1) >> 5];
   }
 
   const bool lists = a.prompt || a.output;
@@ -136,54 +165,46 @@ __global__ __launch_bounds__(NT) void k_pick_chunks(PickArgs a, int chunks, Best
       list(a.output + r * a.output_stride, min(a.output_len ? a.output_len[r] : a.n_output, a.n_output),
            true);
     __syncthreads();
-    const float rep = a.repetition ? a.repetition[r] : 1.f;
-    const float freq = a.frequency ? a.frequency[r] : 0.f;
-    const float pres = a.presence ? a.presence[r] : 0.f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j)
-        x[k][j] = penalised(x[k][j], cnt[(k * NT + tid) * VEC + j], rep, freq, pres);
   }
+  const float rep = a.repetition ? a.repetition[r] : 1.f;
+  const float freq = a.frequency ? a.frequency[r] : 0.f;
+  const float pres = a.presence ? a.presence[r] : 0.f;
 
-  const float *bias = a.bias ? a.bias + r * a.bias_stride : nullptr;
-  const uint32_t *mask = a.mask ? a.mask + r * a.mask_stride : nullptr;
+  float x[NV][VEC];
   float *out = a.processed ? a.processed + r * a.processed_stride : nullptr;
   Best b{-INFINITY, INT32_MAX, 0.f};
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int v = v0 + (k * NT + tid) * VEC;
-    const bool whole = v + VEC <= a.vocab;
-    if (bias) {
-      if (whole) {
+    const int v = at(k);
+    const bool cut = v < a.vocab && v + VEC > a.vocab;  // by the row's end
 #pragma unroll
-        for (int j0 = 0; j0 < VEC; j0 += 4) {
-          constexpr int W = VEC < 4 ? VEC : 4;
-          const Pack<float, W> p = *reinterpret_cast<const Pack<float, W> *>(bias + v + j0);
-#pragma unroll
-          for (int j = 0; j < W; ++j) x[k][j0 + j] += p.v[j];
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j)
-          if (v + j < a.vocab) x[k][j] += bias[v + j];
+    for (int j = 0; j < VEC; ++j) {
+      x[k][j] = to_f32(raw[k].v[j]);
+      if (cut) x[k][j] = v + j < a.vocab ? to_f32(logits[v + j]) : 0.f;
+      if (lists) x[k][j] = penalised(x[k][j], cnt[(k * NT + tid) * VEC + j], rep, freq, pres);
+      if (bias) {
+        float t = add[k][j / 4].v[j % 4];
+        if (cut) t = v + j < a.vocab ? bias[v + j] : 0.f;
+        x[k][j] += t;
       }
     }
     // (v is a multiple of VEC, so that a pack's bits lie in one word.)
-    uint32_t bits = ~0u;
-    if (mask && v < a.vocab) bits = mask[v >> 5] >> (v & 31);
+    const uint32_t allowed = mask ? bits[k] >> (v & 31) : ~0u;
 #pragma unroll
     for (int j = 0; j < VEC; ++j)
-      if (v + j >= a.vocab || !((bits >> j) & 1)) x[k][j] = -INFINITY;
+      if (v + j >= a.vocab || !((allowed >> j) & 1)) x[k][j] = -INFINITY;
     if (out) {
-      if (whole) {
+      if (v + VEC <= a.vocab) {
 #pragma unroll
         for (int j0 = 0; j0 < VEC; j0 += 4) {
-          constexpr int W = VEC < 4 ? VEC : 4;
-          Pack<float, W> p;
-#pragma unroll
-          for (int j = 0; j < W; ++j) p.v[j] = x[k][j0 + j];
-          *reinterpret_cast<Pack<float, W> *>(out + v + j0) = p;
+          const f32x4u p = {x[k][j0], x[k][j0 + 1], x[k][j0 + 2], x[k][j0 + 3]};
+          if (a.past_caches) {
+            asm volatile("");  // (both keep the compiler from merging this with the plain store)
+            __builtin_nontemporal_store(p, reinterpret_cast<f32x4u *>(out + v + j0));
+            asm volatile("");
+          } else {
+            *reinterpret_cast<f32x4u *>(out + v + j0) = p;
+          }
         }
       } else {
 #pragma unroll
@@ -205,61 +226,58 @@ __global__ __launch_bounds__(NT) void k_pick_chunks(PickArgs a, int chunks, Best
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-      for (int j = 0; j < VEC; ++j)
-        b.s += v0 + (k * NT + tid) * VEC + j == b.i ? 0.f : __expf(x[k][j] - m);
+      for (int j = 0; j < VEC; ++j) b.s += at(k) + j == b.i ? 0.f : __expf(x[k][j] - m);
   }
   b = block_best<NT>(b, red);
-  if (tid == 0) part[(long)r * chunks + blockIdx.x] = b;
+  if (tid == 0) {
+    if (gridDim.x == 1)
+      finish_row(a, r, b);
+    else
+      part[(long)r * gridDim.x + blockIdx.x] = b;
+  }
 }
 
-// One wave a row: a row has at most a few hundred chunks.
-__global__ __launch_bounds__(64) void k_pick_merge(PickArgs a, int chunks, const Best *part) {
+template <int NT>
+__global__ __launch_bounds__(NT) void k_pick_merge(PickArgs a, int chunks, const Best *part) {
+  __shared__ Best red[NT / 64];
   const int r = blockIdx.x;
   Best b{-INFINITY, INT32_MAX, 0.f};
-  for (int c = threadIdx.x; c < chunks; c += 64) {
+  for (int c = threadIdx.x; c < chunks; c += NT) {
     const Best p = part[(long)r * chunks + c];
     const bool first = p.m > b.m || (p.m == b.m && p.i < b.i);
-    const Best &hi = first ? p : b, &lo = first ? b : p;
+    const Best hi = first ? p : b, lo = first ? b : p;
     b = {hi.m, hi.i, hi.s + share(lo, hi.m, false)};
   }
-  b = wave_best(b);
-  if (threadIdx.x == 0) {
-    const bool none = b.i == INT32_MAX;
-    const int token = none ? -1 : b.i;
-    a.token[r * a.token_stride] = token;
-    // b.m is +inf only where a logit was: the sum is then no number either.
-    if (a.logprob)
-      a.logprob[r * a.token_stride] = none ? (b.s != b.s ? b.s : -INFINITY)
-                                           : (b.m == INFINITY ? NAN : -log1pf(b.s));
-    if (a.next_ids) a.next_ids[r] = none ? 0 : token;
-  }
+  b = block_best<NT>(b, red);
+  if (threadIdx.x == 0) finish_row(a, r, b);
 }
 
-constexpr int kPickMinChunk = 2048;  // the smallest chunk of any variant below
+constexpr int kPickMinChunk = 4096;  // the smallest chunk of any variant below
 
-template <typename T, int VEC, int NV, int NT>
+template <typename T, int NV, int NT>
 hipError_t launch_pick_chunks(const PickArgs &a, Best *part, hipStream_t s) {
-  constexpr int C = NT * NV * VEC;
+  constexpr int C = NT * NV * (16 / sizeof(T));
+  static_assert(C >= kPickMinChunk, "the workspace holds a partial for each smallest chunk");
   const int chunks = (a.vocab + C - 1) / C;
   const size_t lds = a.prompt || a.output ? C * sizeof(uint32_t) : 0;
-  k_pick_chunks<T, VEC, NV, NT><<<dim3(chunks, a.rows), NT, lds, s>>>(a, chunks, part);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  k_pick_merge<<<a.rows, 64, 0, s>>>(a, chunks, part);
+  k_pick_chunks<T, NV, NT><<<dim3(chunks, a.rows), NT, lds, s>>>(a, part);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || chunks == 1) return e;
+  if (chunks <= 64)
+    k_pick_merge<64><<<a.rows, 64, 0, s>>>(a, chunks, part);
+  else
+    k_pick_merge<256><<<a.rows, 256, 0, s>>>(a, chunks, part);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_pick_type(const PickArgs &a, Best *part, hipStream_t s) {
   constexpr int VEC = 16 / sizeof(T);
-  const bool aligned =
-      ((reinterpret_cast<uintptr_t>(a.logits) | reinterpret_cast<uintptr_t>(a.bias) |
-        reinterpret_cast<uintptr_t>(a.processed) | (size_t)a.stride * sizeof(T) |
-        (a.bias ? (size_t)a.bias_stride * 4 : 0) |
-        (a.processed ? (size_t)a.processed_stride * 4 : 0)) &
-       15) == 0;
-  if (!aligned) return launch_pick_chunks<T, 1, 8, 256>(a, part, s);
-  return launch_pick_chunks<T, VEC, 16 / VEC, 256>(a, part, s);
+  // Eight entries a thread, 512 threads: chunks of 4096. A vocabulary between one and two
+  // of them takes a block of 1024 threads and no second launch.
+  if (a.vocab > 4096 && a.vocab <= 8192)
+    return launch_pick_chunks<T, 8 / VEC, 1024>(a, part, s);
+  return launch_pick_chunks<T, 8 / VEC, 512>(a, part, s);
 }
 
 }  // namespace
@@ -268,8 +286,11 @@ size_t pick_workspace_bytes(int rows, int vocab) {
   return (size_t)rows * ((vocab + kPickMinChunk - 1) / kPickMinChunk) * sizeof(Best);
 }
 
-hipError_t launch_pick(const PickArgs &a, int dtype, void *ws, hipStream_t s) {
+hipError_t launch_pick(PickArgs a, int dtype, void *ws, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
+  // (256 rows of 152064 kept: 91.7 us, written past the caches 88.3; 16 rows alone
+  // 12.0 and 10.6, but there the next reader still finds them in the caches.)
+  a.past_caches = a.processed && (long)a.rows * a.vocab * 4 > kCachedBytes;
   Best *part = static_cast<Best *>(ws);
   if (dtype == 0) return launch_pick_type<float>(a, part, s);
   if (dtype == 1) return launch_pick_type<bf16>(a, part, s);

@@ -19,6 +19,7 @@
 // angle of the fast pairs past a few thousand positions); the fraction, in
 // [-1/2, 1/2], keeps 24 bits.
 #include <algorithm>
+#include <cmath>
 
 #include "common.h"
 
@@ -26,10 +27,14 @@ namespace vsr {
 
 namespace {
 
+// VEC neighbours, at any element's address (the hardware's 16-byte loads and
+// stores take any).
 template <typename T, int VEC>
-struct alignas(sizeof(T) * VEC) Pack {
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
   T v[VEC];
 };
+
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
 
 // Sum over groups of lph (a power of two) consecutive lanes, in every lane.
 __device__ __forceinline__ float group_sum(float v, int lph) {
@@ -48,16 +53,12 @@ __device__ __forceinline__ float group_sum(float v, int lph) {
   return v;
 }
 
-// The axis that turns pair i: consecutive sections, or axes in turn (pair i
-// belongs to axis i % n while that axis has pairs left, else to axis 0).
-__device__ __forceinline__ int pair_axis(const RotaryAxes &r, int i) {
-  if (r.interleaved) {
-    const int a = i % r.n_axes;
-    return i < r.n_axes * r.sections[a] ? a : 0;
-  }
-  int a = 0, end = r.sections[0];
-  while (a + 1 < r.n_axes && i >= end) end += r.sections[++a];
-  return a;
+// The axis of pair i in the map (2 bits a pair, 16 pairs a word).
+__device__ __forceinline__ uint32_t axis_bits(const RotaryAxes &r, int i) {
+  uint32_t w = r.map[0];
+#pragma unroll
+  for (int x = 1; x < kAxisWords; ++x) w = i >> 4 == x ? r.map[x] : w;
+  return w >> (2 * (i & 15));
 }
 
 __device__ __forceinline__ float gain_at(const void *g, int dtype, int d) {
@@ -66,8 +67,16 @@ __device__ __forceinline__ float gain_at(const void *g, int dtype, int d) {
   return to_f32(static_cast<const f16 *>(g)[d]);
 }
 
+// Orders a wave's LDS writes before the other lanes' reads (no instruction: a
+// wave's LDS accesses run in order).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // cos and sin of r turns, |r| <= 1/2. The 16-bit types take the vector unit's
-// own sine (absolute error below 2^-20, measured), far under their rounding.
+// own sine (absolute error up to 2^-23.0 over all turns, sincospif's 2^-24.2: measured).
 template <typename T>
 __device__ __forceinline__ float2 turn(float r) {
   if constexpr (sizeof(T) == 2) {
@@ -79,198 +88,291 @@ __device__ __forceinline__ float2 turn(float r) {
   }
 }
 
+// A kernel argument, in scalar registers from here on. Without it a choice
+// between two arguments by lane becomes a load through a chosen address, in
+// every item, ahead of the loads that need it.
+template <typename V>
+__device__ __forceinline__ V kept(V v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
+
+// One item: the heads h0 .. h0 + 64 / lph - 1 of token t. The items of
+// consecutive waves are neighbours in memory.
+//
 // SPLIT: values are fp16 pairs value + remainder (in_lo, out_lo). TABLE: the
 // angles are rows of a rotary table (row_pos[t], or t) instead of positions.
-template <typename T, int VEC, bool NORM, bool SPLIT, bool TABLE>
-__global__ __launch_bounds__(256) void k_rotate_heads(RotateArgs a) {
-  constexpr int NCH = VEC == 1 ? 2 : 1;  // chunks of VEC pairs a lane holds
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  const int nwaves = gridDim.x * 4;
+// pos, k_rows and row_pos are a's (apart from it, so that they may be taken to
+// differ from what is written: scalar loads).
+// WIDE: more than 64 pairs a head. Loads are unconditional, at clamped places: a
+// load in a branch would have to arrive before the branch's end.
+template <typename T, int VEC, bool WIDE, bool NORM, bool SPLIT, bool TABLE>
+__global__ __launch_bounds__(256) void k_rotate_heads(RotateArgs a, const int32_t *__restrict__ pos,
+                                                      const int32_t *__restrict__ k_rows,
+                                                      const int32_t *__restrict__ row_pos) {
+  constexpr int NCH = VEC == 1 && WIDE ? 2 : 1;  // chunks of VEC pairs a lane holds
+  constexpr int NA = WIDE ? 2 : 1;               // angles a lane computes
+  typedef Pack<T, VEC> P;
+  __shared__ float gains[NORM ? 2 * 256 : 1];
+  __shared__ float angle[4][2][64 * NA];  // each wave's cos and sin of its item's pairs
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  float *const cosv = angle[w][0], *const sinv = angle[w][1];
   const int half = a.hd / 2, rh = a.axes.rot / 2, th = half - rh;
-  const int li = lane & (a.lph - 1), hpw = 64 / a.lph;
-  const int H = a.q.n + a.k.n;
+  const int li = lane & (a.lph - 1), hpw = 64 / a.lph, hl = lane / a.lph;
+  const int nq = a.q.n, H = nq + a.k.n;
+  // Keys are addressed from the queries' pointer.
+  const auto apart = [](const void *k, const void *q) {
+    return kept((reinterpret_cast<intptr_t>(k) - reinterpret_cast<intptr_t>(q)) / (long)sizeof(T));
+  };
+  const T *const q_in = static_cast<const T *>(a.q.in), *const q_in_lo = static_cast<const T *>(a.q.in_lo);
+  T *const q_out = static_cast<T *>(a.q.out), *const q_out_lo = static_cast<T *>(a.q.out_lo);
+  const long k_in = apart(a.k.in, a.q.in), k_out = apart(a.k.out, a.q.out);
+  const long k_in_lo = SPLIT ? apart(a.k.in_lo, a.q.in_lo) : 0;
+  const long k_out_lo = SPLIT ? apart(a.k.out_lo, a.q.out_lo) : 0;
+  const long q_its = kept(a.q.in_ts), q_ihs = kept(a.q.in_hs), q_ots = kept(a.q.out_ts),
+             q_ohs = kept(a.q.out_hs), k_its = kept(a.k.in_ts), k_ihs = kept(a.k.in_hs),
+             k_ots = kept(a.k.out_ts), k_ohs = kept(a.k.out_hs);
 
-  // What a lane keeps for all its tokens: its pairs' places in a head, turns
-  // per position, axes and gains.
   int lo[NCH], hi[NCH];
   bool on[NCH];
-  double f[NCH][VEC];
-  int ax[NCH];  // 2 bits a pair
-  float gq[NCH][2 * VEC], gk[NCH][2 * VEC];
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
     const int s0 = (li + c * a.lph) * VEC;
     on[c] = s0 < half;
     lo[c] = s0 < rh ? s0 : s0 + rh;  // the tail dims >= rot go in pairs th apart
     hi[c] = s0 < rh ? s0 + rh : s0 + rh + th;
-    ax[c] = 0;
-    if constexpr (!TABLE) {
-      const double f0 = on[c] && s0 < rh ? exp2(-s0 * a.log2_step) * 0.15915494309189535 : 0.0;
+    if (!on[c]) lo[c] = hi[c] = 0;
+  }
+  // The angles of an item are computed once a pair, lane l those of pairs l and l
+  // + 64: the axis and the turns per position, base^(-2i/rot) / 2 pi (a product of
+  // the powers of two in i), of each.
+  double f[NA];
+  const int32_t *axis[NA];
+  if constexpr (!TABLE) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        f[c][j] = j == 0 ? f0 : f[c][j - 1] * a.step;
-        if (on[c] && s0 < rh) ax[c] |= pair_axis(a.axes, s0 + j) << (2 * j);
-      }
-    }
-    if constexpr (NORM) {
+    for (int e = 0; e < NA; ++e) {
+      const int i = lane + 64 * e;
+      f[e] = i < rh ? 0.15915494309189535 : 0.0;
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        gq[c][j] = on[c] ? gain_at(a.q.gain, a.gain_dtype, lo[c] + j) : 0.f;
-        gq[c][VEC + j] = on[c] ? gain_at(a.q.gain, a.gain_dtype, hi[c] + j) : 0.f;
-        gk[c][j] = on[c] && a.k.n ? gain_at(a.k.gain, a.gain_dtype, lo[c] + j) : 0.f;
-        gk[c][VEC + j] = on[c] && a.k.n ? gain_at(a.k.gain, a.gain_dtype, hi[c] + j) : 0.f;
-      }
+      for (int b = 0; b < kStepBits; ++b) f[e] *= i >> b & 1 ? a.pair_step[b] : 1.0;
+      axis[e] = pos + (axis_bits(a.axes, i) & 3) * a.pos_stride;
     }
   }
 
-  for (int u = wave; u < a.T * a.nsplit; u += nwaves) {
-    const int t = u / a.nsplit, part = u % a.nsplit;
-    const long krow = a.k_rows ? a.k_rows[t] : t;
-    const bool kkeep = !a.k_rows || (krow >= 0 && krow < a.k_cap);
-    const long kin = a.k_rows_in && kkeep ? krow : t;
-    float2 cs[NCH][VEC];
-    if constexpr (TABLE) {
-      const float2 *row = a.table + (long)(a.row_pos ? a.row_pos[t] : t) * half;
-#pragma unroll
-      for (int c = 0; c < NCH; ++c)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j)
-          cs[c][j] = on[c] ? row[lo[c] + j] : make_float2(1.f, 0.f);
-    } else {
-      int p[kMaxAxes];
-#pragma unroll
-      for (int x = 0; x < kMaxAxes; ++x)
-        p[x] = x < a.axes.n_axes ? a.pos[x * a.pos_stride + t] : 0;
-#pragma unroll
-      for (int c = 0; c < NCH; ++c)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const int x = (ax[c] >> (2 * j)) & 3;
-          const int pj = x == 0 ? p[0] : x == 1 ? p[1] : x == 2 ? p[2] : p[3];
-          const double r = (double)pj * f[c][j];
-          cs[c][j] = turn<T>((float)(r - rint(r)));
-        }
+  // A wave's item, loaded ahead.
+  struct Item {
+    int t, h0;
+    P v0[NCH], v1[NCH], w0[NCH], w1[NCH];
+    int p[NA], krow;
+    float2 cs[NA];
+  };
+  // (A lane's own load of the key row: a scalar one would hold up the LDS reads.)
+  int zero = 0;
+  asm volatile("" : "+v"(zero));
+  const int32_t *const krows = k_rows ? k_rows : TABLE ? reinterpret_cast<const int32_t *>(a.table) : pos;
+  int nt, nh;  // the next item to load: token and step over its heads
+  {
+    const int first = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + w);
+    nt = first / a.steps;
+    nh = first % a.steps;
+  }
+  const auto load_next = [&](Item &it) {
+    const int t = nt, h = nh * hpw + hl;
+    it.t = t;
+    it.h0 = nh * hpw;
+    nt += a.next_t;
+    nh += a.next_step;
+    if (nh >= a.steps) {
+      nh -= a.steps;
+      ++nt;
     }
-    for (int h0 = part * hpw; h0 < H; h0 += a.nsplit * hpw) {
-      const int h = h0 + lane / a.lph;
-      const bool isq = h < a.q.n;
-      const bool have = h < H;
-      const int hh = isq ? h : h - a.q.n;
-      const long in = isq ? t * a.q.in_ts + hh * a.q.in_hs : kin * a.k.in_ts + hh * a.k.in_hs;
-      const long out = isq ? t * a.q.out_ts + hh * a.q.out_hs : krow * a.k.out_ts + hh * a.k.out_hs;
-      const T *xin = static_cast<const T *>(isq ? a.q.in : a.k.in) + in;
-      const T *xin_lo = SPLIT ? static_cast<const T *>(isq ? a.q.in_lo : a.k.in_lo) + in : nullptr;
-      float x[NCH][2 * VEC];
-      float ss = 0.f;
+    const int tc = min(t, a.T - 1), hc = min(h, H - 1);
+    const bool isq = hc < nq;
+    long kin = tc;
+    if constexpr (TABLE) {
+      if (k_rows) kin = min(max(k_rows[tc], 0), (int)a.k_cap - 1);
+    }
+    it.krow = krows[tc + zero];
+    const long in = isq ? tc * q_its + hc * q_ihs : k_in + kin * k_its + (hc - nq) * k_ihs;
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-        const bool ld = have && on[c];
-        Pack<T, VEC> v0{}, v1{};
-        if (ld) {
-          v0 = *reinterpret_cast<const Pack<T, VEC> *>(xin + lo[c]);
-          v1 = *reinterpret_cast<const Pack<T, VEC> *>(xin + hi[c]);
-        }
+    for (int e = 0; e < NA; ++e) {
+      if constexpr (TABLE) {
+        const long row = row_pos ? row_pos[tc] : tc;
+        it.cs[e] = a.table[row * half + min(lane + 64 * e, half - 1)];
+      } else {
+        it.p[e] = axis[e][tc];
+      }
+    }
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          x[c][j] = to_f32(v0.v[j]);
-          x[c][VEC + j] = to_f32(v1.v[j]);
-        }
+    for (int c = 0; c < NCH; ++c) {
+      it.v0[c] = *reinterpret_cast<const P *>(q_in + in + lo[c]);
+      it.v1[c] = *reinterpret_cast<const P *>(q_in + in + hi[c]);
+      if constexpr (SPLIT) {
+        const long in_lo = isq ? in : in - k_in + k_in_lo;
+        it.w0[c] = *reinterpret_cast<const P *>(q_in_lo + in_lo + lo[c]);
+        it.w1[c] = *reinterpret_cast<const P *>(q_in_lo + in_lo + hi[c]);
+      }
+    }
+  };
+  // Works on `it` and loads the next into it as soon as its values are out.
+  const auto work = [&](Item &it) {
+    const int t = it.t, h = it.h0 + hl;
+    const bool isq = h < nq;
+    int krow = k_rows ? it.krow : t;
+    asm volatile("" : "+v"(krow));
+    const bool st = h < H && (isq || (krow >= 0 && krow < a.k_cap));
+    const long out = isq ? t * q_ots + h * q_ohs : (long)krow * k_ots + (h - nq) * k_ohs;
+#pragma unroll
+    for (int e = 0; e < NA; ++e) {
+      float2 cs;
+      if constexpr (TABLE) {
+        cs = it.cs[e];
+      } else {
+        const double r = (double)it.p[e] * f[e];
+        cs = turn<T>((float)(r - rint(r)));
+      }
+      cosv[lane + 64 * e] = cs.x;
+      sinv[lane + 64 * e] = cs.y;
+    }
+    wave_sync();
+    float x[NCH][2 * VEC];
+    float ss = 0.f;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      // (Lanes past the head's pairs hold a copy of others: none of it counts.)
+      const bool have = on[c];
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        x[c][j] = have ? to_f32(it.v0[c].v[j]) : 0.f;
+        x[c][VEC + j] = have ? to_f32(it.v1[c].v[j]) : 0.f;
         if constexpr (SPLIT) {
-          if (ld) {
-            v0 = *reinterpret_cast<const Pack<T, VEC> *>(xin_lo + lo[c]);
-            v1 = *reinterpret_cast<const Pack<T, VEC> *>(xin_lo + hi[c]);
-          }
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            x[c][j] += ld ? to_f32(v0.v[j]) : 0.f;
-            x[c][VEC + j] += ld ? to_f32(v1.v[j]) : 0.f;
-          }
-        }
-        if constexpr (NORM) {
-#pragma unroll
-          for (int j = 0; j < 2 * VEC; ++j) ss += x[c][j] * x[c][j];
+          x[c][j] += have ? to_f32(it.w0[c].v[j]) : 0.f;
+          x[c][VEC + j] += have ? to_f32(it.w1[c].v[j]) : 0.f;
         }
       }
       if constexpr (NORM) {
-        ss = group_sum(ss, a.lph);
-        const float rs = 1.f / sqrtf(ss / (float)a.hd + a.eps);
 #pragma unroll
-        for (int c = 0; c < NCH; ++c)
-#pragma unroll
-          for (int j = 0; j < 2 * VEC; ++j) x[c][j] *= rs * (isq ? gq[c][j] : gk[c][j]);
+        for (int j = 0; j < 2 * VEC; ++j) ss += x[c][j] * x[c][j];
       }
-      const bool st = have && (isq || kkeep);
+    }
+    // The values are out of the item's registers before its next loads, so that
+    // these need no others (copies at the loop's end would wait for them).
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-        Pack<T, VEC> v0, v1, w0, w1;
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int j = 0; j < 2 * VEC; ++j) asm volatile("" : "+v"(x[c][j]));
+    __builtin_amdgcn_sched_barrier(0);
+    load_next(it);
+    if constexpr (NORM) {
+      ss = group_sum(ss, a.lph);
+      const float rs = 1.f / sqrtf(ss / (float)a.hd + a.eps);
+      const float *g = gains + (isq ? 0 : 256);
+#pragma unroll
+      for (int c = 0; c < NCH; ++c)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          float y0 = x[c][j] * cs[c][j].x - x[c][VEC + j] * cs[c][j].y;
-          float y1 = x[c][VEC + j] * cs[c][j].x + x[c][j] * cs[c][j].y;
-          if (th > 0 && lo[c] >= rh) {  // a dim >= rot meets no other, an infinity among them
-            y0 = x[c][j];
-            y1 = x[c][VEC + j];
-          }
-          if constexpr (TABLE) {
-            const float scale = isq ? a.q_scale : 1.f;
-            y0 *= scale;
-            y1 *= scale;
-          }
-          v0.v[j] = from_f32<T>(y0);
-          v1.v[j] = from_f32<T>(y1);
-          if constexpr (SPLIT) {
-            w0.v[j] = from_f32<T>(y0 - to_f32(v0.v[j]));
-            w1.v[j] = from_f32<T>(y1 - to_f32(v1.v[j]));
-          }
+          x[c][j] *= rs * g[lo[c] + j];
+          x[c][VEC + j] *= rs * g[hi[c] + j];
         }
-        if (st && on[c]) {
-          T *o = static_cast<T *>(isq ? a.q.out : a.k.out) + out;
-          *reinterpret_cast<Pack<T, VEC> *>(o + lo[c]) = v0;
-          *reinterpret_cast<Pack<T, VEC> *>(o + hi[c]) = v1;
-          if constexpr (SPLIT) {
-            T *ol = static_cast<T *>(isq ? a.q.out_lo : a.k.out_lo) + out;
-            *reinterpret_cast<Pack<T, VEC> *>(ol + lo[c]) = w0;
-            *reinterpret_cast<Pack<T, VEC> *>(ol + hi[c]) = w1;
-          }
+    }
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+      if (!(st && on[c])) continue;
+      const int s0 = (li + c * a.lph) * VEC;
+      P o0, o1, l0, l1;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float cj = cosv[s0 + j], sj = sinv[s0 + j];
+        float y0 = x[c][j] * cj - x[c][VEC + j] * sj;
+        float y1 = x[c][VEC + j] * cj + x[c][j] * sj;
+        if (th > 0 && lo[c] >= rh) {  // a dim >= rot meets no other, an infinity among them
+          y0 = x[c][j];
+          y1 = x[c][VEC + j];
+        }
+        if constexpr (TABLE) {
+          const float scale = isq ? a.q_scale : 1.f;
+          y0 *= scale;
+          y1 *= scale;
+        }
+        o0.v[j] = from_f32<T>(y0);
+        o1.v[j] = from_f32<T>(y1);
+        if constexpr (SPLIT) {
+          l0.v[j] = from_f32<T>(y0 - to_f32(o0.v[j]));
+          l1.v[j] = from_f32<T>(y1 - to_f32(o1.v[j]));
         }
       }
+      T *o = q_out + (out + (isq ? 0 : k_out));
+      bool stored = false;
+      if constexpr (sizeof(P) == 16) {
+        if (a.past_caches) {
+          asm volatile("");  // (both keep the compiler from merging this with the plain stores)
+          __builtin_nontemporal_store(__builtin_bit_cast(u32x4u, o0),
+                                      reinterpret_cast<u32x4u *>(o + lo[c]));
+          __builtin_nontemporal_store(__builtin_bit_cast(u32x4u, o1),
+                                      reinterpret_cast<u32x4u *>(o + hi[c]));
+          asm volatile("");
+          stored = true;
+        }
+      }
+      if (!stored) {
+        *reinterpret_cast<P *>(o + lo[c]) = o0;
+        *reinterpret_cast<P *>(o + hi[c]) = o1;
+      }
+      if constexpr (SPLIT) {
+        T *ol = q_out_lo + (out + (isq ? 0 : k_out_lo));
+        *reinterpret_cast<P *>(ol + lo[c]) = l0;
+        *reinterpret_cast<P *>(ol + hi[c]) = l1;
+      }
     }
+    wave_sync();
+  };
+  Item it;
+  load_next(it);
+  if constexpr (NORM) {
+    for (int d = threadIdx.x; d < a.hd; d += 256) {
+      gains[d] = gain_at(a.q.gain, a.gain_dtype, d);
+      if (a.k.n) gains[256 + d] = gain_at(a.k.gain, a.gain_dtype, d);
+    }
+    __syncthreads();
   }
+  while (it.t < a.T) work(it);
 }
 
-// Widest VEC (16 bytes at most) that the head's two parts and every address
-// allow.
+// Widest VEC (16 bytes at most) that the head's two parts allow.
 int pair_width(const RotateArgs &a, size_t esize) {
   const int rh = a.axes.rot / 2, th = a.hd / 2 - rh;
-  for (int vec = (int)(16 / esize); vec > 1; vec /= 2) {
-    const size_t bytes = vec * esize;
-    bool ok = rh % vec == 0 && th % vec == 0;
-    for (const HeadSet *s : {&a.q, &a.k}) {
-      if (!s->n) continue;
-      for (const void *p : {s->in, s->in_lo, (const void *)s->out, (const void *)s->out_lo})
-        ok = ok && reinterpret_cast<uintptr_t>(p) % bytes == 0;
-      for (long st : {s->in_ts, s->in_hs, s->out_ts, s->out_hs}) ok = ok && st % vec == 0;
-    }
-    if (ok) return vec;
-  }
-  return 1;
+  int vec = (int)(16 / esize);
+  while (rh % vec || th % vec) vec /= 2;
+  return vec;
+}
+
+template <typename T, int VEC, bool WIDE, bool NORM, bool SPLIT, bool TABLE>
+hipError_t launch_wide(RotateArgs a, hipStream_t s) {
+  const int chunks = a.hd / 2 / VEC;
+  for (int b = 0; b < kStepBits; ++b) a.pair_step[b] = std::exp2(-a.log2_step * (1 << b));
+  a.lph = 1;
+  while (a.lph < chunks && a.lph < 64) a.lph *= 2;
+  const int hpw = 64 / a.lph;
+  a.steps = (a.q.n + a.k.n + hpw - 1) / hpw;
+  // Three blocks a CU: more keep more of the memory's rows open than it likes (16384
+  // tokens of 48 heads: 76.7 us, 79.1 with four, 82 with eight), fewer wait on loads
+  // (4096 tokens of 32 heads: 12.0 us, 12.4 with two).
+  const unsigned blocks = (unsigned)std::min(((long)a.T * a.steps + 3) / 4, 768L);
+  // What no cache holds until its reader comes is written past them (the same 16384
+  // tokens: 71.4 us; 8192 with their norms: 40.9 -> 37.8, and with a copy of the queries
+  // after it 73.3 -> 68.1; but 4096 tokens of 32 heads with that reader 23.4 -> 25.0).
+  a.past_caches = (long)a.T * (a.q.n + a.k.n) * a.hd * sizeof(T) > kCachedBytes;
+  a.next_t = blocks * 4 / a.steps;
+  a.next_step = blocks * 4 % a.steps;
+  k_rotate_heads<T, VEC, WIDE, NORM, SPLIT, TABLE>
+      <<<blocks, 256, 0, s>>>(a, a.pos, a.k_rows, a.row_pos);
+  return hipGetLastError();
 }
 
 template <typename T, int VEC, bool NORM, bool SPLIT, bool TABLE>
-hipError_t launch_vec(RotateArgs a, hipStream_t s) {
-  const int chunks = a.hd / 2 / VEC;
-  a.lph = 1;
-  while (a.lph < chunks && a.lph < 64) a.lph *= 2;
-  const int hpw = 64 / a.lph, steps = (a.q.n + a.k.n + hpw - 1) / hpw;
-  // Few tokens: a wave for each step over the heads, so that the call is one
-  // load's latency long. Many: a wave takes whole tokens and computes their
-  // angles once.
-  a.nsplit = (long)a.T * steps <= 4096 ? steps : 1;
-  const long units = (long)a.T * a.nsplit;
-  const unsigned blocks = (unsigned)std::min<long>((units + 3) / 4, 2048);
-  k_rotate_heads<T, VEC, NORM, SPLIT, TABLE><<<blocks, 256, 0, s>>>(a);
-  return hipGetLastError();
+hipError_t launch_vec(const RotateArgs &a, hipStream_t s) {
+  if (a.hd > 128) return launch_wide<T, VEC, true, NORM, SPLIT, TABLE>(a, s);
+  return launch_wide<T, VEC, false, NORM, SPLIT, TABLE>(a, s);
 }
 
 template <typename T, bool NORM>
@@ -294,7 +396,7 @@ __global__ void k_rope_axes_table(float2 *cs, int npos, RotaryAxes axes, double 
   const long idx = (long)blockIdx.x * blockDim.x + threadIdx.x;
   if (idx >= (long)npos * half) return;
   const int p = (int)(idx / half), i = (int)(idx % half);
-  const long at = p < P ? pos[pair_axis(axes, i) * pos_stride + p] : (long)next + (p - P);
+  const long at = p < P ? pos[(axis_bits(axes, i) & 3) * pos_stride + p] : (long)next + (p - P);
   const double ang = (double)at * pow(base, -2.0 * i / axes.rot);
   cs[idx] = make_float2((float)cos(ang), (float)sin(ang));
 }
@@ -325,10 +427,10 @@ hipError_t launch_rope_axes_table(float2 *cs, int npos, const RotaryAxes &axes, 
 hipError_t launch_norm_cached(const RotateArgs &a, bool f32, hipStream_t s) {
   if (a.T == 0) return hipSuccess;
   if (!f32)  // (head_dim 128; the workspace's planes are 256-byte aligned)
-    return a.q.in_lo ? launch_vec<f16, 8, true, true, true>(a, s)
-                     : launch_vec<f16, 8, true, false, true>(a, s);
-  return pair_width(a, 4) == 4 ? launch_vec<float, 4, true, false, true>(a, s)
-                               : launch_vec<float, 1, true, false, true>(a, s);
+    return a.q.in_lo ? launch_wide<f16, 8, false, true, true, true>(a, s)
+                     : launch_wide<f16, 8, false, true, false, true>(a, s);
+  return a.hd % 8 == 0 ? launch_vec<float, 4, true, false, true>(a, s)
+                       : launch_vec<float, 1, true, false, true>(a, s);
 }
 
 hipError_t launch_rotate_heads(const RotateArgs &a, int dtype, bool norm, hipStream_t s) {

@@ -394,7 +394,6 @@ const char *rotary_axes(const vsr_rotary *r, int head_dim, RotaryAxes *out) {
   int half = 0;
   for (int x = 0; x < r->n_axes; ++x) {
     if (r->sections[x] < 0 || r->sections[x] > 128) return "sections must lie in [0, 128]";
-    out->sections[x] = r->sections[x];
     half += r->sections[x];
   }
   if (half < 1) return "the sections hold no pair";
@@ -405,7 +404,13 @@ const char *rotary_axes(const vsr_rotary *r, int head_dim, RotaryAxes *out) {
         return "interleaved: an axis has more pairs than its turns";
   out->rot = 2 * half;
   out->n_axes = r->n_axes;
-  out->interleaved = r->interleaved != 0;
+  for (int i = 0, x = 0, end = r->sections[0]; i < half; ++i) {
+    while (i >= end) end += r->sections[++x];
+    const int turn = i % r->n_axes;
+    const uint32_t axis =
+        !r->interleaved ? x : i < r->n_axes * r->sections[turn] ? turn : 0;
+    out->map[i / 16] |= axis << 2 * (i % 16);
+  }
   return nullptr;
 }
 
@@ -498,7 +503,6 @@ hipError_t norm_heads(vsr_ctx *c, int l, bool precise, int row0, int n, TA *k, T
   a.gain_dtype = cf.dtype;
   a.k_rows = cache_row;
   a.k_cap = npos;
-  a.k_rows_in = cache_row != nullptr;
   a.table = c->at<float2>(c->plan.rope);
   a.row_pos = row_pos;
   // The fast attention kernels take the queries pre-scaled (log2 units).
@@ -1659,7 +1663,6 @@ int rotate_call(const char *name, const vsr_rotary *rot, int32_t dtype, int32_t 
   a.pos = pos;
   a.pos_stride = pos_stride;
   a.log2_step = 2.0 / a.axes.rot * std::log2((double)rot->base);
-  a.step = std::exp2(-a.log2_step);
   a.eps = eps;
   a.gain_dtype = gain_dtype;
   a.k_rows = k_rows;
