@@ -277,7 +277,8 @@ typedef struct vsr_heads {
  * (head_dim - rot) / 2 that are multiples of 8 (fp32: 4) are fastest. k_in and k_out may both be NULL. q_out may be q_in, and
  * k_out k_in (with k_rows NULL); other overlaps are refused, but for an output
  * in columns of stacked rows that the input does not use. Outputs must not
- * overlap themselves (one stride at least the other's whole extent).
+ * overlap themselves (one stride at least the other's whole extent), nor pos,
+ * k_rows or the gains.
  * head_dim even, 2 to 256, >= rot; 0 <= T <= 2^30 (0: nothing is done); n_heads 1
  * to 4096 (a NULL k: none); k_cap < 2^31; no set of heads spans over 2^46 elements. Enqueued on hip_stream, whose device must be the
  * current one; errors via vsr_last_error(NULL). */
@@ -288,7 +289,8 @@ int vsr_rope_axes(const vsr_rotary *rot, int32_t dtype, int32_t head_dim, int32_
 
 /* vsr_rope_axes on normed heads, in the same pass: every query head x becomes
  * x / sqrt(mean(x^2) + eps) * q_gain (k_gain for keys; over all head_dim dims)
- * before it is rotated. Statistics in fp32, one rounding at the end.
+ * before it is rotated. Statistics in fp32, one rounding at the end (with eps 0
+ * a head of zeros becomes NaN).
  *   q_gain, k_gain : device [head_dim] of gain_dtype (VSR_F32, VSR_BF16 or
  *                    VSR_F16); k_gain may be NULL with k; eps finite, >= 0. */
 int vsr_qk_norm_rope(const vsr_rotary *rot, int32_t dtype, int32_t head_dim, int32_t T,
@@ -368,8 +370,9 @@ size_t vsr_pick_workspace_size(int32_t rows, int32_t vocab);
  *               forbids is not looked at. An allowed NaN is never picked and makes
  *               the logprob NaN, as an allowed +inf does;
  *   workspace : device, >= vsr_pick_workspace_size(rows, vocab) bytes, 16-byte
- *               aligned, caller-owned; calls that overlap in time need their own.
- * 0 <= rows <= 65535 (0: nothing is done), 1 <= vocab <= 2^24.
+ *               aligned, caller-owned; calls that overlap in time need their own
+ *               (two captured graphs that share one must not replay at once).
+ * Outputs must not overlap inputs, but for processed as above. 0 <= rows <= 65535 (0: nothing is done), 1 <= vocab <= 2^24.
  * Enqueued on hip_stream, whose device must be the current one; errors via
  * vsr_last_error(NULL). */
 int vsr_pick_tokens(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,

@@ -287,6 +287,16 @@ class Verifier:
             raise VsrError(rc, self.lib.vsr_last_error(self.h).decode())
 
     def load_weights(self, w: Dict):
+        # Decoders with query/key norms carry their gains as q_norm and k_norm.
+        norms = [[lw.get(k) for lw in w["layers"]] for k in ("q_norm", "k_norm")]
+        gains = [t for ts in norms for t in ts if t is not None]
+        if gains and len(gains) != 2 * len(w["layers"]):
+            raise VsrError(VSR_EINVAL, "q_norm and k_norm must be given in every layer or none")
+        for t in gains:
+            if t.numel() != self.cfg.head_dim or not t.is_contiguous() or \
+                    t.dtype != w["final_norm"].dtype or t.device != w["final_norm"].device:
+                raise VsrError(VSR_EINVAL, "q_norm, k_norm: contiguous [head_dim] gains in the "
+                                           "model's dtype and on its device expected")
         if self.gemm_f16:  # one-time fp16 copies of the GEMM matrices
             f16 = lambda t: weights_to_f16(t, self.stream)  # noqa: E731
             w = dict(w, lm_head=f16(w["lm_head"]),
@@ -302,21 +312,10 @@ class Verifier:
                         *[ctypes.cast(arrs[k], _PP) for k in
                           ("attn_norm", "wqkv", "wo", "ffn_norm", "wgu", "wdown")])
         self._check(self.lib.vsr_load_weights(self.h, ctypes.byref(cw)))
-        # Decoders with query/key norms carry their gains as q_norm and k_norm.
-        self._qk_norm = [[lw.get(k) for lw in w["layers"]] for k in ("q_norm", "k_norm")]
-        given = [t is not None for ts in self._qk_norm for t in ts]
-        if any(given) != all(given):
-            raise VsrError(VSR_EINVAL, "q_norm and k_norm must be given in every layer or none")
-        for t in (t for ts in self._qk_norm for t in ts if t is not None):
-            if t.numel() != self.cfg.head_dim or not t.is_contiguous() or \
-                    t.dtype != w["final_norm"].dtype:
-                raise VsrError(VSR_EINVAL, "q_norm, k_norm: contiguous [head_dim] gains in the "
-                                           "model's dtype expected")
-        if any(given) or self._has_qk_norm:
-            arrs = [(ctypes.c_void_p * L)(*map(_ptr, ts)) if any(given) else None
-                    for ts in self._qk_norm]
+        if gains or self._has_qk_norm:
+            arrs = [(ctypes.c_void_p * L)(*map(_ptr, ts)) if gains else None for ts in norms]
             self._check(self.lib.vsr_load_qk_norms(self.h, *[ctypes.cast(a, _PP) for a in arrs]))
-        self._has_qk_norm = any(given)
+        self._has_qk_norm, self._qk_norm = bool(gains), norms
 
     def set_positions(self, rot=None, pos=None, next: int = 0):
         """Positions of the prefix on several axes (vsr_set_positions) for the
@@ -326,10 +325,11 @@ class Verifier:
         if rot is None:
             self._check(self.lib.vsr_set_positions(self.h, None, None, 0, 0, 0))
             return
-        _check_pos(_torch_names(), rot, pos, int(pos.shape[-1]), pos.get_device())
+        P = int(pos.shape[-1])
+        stride = _check_pos(_torch_names(), rot, pos, P, self.workspace.get_device())
         self._pos = pos
-        self._check(self.lib.vsr_set_positions(self.h, ctypes.byref(rot), _ptr(pos),
-                                               pos.stride(0), int(pos.shape[1]), int(next)))
+        self._check(self.lib.vsr_set_positions(self.h, ctypes.byref(rot), _ptr(pos), stride, P,
+                                               int(next)))
 
     def prefill(self, visual, ids):
         """visual: device [Pv][d] (config dtype) or None; ids: device int32 [Pt] or None."""
@@ -419,10 +419,18 @@ class Verifier:
         tokens it got so far). mask: int32 words [1 or M][ceil(vocab/32)], or
         [n_new][1 or M][...] with one mask a step. out: (tokens [M][n_new] int32,
         logprobs [M][n_new] f32 or None). Returns (tokens, logprobs)."""
-        torch = self._torch
+        torch = _torch_names()
         M, cmax = int(prompt_ids.shape[0]), int(prompt_ids.shape[1])
         lens = (ctypes.c_int32 * M)(*[int(x) for x in prompt_len])
-        step, dev = 0, prompt_ids.get_device()
+        step, dev = 0, self.workspace.get_device()
+
+        def given(t, dtype, shape, what):
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or \
+                    t.get_device() != dev:
+                raise VsrError(VSR_EINVAL, f"{what}: contiguous {dtype} {list(shape)} on the "
+                                           "context's device expected")
+
+        given(prompt_ids, torch.int32, (M, cmax), "prompt_ids")
         if mask is not None and mask.dim() == 3:
             if int(mask.shape[0]) != int(n_new):
                 raise VsrError(VSR_EINVAL, "mask: one row of masks a step expected")
@@ -439,6 +447,10 @@ class Verifier:
             size = self.lib.vsr_draft_ruled_workspace_size(ctypes.byref(self.c), M)
             workspace = _empty(torch, max(size, 256), torch.uint8, self.device, self.stream)
         tokens, logprobs = out
+        given(tokens, torch.int32, (M, int(n_new)), "tokens")
+        if logprobs is not None:
+            given(logprobs, torch.float32, (M, int(n_new)), "logprobs")
+        given(workspace, torch.uint8, (workspace.numel(),), "workspace")
         self._check(self.lib.vsr_draft_ruled(
             self.h, _ptr(prompt_ids), lens, M, cmax, int(n_new), ctypes.byref(rules), step,
             _ptr(tokens), _ptr(logprobs), _ptr(workspace), workspace.numel()))
@@ -504,18 +516,21 @@ def rotary(sections: Sequence[int], base: float, interleaved: bool = False) -> V
 
 _float_types = None  # torch float dtype -> VSR_*
 _raw_stream = None   # device index -> its current stream's handle
+_device_now = None   # -> the current device's index
 
 
 def _torch_names():
-    """torch (imported on first use), with the library and the two names above set."""
-    global _float_types, _raw_stream
+    """torch (imported on first use), with the library and the names above set."""
+    global _float_types, _raw_stream, _device_now
     import torch
     if _float_types is None:
         load_library()
-        _float_types = {torch.float32: VSR_F32, torch.bfloat16: VSR_BF16, torch.float16: VSR_F16}
         # (A Stream object takes longer to make than a call's whole argument list.)
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        # Set last: another thread that finds it set finds the rest set too.
+        _float_types = {torch.float32: VSR_F32, torch.bfloat16: VSR_BF16, torch.float16: VSR_F16}
     return torch
 
 
@@ -525,7 +540,7 @@ def _call(torch, dev, stream, f, args):
     if dev < 0:
         raise VsrError(VSR_EINVAL, "device tensors expected")
     st = stream.cuda_stream if stream is not None else _raw_stream(dev)
-    if dev == torch.cuda.current_device():
+    if dev == _device_now():
         rc = f(*args, st)
     else:
         with torch.cuda.device(dev):
@@ -547,10 +562,10 @@ def _check_pos(torch, rot, pos, T, dev):
 
 def _heads(t, dtype, hd, dev, rows):
     """vsr_heads of t, [rows][n_heads][hd] (rows < 0: any) of dtype on device dev."""
-    if t.dim() == 3 and t.dtype is dtype and t.get_device() == dev:
+    if t.dtype is dtype and t.get_device() == dev and t.dim() == 3:
         n, heads, d = t.shape
         ts, hs, ds = t.stride()
-        if d == hd and ds == 1 and (n == rows or rows < 0):
+        if ds == 1 and d == hd and (n == rows or rows < 0):
             return VsrHeads(t.data_ptr(), heads, ts, hs)
     raise VsrError(VSR_EINVAL, "heads: [tokens][n_heads][head_dim] tensors of one dtype, device "
                                "and size, head_dim contiguous, expected")

@@ -9,12 +9,19 @@
 //   token = lowest v of the largest l (-1 if that is -inf);
 //   logprob = l[token] - log sum_v exp(l[v])
 //
-// Bound by one read of the logits (and one write, where the processed logits
-// are asked for). A block takes a chunk of one row's vocabulary: it counts the
-// row's lists into an LDS table of the chunk (one word an entry: bit 31 "in the
-// prompt", the rest the output count; integer atomics, so no order shows), holds
-// the chunk's processed logits in registers and leaves (largest, its index,
-// sum of the others' exp); a second small kernel merges a row's chunks.
+// Bound by one read of the logits (and of the bias, and one write where the
+// processed logits are asked for): 256 rows of 152064 fp32 logits with every rule, a bias a
+// row and the result kept, 472 MB, take 88 us (5.4 TB/s). Few rows are bound by two
+// launches and the steps between loads: 3 rows 7.1 us, 1 masked row 5.4.
+//
+// A block takes a chunk of one row's vocabulary: its loads go out first, then it
+// counts the row's lists into an LDS table of the chunk (one word an entry: bit 31
+// "in the prompt", the rest the output count; integer atomics, so no order shows),
+// holds the chunk's processed logits in registers and leaves (largest, its index,
+// sum of the others' exp); a second small kernel merges a row's chunks. Every block of
+// a row reads its lists, so chunks are as large as a few rows can bear: 4096
+// entries (256 rows 91.7 us with plain stores, against 98 with 1024, 99 with 8192 and
+// 102 with 16384 entries; 3 rows 7.2, 6.8, 7.8 and 10.2).
 //
 // The sums leave the largest entry out: with S' = sum over the others of
 // exp(l - max), logprob = -log1p(S') keeps its relative accuracy where one token

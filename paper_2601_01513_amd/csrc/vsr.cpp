@@ -457,15 +457,22 @@ extern "C" int vsr_load_qk_norms(vsr_ctx *ctx, const void *const *q_norm,
   for (int l = 0; l < L; ++l)
     if (!q_norm[l] || !k_norm[l])
       return ctx->fail(VSR_EINVAL, "query/key norms: layer %d has a NULL tensor", l);
+  std::vector<const void *> qs, ks;
+  try {
+    qs.assign(q_norm, q_norm + L);
+    ks.assign(k_norm, k_norm + L);
+  } catch (...) {
+    return VSR_ENOMEM;
+  }
   if (const int rc = set_device(ctx)) return rc;
-  ctx->prefilled = false;
   if (L > 0)
     HIPCHECK(ctx, "query/key norms",
              launch_no_turn(ctx->at<int32_t>(ctx->plan.zero_pos), ctx->plan.rows_max,
                             ctx->at<float2>(ctx->plan.no_turn), ctx->cfg.head_dim / 2,
                             ctx->stream));
-  ctx->q_norm.assign(q_norm, q_norm + L);
-  ctx->k_norm.assign(k_norm, k_norm + L);
+  ctx->prefilled = false;
+  ctx->q_norm.swap(qs);
+  ctx->k_norm.swap(ks);
   return VSR_OK;
 }
 
@@ -1554,6 +1561,17 @@ extern "C" int vsr_weights_to_f16(const void *src, void *dst, size_t n, void *hi
 
 namespace {
 
+// The message of a context-free call, "name: what" (lost if there is no memory
+// for it: no call throws), and its code.
+int refuse(int code, const char *name, const char *what) {
+  try {
+    g_create_error = std::string(name) + ": " + what;
+  } catch (...) {
+    g_create_error.clear();
+  }
+  return code;
+}
+
 // One set of heads as the call gives it: its message if it is wrong, else NULL.
 const char *heads_error(const vsr_heads *h, size_t esize, bool out, int head_dim, long rows) {
   if (!h->data || reinterpret_cast<uintptr_t>(h->data) % esize)
@@ -1651,10 +1669,7 @@ int rotate_call(const char *name, const vsr_rotary *rot, int32_t dtype, int32_t 
     if (heads_clash(k_out, rows, q_out, T, head_dim, esize)) return "k_out overlaps q_out";
     return nullptr;
   };
-  if (const char *msg = check()) {
-    g_create_error = std::string(name) + ": " + msg;
-    return VSR_EINVAL;
-  }
+  if (const char *msg = check()) return refuse(VSR_EINVAL, name, msg);
   if (T == 0) return VSR_OK;
   set_heads(&a.q, q_in, q_out, q_gain);
   if (k_in) set_heads(&a.k, k_in, k_out, k_gain);
@@ -1665,15 +1680,12 @@ int rotate_call(const char *name, const vsr_rotary *rot, int32_t dtype, int32_t 
   a.log2_step = 2.0 / a.axes.rot * std::log2((double)rot->base);
   a.eps = eps;
   a.gain_dtype = gain_dtype;
-  a.k_rows = k_rows;
+  a.k_rows = k_in ? k_rows : nullptr;
   a.k_cap = k_cap;
   a.q_scale = 1.f;
   const hipError_t e =
       launch_rotate_heads(a, dtype, norm, static_cast<hipStream_t>(hip_stream));
-  if (e != hipSuccess) {
-    g_create_error = std::string("HIP error in ") + name + ": " + hipGetErrorString(e);
-    return VSR_EHIP;
-  }
+  if (e != hipSuccess) return refuse(VSR_EHIP, name, hipGetErrorString(e));
   return VSR_OK;
 }
 
@@ -1748,10 +1760,7 @@ extern "C" int vsr_pick_tokens(const void *logits, int32_t dtype, int32_t rows, 
       return "workspace smaller than vsr_pick_workspace_size";
     return nullptr;
   };
-  if (const char *msg = check()) {
-    g_create_error = std::string("pick_tokens: ") + msg;
-    return VSR_EINVAL;
-  }
+  if (const char *msg = check()) return refuse(VSR_EINVAL, "pick_tokens", msg);
   if (rows == 0) return VSR_OK;
   a.logits = logits;
   a.stride = stride;
@@ -1776,10 +1785,7 @@ extern "C" int vsr_pick_tokens(const void *logits, int32_t dtype, int32_t rows, 
   a.logprob = logprob;
   a.token_stride = 1;
   const hipError_t e = launch_pick(a, dtype, workspace, static_cast<hipStream_t>(hip_stream));
-  if (e != hipSuccess) {
-    g_create_error = std::string("HIP error in pick_tokens: ") + hipGetErrorString(e);
-    return VSR_EHIP;
-  }
+  if (e != hipSuccess) return refuse(VSR_EHIP, "pick_tokens", hipGetErrorString(e));
   return VSR_OK;
 }
 

@@ -251,3 +251,37 @@ def test_no_rows_another_stream_and_a_captured_call():
         want = B.pick_tokens(logits, **kw)
         torch.cuda.synchronize()
         assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+def test_many_chunks_and_outputs_larger_than_the_caches():
+    """More chunks than lanes of a wave; processed logits above 64 MB."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    logits, kw = _inputs(torch, 2, 300001, "bf16", 21, 900, 90, True, "one", "rows")
+    processed = torch.empty((2, 300001), device="cuda")
+    token, logprob = B.pick_tokens(logits, processed=processed, **kw)
+    _check(torch, logits, kw, token, logprob, processed)
+    logits, kw = _inputs(torch, 130, 130003, "f16", 22, 40, 40, True, "none", "one")
+    processed = torch.empty((130, 130003), device="cuda")
+    assert processed.numel() * 4 > 64 << 20
+    token, logprob = B.pick_tokens(logits, processed=processed, **kw)
+    for r in (0, 64, 129):
+        one = {k: v if k == "mask" else v[r:r + 1] for k, v in kw.items()}
+        _check(torch, logits[r:r + 1], one, token[r:r + 1], logprob[r:r + 1], processed[r:r + 1])
+    assert torch.equal(processed.argmax(1).int().cpu(), token.cpu())
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, each with its own workspace."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    cases = [_inputs(torch, 24, 60001, "f32", s, 500, 200, True, "one", "rows") for s in (31, 32)]
+    want = [B.pick_tokens(x, **kw) for x, kw in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[B.pick_tokens(x, stream=s, **kw) for (x, kw), s in zip(cases, streams)]
+           for _ in range(5)]
+    torch.cuda.synchronize()
+    for pair in got:
+        for (t, p), (wt, wp) in zip(pair, want):
+            assert torch.equal(t, wt) and torch.equal(p, wp)

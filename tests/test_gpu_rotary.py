@@ -234,3 +234,24 @@ def test_another_stream_and_a_captured_call():
         graph.replay()
         torch.cuda.synchronize()
         assert all(map(torch.equal, outs, B.qk_norm_rope(rot, pos, q, k, ones, ones, 1e-6)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_outputs_larger_than_the_caches(dtype):
+    """Outputs above 64 MB are stored past the caches: the values of small calls on
+    the same tokens, bit for bit."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    T, hq, hk, hd = 4200 if dtype == "f32" else 8400, 28, 4, 128
+    assert T * (hq + hk) * hd * (4 if dtype == "f32" else 2) > 64 << 20
+    g = torch.Generator(device="cuda").manual_seed(6)
+    qkv = torch.randn((T, hq + hk, hd), generator=g, device="cuda").to(_dt(dtype))
+    q, k = qkv[:, :hq], qkv[:, hq:]
+    pos = torch.randint(0, 30000, (3, T), generator=g, device="cuda", dtype=torch.int32)
+    rot, ones = B.rotary((24, 20, 20), 1e6, True), torch.ones(hd, device="cuda")
+    big = B.qk_norm_rope(rot, pos, q, k, ones, ones, 1e-6)
+    for t0 in (0, 1000, T - 37):
+        part = slice(t0, t0 + 37)
+        small = B.qk_norm_rope(rot, pos[:, part], q[part], k[part], ones, ones, 1e-6)
+        torch.cuda.synchronize()
+        assert torch.equal(big[0][part], small[0]) and torch.equal(big[1][part], small[1])

@@ -254,3 +254,95 @@ def test_a_shared_mask_and_prefix_calls_between():
     assert all(map(torch.equal, first, again))
     t = first[0].cpu().numpy()
     assert np.all((allowed[t // 32] >> (t % 32).astype(np.uint32)) & 1 == 1)
+
+
+def test_the_binding_refuses_host_tensors_and_wrong_shapes():
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    cfg = SMALL_BF16
+    wl, v = _case(cfg, 4, False, max_new=3)
+    pos, nxt = _positions(cfg)
+    rot = B.rotary(SECTIONS[128], cfg.rope_base)
+    v.prefill(wl.visual, _ids(wl.prefix_ids))
+    prompts, lens, M = _ids(wl.cand_ids), [2] * cfg.n_cands, cfg.n_cands
+    ones = torch.ones(M, device="cuda")
+    out = torch.empty((M, 3), dtype=torch.int32, device="cuda")
+    for f in (lambda: v.set_positions(rot, torch.tensor(pos), nxt),
+              lambda: v.set_positions(rot, _ids(pos)[:2], nxt),
+              lambda: v.set_positions(rot, _ids(pos).long(), nxt),
+              lambda: v.draft_ruled(prompts.cpu(), lens, 3),
+              lambda: v.draft_ruled(prompts.long(), lens, 3),
+              lambda: v.draft_ruled(prompts.t().contiguous().t(), lens, 3),
+              lambda: v.draft_ruled(prompts, lens, 3, repetition=ones.cpu()),
+              lambda: v.draft_ruled(prompts, lens, 3, repetition=ones[:2]),
+              lambda: v.draft_ruled(prompts, lens, 3, bias=torch.zeros(1, 999, device="cuda")),
+              lambda: v.draft_ruled(prompts, lens, 3, out=(out.cpu(), None)),
+              lambda: v.draft_ruled(prompts, lens, 3, out=(out[:, :2], None)),
+              lambda: v.draft_ruled(prompts, lens, 2, out=(out, None)),
+              lambda: v.draft_ruled(prompts, lens, 3, workspace=torch.empty(1 << 20, dtype=torch.uint8))):
+        with pytest.raises(B.VsrError) as e:
+            f()
+        assert e.value.code == B.VSR_EINVAL
+    layers = wl.weights["layers"]
+    one = torch.ones(128, device="cuda", dtype=torch.bfloat16)
+    for bad in ([dict(layers[0], q_norm=one, k_norm=one), layers[1]],
+                [dict(lw, q_norm=one) for lw in layers],
+                [dict(lw, q_norm=one.float(), k_norm=one.float()) for lw in layers],
+                [dict(lw, q_norm=one[:64], k_norm=one[:64]) for lw in layers],
+                [dict(lw, q_norm=one.cpu(), k_norm=one.cpu()) for lw in layers]):
+        with pytest.raises(B.VsrError):
+            v.load_weights(dict(wl.weights, layers=bad))
+
+
+def test_a_decoder_without_layers():
+    torch = _torch()
+    cfg = SMALL_F32.replace(name="fp32 no layers", n_layers=0)
+    wl, v = _case(cfg, 8, False, max_new=3)
+    _place(cfg, v, False)
+    v.prefill(wl.visual, _ids(wl.prefix_ids))
+    lens = [3] * cfg.n_cands
+    a = v.draft(_ids(wl.cand_ids), lens, 3)
+    b, _ = v.draft_ruled(_ids(wl.cand_ids), lens, 3)
+    torch.cuda.synchronize()
+    assert torch.equal(a, b)
+
+
+def test_a_captured_draft():
+    """A ruled draft captured into a graph and replayed, with other work and other
+    rules' values between the replays."""
+    torch = _torch()
+    cfg = SMALL_BF16.replace(name="bf16 V1024", vocab=1024)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        wl, v = _case(cfg, 12, True, max_new=4)
+        pos, nxt, axis = _place(cfg, v, True)
+        v.prefill(wl.visual, _ids(wl.prefix_ids))
+        M, V = cfg.n_cands, cfg.vocab
+        prompts, lens = _ids(wl.cand_ids), [3, 1, 4, 2, 5]
+        rep = torch.full((M,), 1.3, device="cuda")
+        bias = torch.zeros((1, V), device="cuda")
+        from paper_2601_01513_amd import binding as B
+        import ctypes
+        ws = torch.empty(B.load_library().vsr_draft_ruled_workspace_size(ctypes.byref(v.c), M),
+                         dtype=torch.uint8, device="cuda")
+        out = (torch.empty((M, 4), dtype=torch.int32, device="cuda"),
+               torch.empty((M, 4), device="cuda"))
+        run = lambda o: v.draft_ruled(prompts, lens, 4, repetition=rep, bias=bias, out=o,  # noqa: E731
+                                      workspace=ws)
+        run(out)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            run(out)
+        seen = set()
+        for seed in range(3):
+            g = torch.Generator(device="cuda").manual_seed(seed)
+            bias.copy_(torch.randn((1, V), generator=g, device="cuda"))
+            graph.replay()
+            side.synchronize()
+            got = [t.clone() for t in out]
+            want = v.draft_ruled(prompts, lens, 4, repetition=rep, bias=bias)
+            side.synchronize()
+            assert all(map(torch.equal, got, want))
+            seen.add(tuple(got[0].flatten().tolist()))
+        assert len(seen) > 1
