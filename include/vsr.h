@@ -273,8 +273,7 @@ typedef struct vsr_heads {
  *            -1 for padding). Rows inside it must differ: of two tokens of
  *            one row either's values, or a mix, remain. Other rows of k_out are
  *            left as they are. k_cap: rows of k_out (with k_rows NULL: >= T).
- * All four of one dtype (VSR_F32, VSR_BF16, VSR_F16), element-aligned; rot / 2 and
- * (head_dim - rot) / 2 that are multiples of 8 (fp32: 4) are fastest. k_in and k_out may both be NULL. q_out may be q_in, and
+ * All four of one dtype (VSR_F32, VSR_BF16, VSR_F16), element-aligned. k_in and k_out may both be NULL. q_out may be q_in, and
  * k_out k_in (with k_rows NULL); other overlaps are refused, but for an output
  * in columns of stacked rows that the input does not use. Outputs must not
  * overlap themselves (one stride at least the other's whole extent), nor pos,

@@ -197,10 +197,11 @@ struct RotateArgs {
   const float2 *table;
   const int32_t *row_pos;
   float q_scale;
-  // Set by the launchers: lanes a head, steps over a token's heads, a wave's
-  // stride over tokens and steps, whether outputs are written past the caches, the
-  // angle ratio of pairs 2^b apart.
-  int lph, steps, next_t, next_step, past_caches;
+  // Set by the launchers: lanes a head, the first of them on pairs that turn, steps
+  // over a token's heads, a wave's stride over tokens and steps, whether lanes hold
+  // pairs twice or none, whether outputs are written past the caches, the angle ratio
+  // of pairs 2^b apart.
+  int lph, rot_chunks, steps, next_t, next_step, uneven, past_caches;
   double pair_step[kStepBits];
 };
 // dtype: a VSR_* value, of every tensor but the gains; norm: RMSNorm first.

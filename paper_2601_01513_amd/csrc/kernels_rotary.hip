@@ -143,15 +143,23 @@ __global__ __launch_bounds__(256) void k_rotate_heads(RotateArgs a, const int32_
              q_ohs = kept(a.q.out_hs), k_its = kept(a.k.in_ts), k_ihs = kept(a.k.in_hs),
              k_ots = kept(a.k.out_ts), k_ohs = kept(a.k.out_hs);
 
-  int lo[NCH], hi[NCH];
+  // A lane's chunks of VEC pairs: `rot_chunks` of them over the pairs that turn, then
+  // those over the pairs of dims >= rot, th apart. The last of each ends where its
+  // pairs end, so that it repeats up to VEC - 1 of the chunk before it (`twice`:
+  // read and written by both with the same values, summed once).
+  int s0[NCH], lo[NCH], hi[NCH], twice[NCH];
   bool on[NCH];
 #pragma unroll
   for (int c = 0; c < NCH; ++c) {
-    const int s0 = (li + c * a.lph) * VEC;
-    on[c] = s0 < half;
-    lo[c] = s0 < rh ? s0 : s0 + rh;  // the tail dims >= rot go in pairs th apart
-    hi[c] = s0 < rh ? s0 + rh : s0 + rh + th;
-    if (!on[c]) lo[c] = hi[c] = 0;
+    const int ch = li + c * a.lph;
+    const bool turns = ch < a.rot_chunks;
+    const int i = (turns ? ch : ch - a.rot_chunks) * VEC, n = turns ? rh : th;
+    const int i0 = min(i, n - VEC);
+    on[c] = i < n;
+    twice[c] = on[c] ? i - i0 : VEC;
+    s0[c] = on[c] ? (turns ? i0 : rh + i0) : 0;
+    lo[c] = on[c] ? (turns ? i0 : 2 * rh + i0) : 0;
+    hi[c] = on[c] ? lo[c] + n : 0;
   }
   // The angles of an item are computed once a pair, lane l those of pairs l and l
   // + 64: the axis and the turns per position, base^(-2i/rot) / 2 pi (a product of
@@ -249,20 +257,31 @@ __global__ __launch_bounds__(256) void k_rotate_heads(RotateArgs a, const int32_
     float ss = 0.f;
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-      // (Lanes past the head's pairs hold a copy of others: none of it counts.)
-      const bool have = on[c];
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        x[c][j] = have ? to_f32(it.v0[c].v[j]) : 0.f;
-        x[c][VEC + j] = have ? to_f32(it.v1[c].v[j]) : 0.f;
+        x[c][j] = to_f32(it.v0[c].v[j]);
+        x[c][VEC + j] = to_f32(it.v1[c].v[j]);
         if constexpr (SPLIT) {
-          x[c][j] += have ? to_f32(it.w0[c].v[j]) : 0.f;
-          x[c][VEC + j] += have ? to_f32(it.w1[c].v[j]) : 0.f;
+          x[c][j] += to_f32(it.w0[c].v[j]);
+          x[c][VEC + j] += to_f32(it.w1[c].v[j]);
         }
       }
-      if constexpr (NORM) {
+    }
+    if constexpr (NORM) {
+      const auto add = [&](bool even) {
 #pragma unroll
-        for (int j = 0; j < 2 * VEC; ++j) ss += x[c][j] * x[c][j];
+        for (int c = 0; c < NCH; ++c)
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) {
+            const float sq = x[c][j] * x[c][j] + x[c][VEC + j] * x[c][VEC + j];
+            ss += even || j >= twice[c] ? sq : 0.f;
+          }
+      };
+      if (a.uneven) {
+        asm volatile("");  // (a branch, not the masks of both)
+        add(false);
+      } else {
+        add(true);
       }
     }
     // The values are out of the item's registers before its next loads, so that
@@ -288,14 +307,13 @@ __global__ __launch_bounds__(256) void k_rotate_heads(RotateArgs a, const int32_
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       if (!(st && on[c])) continue;
-      const int s0 = (li + c * a.lph) * VEC;
       P o0, o1, l0, l1;
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const float cj = cosv[s0 + j], sj = sinv[s0 + j];
+        const float cj = cosv[s0[c] + j], sj = sinv[s0[c] + j];
         float y0 = x[c][j] * cj - x[c][VEC + j] * sj;
         float y1 = x[c][VEC + j] * cj + x[c][j] * sj;
-        if (th > 0 && lo[c] >= rh) {  // a dim >= rot meets no other, an infinity among them
+        if (th > 0 && s0[c] >= rh) {  // a dim >= rot meets no other, an infinity among them
           y0 = x[c][j];
           y1 = x[c][VEC + j];
         }
@@ -348,20 +366,31 @@ __global__ __launch_bounds__(256) void k_rotate_heads(RotateArgs a, const int32_
   while (it.t < a.T) work(it);
 }
 
-// Widest VEC (16 bytes at most) that the head's two parts allow.
+// Chunks of vec pairs over the pairs that turn and the others.
+int rot_chunks(const RotateArgs &a, int vec) { return (a.axes.rot / 2 + vec - 1) / vec; }
+int tail_chunks(const RotateArgs &a, int vec) {
+  return ((a.hd - a.axes.rot) / 2 + vec - 1) / vec;
+}
+
+// Widest VEC (16 bytes at most) that the head's two parts have pairs for and a wave
+// has lanes for.
 int pair_width(const RotateArgs &a, size_t esize) {
   const int rh = a.axes.rot / 2, th = a.hd / 2 - rh;
   int vec = (int)(16 / esize);
-  while (rh % vec || th % vec) vec /= 2;
+  while (vec > 1 && (rh < vec || (th > 0 && th < vec) ||
+                     rot_chunks(a, vec) + tail_chunks(a, vec) > 64))
+    vec /= 2;
   return vec;
 }
 
 template <typename T, int VEC, bool WIDE, bool NORM, bool SPLIT, bool TABLE>
 hipError_t launch_wide(RotateArgs a, hipStream_t s) {
-  const int chunks = a.hd / 2 / VEC;
+  a.rot_chunks = rot_chunks(a, VEC);
+  const int chunks = a.rot_chunks + tail_chunks(a, VEC);
   for (int b = 0; b < kStepBits; ++b) a.pair_step[b] = std::exp2(-a.log2_step * (1 << b));
   a.lph = 1;
   while (a.lph < chunks && a.lph < 64) a.lph *= 2;
+  a.uneven = a.axes.rot / 2 % VEC || (a.hd - a.axes.rot) / 2 % VEC || chunks % a.lph;
   const int hpw = 64 / a.lph;
   a.steps = (a.q.n + a.k.n + hpw - 1) / hpw;
   // Three blocks a CU: more keep more of the memory's rows open than it likes (16384
@@ -439,8 +468,8 @@ hipError_t launch_norm_cached(const RotateArgs &a, bool f32, hipStream_t s) {
   if (!f32)  // (head_dim 128; the workspace's planes are 256-byte aligned)
     return a.q.in_lo ? launch_wide<f16, 8, false, true, true, true>(a, s)
                      : launch_wide<f16, 8, false, true, false, true>(a, s);
-  return a.hd % 8 == 0 ? launch_vec<float, 4, true, false, true>(a, s)
-                       : launch_vec<float, 1, true, false, true>(a, s);
+  return a.hd >= 8 ? launch_vec<float, 4, true, false, true>(a, s)
+                   : launch_vec<float, 1, true, false, true>(a, s);
 }
 
 hipError_t launch_rotate_heads(const RotateArgs &a, int dtype, bool norm, hipStream_t s) {
