@@ -339,7 +339,7 @@ typedef struct vsr_token_rules {
 /* Token lists of the rows: row r's prompt is prompt[r prompt_stride + i], i <
  * prompt_len[r] (device [rows]; NULL: n_prompt for each; clamped to [0,
  * n_prompt]); likewise its output (the tokens picked so far). Ids outside [0,
- * vocab) are ignored. prompt and output may be NULL. */
+ * vocab) are ignored. n_prompt, n_output <= 2^30; prompt and output may be NULL. */
 typedef struct vsr_token_lists {
   const int32_t *prompt;
   int64_t prompt_stride;

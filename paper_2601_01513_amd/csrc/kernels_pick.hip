@@ -124,7 +124,28 @@ __global__ __launch_bounds__(NT) void k_pick_chunks(PickArgs a, Best *part) {
   const float *bias = a.bias ? a.bias + r * a.bias_stride : nullptr;
   const uint32_t *mask = a.mask ? a.mask + r * a.mask_stride : nullptr;
 
-  // Everything the chunk reads is on its way before the lists are counted. Loads
+  // The lists, four ids a load (16 rows with lists of 4600: 12.0 -> 11.3 us), the last
+  // load moved back to end with the list. The first of each goes out before all else, so that
+  // counting does not wait for the logits.
+  typedef Pack<int32_t, 4> I4;
+  const auto length = [&](const int32_t *list, const int32_t *len, int most) {
+    return !list ? 0 : len ? max(0, min(len[r], most)) : most;
+  };
+  const int32_t *prompt = a.prompt + r * a.prompt_stride, *output = a.output + r * a.output_stride;
+  const int np = length(a.prompt, a.prompt_len, a.n_prompt);
+  const int no = length(a.output, a.output_len, a.n_output);
+  const auto ids_at = [](const int32_t *ids, int n, int i) {
+    if (n >= 4) return *reinterpret_cast<const I4 *>(ids + min(i, n - 4));
+    I4 p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p.v[j] = j < n ? ids[j] : -1;
+    return p;
+  };
+  I4 first_p, first_o;
+  if (4 * tid < np) first_p = ids_at(prompt, np, 4 * tid);
+  if (4 * tid < no) first_o = ids_at(output, no, 4 * tid);
+
+  // Everything else the chunk reads is on its way before the lists are counted. Loads
   // past the row's end are moved back inside it (the pack the end cuts through is
   // read again below, the rest is not used).
   const auto at = [&](int k) { return v0 + (k * NT + tid) * VEC; };
@@ -153,11 +174,12 @@ __global__ __launch_bounds__(NT) void k_pick_chunks(PickArgs a, Best *part) {
   if (lists) {
     for (int i = tid; i < C; i += NT) cnt[i] = 0;
     __syncthreads();
-    const auto list = [&](const int32_t *ids, int n, bool output) {
-#pragma unroll 4
-      for (int i = tid; i < n; i += NT) {
-        const uint32_t o = (uint32_t)ids[i] - (uint32_t)v0;
-        if (o < (uint32_t)C) {
+    const auto count = [&](const I4 &p, int n, int i, bool output) {
+      const int from = n >= 4 ? i - min(i, n - 4) : 0;  // (the ones before were the last load's)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t o = (uint32_t)p.v[j] - (uint32_t)v0;
+        if (j >= from && o < (uint32_t)C) {
           if (output)
             atomicAdd(&cnt[o], 1u);
           else
@@ -165,12 +187,10 @@ __global__ __launch_bounds__(NT) void k_pick_chunks(PickArgs a, Best *part) {
         }
       }
     };
-    if (a.prompt)
-      list(a.prompt + r * a.prompt_stride, min(a.prompt_len ? a.prompt_len[r] : a.n_prompt, a.n_prompt),
-           false);
-    if (a.output)
-      list(a.output + r * a.output_stride, min(a.output_len ? a.output_len[r] : a.n_output, a.n_output),
-           true);
+    if (4 * tid < np) count(first_p, np, 4 * tid, false);
+    if (4 * tid < no) count(first_o, no, 4 * tid, true);
+    for (int i = 4 * (tid + NT); i < np; i += 4 * NT) count(ids_at(prompt, np, i), np, i, false);
+    for (int i = 4 * (tid + NT); i < no; i += 4 * NT) count(ids_at(output, no, i), no, i, true);
     __syncthreads();
   }
   const float rep = a.repetition ? a.repetition[r] : 1.f;

@@ -1747,9 +1747,9 @@ extern "C" int vsr_pick_tokens(const void *logits, int32_t dtype, int32_t rows, 
         return "processed overlaps logits";
     }
     if (lists) {
-      if (lists->n_prompt < 0 || lists->n_output < 0 || lists->prompt_stride < 0 ||
-          lists->output_stride < 0)
-        return "list sizes and strides must be >= 0";
+      if (lists->n_prompt < 0 || lists->n_output < 0 || lists->n_prompt > 1 << 30 ||
+          lists->n_output > 1 << 30 || lists->prompt_stride < 0 || lists->output_stride < 0)
+        return "list sizes must lie in [0, 2^30], strides be >= 0";
       if ((reinterpret_cast<uintptr_t>(lists->prompt) | reinterpret_cast<uintptr_t>(lists->output) |
            reinterpret_cast<uintptr_t>(lists->prompt_len) |
            reinterpret_cast<uintptr_t>(lists->output_len)) & 3)

@@ -131,7 +131,7 @@ def _pick(**kw):
     (dict(processed=MB + 400, processed_stride=1000), "overlaps"),
     (dict(processed=MB, processed_stride=1004), "overlaps"),
     (dict(processed=MB, processed_stride=1000, dtype=B.VSR_F16), "overlaps"),
-    (dict(n_prompt=-1), "list"), (dict(output_stride=-8), "list"), (dict(prompt=5 * MB + 2), "lists"),
+    (dict(n_prompt=-1), "list"), (dict(n_output=(1 << 30) + 1), "list"), (dict(output_stride=-8), "list"), (dict(prompt=5 * MB + 2), "lists"),
     (dict(prompt_len=5 * MB + 1), "lists"), (dict(ws=9 * MB + 8), "workspace"), (dict(wsb=47), "smaller"),
 ])
 def test_pick_tokens_refuses(kw, word):
