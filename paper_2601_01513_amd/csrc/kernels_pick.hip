@@ -89,12 +89,11 @@ typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 // steps in any fp32 arithmetic, so that equal logits stay equal.
 __device__ __forceinline__ float penalised(float l, uint32_t c, float rep, float freq, float pres) {
 #pragma clang fp contract(off)
-  if (c == 0) return l;
-  l = l > 0.f ? l / rep : l * rep;
+  const float t = l > 0.f ? l / rep : l * rep;
   const uint32_t n = c & 0x7fffffffu;
   const float a = freq * (float)n, b = n ? pres : 0.f;
   const float p = a + b;
-  return l - p;
+  return c ? t - p : l;
 }
 
 // A row's outputs, by one thread.
@@ -113,7 +112,7 @@ __device__ __forceinline__ void finish_row(const PickArgs &a, int r, const Best 
 // thread; cnt: the chunk's table where the row has lists.
 template <typename T, int NV, int NT>
 __global__ __launch_bounds__(NT) void k_pick_chunks(PickArgs a, Best *part) {
-  extern __shared__ uint32_t cnt[];
+  extern __shared__ __align__(16) uint32_t cnt[];
   __shared__ Best red[NT / 64];
   constexpr int VEC = 16 / sizeof(T), C = NT * NV * VEC;
   typedef Pack<T, VEC> P;
@@ -170,9 +169,12 @@ __global__ __launch_bounds__(NT) void k_pick_chunks(PickArgs a, Best *part) {
     for (int k = 0; k < NV; ++k) bits[k] = mask[min(at(k), a.vocab - 1) >> 5];
   }
 
+  const float rep = a.repetition ? a.repetition[r] : 1.f;
+  const float freq = a.frequency ? a.frequency[r] : 0.f;
+  const float pres = a.presence ? a.presence[r] : 0.f;
   const bool lists = a.prompt || a.output;
   if (lists) {
-    for (int i = tid; i < C; i += NT) cnt[i] = 0;
+    for (int i = 4 * tid; i < C; i += 4 * NT) *reinterpret_cast<u32x4 *>(cnt + i) = u32x4{};
     __syncthreads();
     const auto count = [&](const I4 &p, int n, int i, bool output) {
       const int from = n >= 4 ? i - min(i, n - 4) : 0;  // (the ones before were the last load's)
@@ -193,27 +195,38 @@ __global__ __launch_bounds__(NT) void k_pick_chunks(PickArgs a, Best *part) {
     for (int i = 4 * (tid + NT); i < no; i += 4 * NT) count(ids_at(output, no, i), no, i, true);
     __syncthreads();
   }
-  const float rep = a.repetition ? a.repetition[r] : 1.f;
-  const float freq = a.frequency ? a.frequency[r] : 0.f;
-  const float pres = a.presence ? a.presence[r] : 0.f;
-
   float x[NV][VEC];
   float *out = a.processed ? a.processed + r * a.processed_stride : nullptr;
   Best b{-INFINITY, INT32_MAX, 0.f};
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int v = at(k);
-    const bool cut = v < a.vocab && v + VEC > a.vocab;  // by the row's end
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      x[k][j] = to_f32(raw[k].v[j]);
-      if (cut) x[k][j] = v + j < a.vocab ? to_f32(logits[v + j]) : 0.f;
-      if (lists) x[k][j] = penalised(x[k][j], cnt[(k * NT + tid) * VEC + j], rep, freq, pres);
-      if (bias) {
-        float t = add[k][j / 4].v[j % 4];
-        if (cut) t = v + j < a.vocab ? bias[v + j] : 0.f;
-        x[k][j] += t;
+    for (int j = 0; j < VEC; ++j) x[k][j] = to_f32(raw[k].v[j]);
+    if (v < a.vocab && v + VEC > a.vocab) {  // cut by the row's end
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        x[k][j] = v + j < a.vocab ? to_f32(logits[v + j]) : 0.f;
+        if (bias) add[k][j / 4].v[j % 4] = v + j < a.vocab ? bias[v + j] : 0.f;
       }
+    }
+    if (lists) {
+      uint32_t c[VEC], any = 0;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        if (j % 4 == 0)
+          *reinterpret_cast<u32x4 *>(c + j) =
+              *reinterpret_cast<const u32x4 *>(cnt + (k * NT + tid) * VEC + j);
+        any |= c[j];
+      }
+      if (any) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[k][j] = penalised(x[k][j], c[j], rep, freq, pres);
+      }
+    }
+    if (bias) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[k][j] += add[k][j / 4].v[j % 4];
     }
     // (v is a multiple of VEC, so that a pack's bits lie in one word.)
     const uint32_t allowed = mask ? bits[k] >> (v & 31) : ~0u;
