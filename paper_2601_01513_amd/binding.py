@@ -432,7 +432,7 @@ class Verifier:
 
         given(prompt_ids, torch.int32, (M, cmax), "prompt_ids")
         if mask is not None and mask.dim() == 3:
-            if int(mask.shape[0]) != int(n_new):
+            if not 0 < int(n_new) == int(mask.shape[0]):
                 raise VsrError(VSR_EINVAL, "mask: one row of masks a step expected")
             step = mask.stride(0)
             rules = _token_rules(torch, M, self.cfg.vocab, dev, repetition, presence, frequency,
@@ -441,15 +441,15 @@ class Verifier:
             rules = _token_rules(torch, M, self.cfg.vocab, dev, repetition, presence, frequency,
                                  bias, mask)
         if out is None:
-            out = (torch.empty((M, int(n_new)), dtype=torch.int32, device=self.device),
-                   torch.empty((M, int(n_new)), dtype=torch.float32, device=self.device))
+            out = tuple(_empty(torch, (M, max(int(n_new), 0)), dt, self.device, self.stream)
+                        for dt in (torch.int32, torch.float32))
         if workspace is None:
             size = self.lib.vsr_draft_ruled_workspace_size(ctypes.byref(self.c), M)
             workspace = _empty(torch, max(size, 256), torch.uint8, self.device, self.stream)
         tokens, logprobs = out
-        given(tokens, torch.int32, (M, int(n_new)), "tokens")
+        given(tokens, torch.int32, (M, max(int(n_new), 0)), "tokens")
         if logprobs is not None:
-            given(logprobs, torch.float32, (M, int(n_new)), "logprobs")
+            given(logprobs, torch.float32, (M, max(int(n_new), 0)), "logprobs")
         given(workspace, torch.uint8, (workspace.numel(),), "workspace")
         self._check(self.lib.vsr_draft_ruled(
             self.h, _ptr(prompt_ids), lens, M, cmax, int(n_new), ctypes.byref(rules), step,
@@ -539,6 +539,8 @@ def _call(torch, dev, stream, f, args):
     current stream."""
     if dev < 0:
         raise VsrError(VSR_EINVAL, "device tensors expected")
+    if stream is not None and stream.device_index != dev:
+        raise VsrError(VSR_EINVAL, "a stream of the tensors' device expected")
     st = stream.cuda_stream if stream is not None else _raw_stream(dev)
     if dev == _device_now():
         rc = f(*args, st)

@@ -267,6 +267,7 @@ def test_the_binding_refuses_host_tensors_and_wrong_shapes():
     prompts, lens, M = _ids(wl.cand_ids), [2] * cfg.n_cands, cfg.n_cands
     ones = torch.ones(M, device="cuda")
     out = torch.empty((M, 3), dtype=torch.int32, device="cuda")
+    mask = torch.zeros((3, 1, (cfg.vocab + 31) // 32), dtype=torch.int32, device="cuda")
     for f in (lambda: v.set_positions(rot, torch.tensor(pos), nxt),
               lambda: v.set_positions(rot, _ids(pos)[:2], nxt),
               lambda: v.set_positions(rot, _ids(pos).long(), nxt),
@@ -279,10 +280,16 @@ def test_the_binding_refuses_host_tensors_and_wrong_shapes():
               lambda: v.draft_ruled(prompts, lens, 3, out=(out.cpu(), None)),
               lambda: v.draft_ruled(prompts, lens, 3, out=(out[:, :2], None)),
               lambda: v.draft_ruled(prompts, lens, 2, out=(out, None)),
+              lambda: v.draft_ruled(prompts, lens, 0, mask=mask[:0]),
+              lambda: v.draft_ruled(prompts, lens, -1, mask=mask),
               lambda: v.draft_ruled(prompts, lens, 3, workspace=torch.empty(1 << 20, dtype=torch.uint8))):
         with pytest.raises(B.VsrError) as e:
             f()
         assert e.value.code == B.VSR_EINVAL
+    for n_new in (0, -1, 4):  # the library's own answer, as draft()'s
+        with pytest.raises(B.VsrError) as e:
+            v.draft_ruled(prompts, lens, n_new)
+        assert e.value.code == B.VSR_ERANGE
     layers = wl.weights["layers"]
     one = torch.ones(128, device="cuda", dtype=torch.bfloat16)
     for bad in ([dict(layers[0], q_norm=one, k_norm=one), layers[1]],

@@ -199,6 +199,15 @@ def test_the_binding_refuses_what_the_library_cannot_see():
         assert e.value.code == B.VSR_EINVAL, i
 
 
+def test_a_stream_of_another_device_is_refused():
+    """Before anything is launched on it."""
+    torch = pytest.importorskip("torch")
+    stream, calls = type("Stream", (), {"device_index": 1, "cuda_stream": 0})(), []
+    with pytest.raises(B.VsrError) as e:
+        B._call(torch, 0, stream, lambda *a: calls.append(a), ())
+    assert e.value.code == B.VSR_EINVAL and "stream" in str(e.value) and not calls
+
+
 def test_plain_forms_by_hand():
     """The comparison's own pieces: axes of pairs, a quarter turn, the rules."""
     assert list(PD.axis_of_pair((2, 1, 1), False)) == [0, 0, 1, 2]
