@@ -273,14 +273,16 @@ typedef struct vsr_heads {
  *            -1 for padding). Rows inside it must differ: of two tokens of
  *            one row either's values, or a mix, remain. Other rows of k_out are
  *            left as they are. k_cap: rows of k_out (with k_rows NULL: >= T).
- * All four of one dtype (VSR_F32, VSR_BF16, VSR_F16), element-aligned. k_in and k_out may both be NULL. q_out may be q_in, and
- * k_out k_in (with k_rows NULL); other overlaps are refused, but for an output
- * in columns of stacked rows that the input does not use. Outputs must not
+ * All four of one dtype (VSR_F32, VSR_BF16, VSR_F16), element-aligned. k_in and
+ * k_out may both be NULL. q_out may be q_in, and k_out k_in (with k_rows NULL);
+ * other overlaps are refused, but for an output in columns of stacked rows that
+ * the input does not use. Outputs must not
  * overlap themselves (one stride at least the other's whole extent), nor pos,
  * k_rows or the gains.
  * head_dim even, 2 to 256, >= rot; 0 <= T <= 2^30 (0: nothing is done); n_heads 1
- * to 4096 (a NULL k: none); k_cap < 2^31; no set of heads spans over 2^46 elements. Enqueued on hip_stream, whose device must be the
- * current one; errors via vsr_last_error(NULL). */
+ * to 4096 (a NULL k: none); k_cap < 2^31; no set of heads spans over 2^46
+ * elements. Enqueued on hip_stream, whose device must be the current one; errors
+ * via vsr_last_error(NULL). */
 int vsr_rope_axes(const vsr_rotary *rot, int32_t dtype, int32_t head_dim, int32_t T,
                   const int32_t *pos, int64_t pos_stride, const vsr_heads *q_in,
                   const vsr_heads *q_out, const vsr_heads *k_in, const vsr_heads *k_out,
@@ -371,7 +373,8 @@ size_t vsr_pick_workspace_size(int32_t rows, int32_t vocab);
  *   workspace : device, >= vsr_pick_workspace_size(rows, vocab) bytes, 16-byte
  *               aligned, caller-owned; calls that overlap in time need their own
  *               (two captured graphs that share one must not replay at once).
- * Outputs must not overlap inputs, but for processed as above. 0 <= rows <= 65535 (0: nothing is done), 1 <= vocab <= 2^24.
+ * Outputs must not overlap inputs, but for processed as above. 0 <= rows <= 65535
+ * (0: nothing is done), 1 <= vocab <= 2^24.
  * Enqueued on hip_stream, whose device must be the current one; errors via
  * vsr_last_error(NULL). */
 int vsr_pick_tokens(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,

@@ -285,3 +285,18 @@ def test_two_calls_at_once():
     for pair in got:
         for (t, p), (wt, wp) in zip(pair, want):
             assert torch.equal(t, wt) and torch.equal(p, wp)
+
+
+def test_rows_far_apart():
+    """Offsets that pass 2^31 elements, of the logits and of the kept ones."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    rows, V, stride = 3, 5001, 1_100_000_003
+    assert (rows - 1) * stride > 2 ** 31
+    x, kw = _inputs(torch, rows, V, "bf16", 41, 30, 30, True, "rows", "rows")
+    far = torch.empty((rows - 1) * stride + V, dtype=torch.bfloat16,
+                      device="cuda").as_strided((rows, V), (stride, 1))
+    far.copy_(x)
+    kept = torch.empty((rows - 1) * stride + V, device="cuda").as_strided((rows, V), (stride, 1))
+    token, logprob = B.pick_tokens(far, processed=kept, **kw)
+    _check(torch, x, kw, token, logprob, kept)

@@ -255,3 +255,41 @@ def test_outputs_larger_than_the_caches(dtype):
         small = B.qk_norm_rope(rot, pos[:, part], q[part], k[part], ones, ones, 1e-6)
         torch.cuda.synchronize()
         assert torch.equal(big[0][part], small[0]) and torch.equal(big[1][part], small[1])
+
+
+def test_a_long_cache_and_far_rows():
+    """Offsets that pass 2^31 elements, of the queries read and the keys stored; other
+    rows of the cache, the last ones among them, as they were."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    T, hk, hd, cap, stride = 5, 3, 128, 6_000_000, 550_000_008
+    assert hk * cap * hd > 2 ** 31 and (T - 1) * stride > 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(12)
+    far = torch.empty((T - 1) * stride + 2 * hd, dtype=torch.float16, device="cuda")
+    q = far.as_strided((T, 2, hd), (stride, hd, 1))
+    q.copy_(torch.randn((T, 2, hd), generator=g, device="cuda"))
+    k = torch.randn((T, hk, hd), generator=g, device="cuda").half()
+    cache = torch.empty((hk, cap, hd), dtype=torch.float16, device="cuda")
+    near = cache[:, cap - 20:]
+    near.fill_(7.0)
+    slots = torch.tensor([cap - 18, cap - 3, cap - 19, cap - 9, cap - 2], dtype=torch.int32,
+                         device="cuda")
+    pos = torch.randint(0, 6_000_000, (1, T), generator=g, device="cuda", dtype=torch.int32)
+    rot, ones = B.rotary((64,), 1e6), torch.ones(hd, device="cuda")
+    want = B.qk_norm_rope(rot, pos, q.contiguous(), k, ones, ones, 1e-6)
+    B.qk_norm_rope(rot, pos, q, k, ones, ones, 1e-6, q_out=q, k_out=cache.transpose(0, 1),
+                   k_rows=slots)
+    torch.cuda.synchronize()
+    assert torch.equal(q, want[0])
+    at = (slots - (cap - 20)).long()
+    assert torch.equal(near[:, at], want[1].transpose(0, 1))
+    left = torch.ones(20, dtype=torch.bool, device="cuda")
+    left[at] = False
+    assert bool((near[:, left] == 7).all())
+    # Without slots: the first T rows only.
+    cache[:, :T + 3] = 7.0
+    B.rope_axes(rot, pos, q, k, k_out=cache.transpose(0, 1))
+    _, plain = B.rope_axes(rot, pos, q, k)
+    torch.cuda.synchronize()
+    assert torch.equal(cache[:, :T], plain.transpose(0, 1))
+    assert bool((cache[:, T:T + 3] == 7).all())
