@@ -184,10 +184,15 @@ __global__ __launch_bounds__(256) void k_rotate_heads(RotateArgs a, const int32_
     int p[NA], krow;
     float2 cs[NA];
   };
-  // (A lane's own load of the key row: a scalar one would hold up the LDS reads.)
+  // (A lane's own load of the key row: a scalar one would hold up the LDS reads.
+  // Without k_rows the load goes to rows that hold a word a token, unused: positions,
+  // or, where token t takes table row t, the table's.)
   int zero = 0;
   asm volatile("" : "+v"(zero));
-  const int32_t *const krows = k_rows ? k_rows : TABLE ? reinterpret_cast<const int32_t *>(a.table) : pos;
+  const int32_t *const krows = k_rows    ? k_rows
+                               : !TABLE  ? pos
+                               : row_pos ? row_pos
+                                         : reinterpret_cast<const int32_t *>(a.table);
   int nt, nh;  // the next item to load: token and step over its heads
   {
     const int first = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + w);

@@ -353,3 +353,27 @@ def test_a_captured_draft():
             assert all(map(torch.equal, got, want))
             seen.add(tuple(got[0].flatten().tolist()))
         assert len(seen) > 1
+
+
+def test_more_candidate_rows_than_the_rotary_table_has_words():
+    """256 candidates of up to 4 tokens after a prefix of 1, heads of 2: 1024 rows
+    normed and rotated against a table of 68 rows of one pair."""
+    torch = _torch()
+    cfg = SMALL_F32.replace(name="fp32 hd2 256 candidates", head_dim=2, n_cands=256, cand_len=4,
+                            n_prefix=1, n_visual=0, vocab=64)
+    wl, v = _case(cfg, 13, True)
+    hw = W.host_weights(wl.weights)
+    lens = np.arange(256) % 5
+    ids = _ids(wl.prefix_ids)
+    v.prefill(None, ids)
+    two = v.score(_ids(wl.cand_ids), lens)[0].clone()
+    one = v.verify(None, ids, _ids(wl.cand_ids), lens)[0]
+    torch.cuda.synchronize()
+    pos, axis = np.zeros((1, 1), np.int64), PD.axis_of_pair((1,), False)
+    for m in range(0, 256, 9):
+        branch = wl.cand_ids[m, :lens[m]]
+        lp = _log_softmax(PD.logits_after(cfg, hw, np.zeros((0, cfg.d_model)), wl.prefix_ids,
+                                          branch, pos, 1, axis))
+        want = lp[np.arange(len(branch)), branch]
+        for got in (two, one):
+            assert np.all(np.abs(got[m, :lens[m]].cpu().numpy() - want) <= 1e-4), m
