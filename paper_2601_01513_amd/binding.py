@@ -246,6 +246,14 @@ def _ptr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
 
+def _hold(stream, *tensors):
+    """Memory of `tensors` that are dropped is not reused before `stream` is past
+    the work queued on it by then."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+
+
 class Verifier:
     """One vsr context: workspace, borrowed weights and the current prefix.
 
@@ -314,6 +322,7 @@ class Verifier:
         self._check(self.lib.vsr_load_weights(self.h, ctypes.byref(cw)))
         if gains or self._has_qk_norm:
             arrs = [(ctypes.c_void_p * L)(*map(_ptr, ts)) if gains else None for ts in norms]
+            _hold(self.stream, *gains)
             self._check(self.lib.vsr_load_qk_norms(self.h, *[ctypes.cast(a, _PP) for a in arrs]))
         self._has_qk_norm, self._qk_norm = bool(gains), norms
 
@@ -327,7 +336,7 @@ class Verifier:
             return
         P = int(pos.shape[-1])
         stride = _check_pos(_torch_names(), rot, pos, P, self.workspace.get_device())
-        self._pos = pos
+        _hold(self.stream, pos)
         self._check(self.lib.vsr_set_positions(self.h, ctypes.byref(rot), _ptr(pos), stride, P,
                                                int(next)))
 
@@ -451,6 +460,8 @@ class Verifier:
         if logprobs is not None:
             given(logprobs, torch.float32, (M, max(int(n_new), 0)), "logprobs")
         given(workspace, torch.uint8, (workspace.numel(),), "workspace")
+        _hold(self.stream, prompt_ids, repetition, presence, frequency, bias, mask, tokens,
+              logprobs, workspace)
         self._check(self.lib.vsr_draft_ruled(
             self.h, _ptr(prompt_ids), lens, M, cmax, int(n_new), ctypes.byref(rules), step,
             _ptr(tokens), _ptr(logprobs), _ptr(workspace), workspace.numel()))

@@ -377,3 +377,53 @@ def test_more_candidate_rows_than_the_rotary_table_has_words():
         want = lp[np.arange(len(branch)), branch]
         for got in (two, one):
             assert np.all(np.abs(got[m, :lens[m]].cpu().numpy() - want) <= 1e-4), m
+
+
+def test_tensors_of_another_stream_dropped_at_once():
+    """A context on a stream of its own, behind long work there; positions, prompts
+    and rules made on the current stream, dropped after the call, their memory
+    given to others: the results of the kept ones."""
+    torch = _torch()
+    cfg = SMALL_BF16
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        wl, v = _case(cfg, 15, False, max_new=4)
+        busy = torch.randn((4096, 4096), device="cuda")
+    side.synchronize()
+    pos, nxt = _positions(cfg)
+    from paper_2601_01513_amd import binding as B
+    rot, lens, M = B.rotary(SECTIONS[128], cfg.rope_base), [3, 1, 4, 2, 5], cfg.n_cands
+    rng = np.random.default_rng(15)
+    bias = (4 * rng.normal(size=(M, cfg.vocab))).astype(np.float32)
+    rep = rng.uniform(1, 2, M).astype(np.float32)
+    prefix = _ids(wl.prefix_ids)
+
+    def run(drop):
+        kept = []
+        if drop:
+            with torch.cuda.stream(side):
+                for _ in range(20):
+                    torch.mm(busy, busy)
+        made = _ids(pos)
+        v.set_positions(rot, made, nxt)
+        if drop:
+            del made
+            kept.append(_ids(np.zeros_like(pos)))
+        v.prefill(wl.visual, prefix)
+        made = [_ids(wl.cand_ids), torch.tensor(rep, device="cuda"), torch.tensor(bias, device="cuda")]
+        out = v.draft_ruled(made[0], lens, 4, repetition=made[1], bias=made[2])
+        if drop:
+            del made
+            kept += [_ids(np.zeros_like(wl.cand_ids)), torch.ones(M, device="cuda"),
+                     torch.zeros((M, cfg.vocab), device="cuda")]
+        else:
+            kept.append(made)
+        side.synchronize()
+        return [t.clone() for t in out], kept
+
+    torch.cuda.synchronize()
+    want, _ = run(False)
+    torch.cuda.synchronize()
+    got, _ = run(True)
+    torch.cuda.synchronize()
+    assert all(map(torch.equal, got, want))

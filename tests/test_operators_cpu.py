@@ -220,3 +220,52 @@ def test_plain_forms_by_hand():
     y = PD.apply_rules(l, [0, -1, 9], [1, 1, 3], 2.0, 0.5, 0.25, np.full(5, 1.0, np.float32),
                        np.array([0b01111], np.uint32))
     assert np.array_equal(y, np.array([2.0, -4.0, 2.0, 2.25, -np.inf], np.float32))
+
+
+class _Ok:
+    """A library whose every call succeeds and does nothing."""
+    def __getattr__(self, name):
+        return lambda *a: B.VSR_OK
+
+
+@pytest.fixture
+def held(monkeypatch):
+    """[(tensor, stream)] of the record_stream calls."""
+    torch = pytest.importorskip("torch")
+    _lib()
+    seen = []
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: seen.append((t, s)))
+    return seen
+
+
+def _all_held(held, stream, tensors):
+    ptrs = {t.data_ptr() for t, s in held if s is stream}
+    return all(t.data_ptr() in ptrs for t in tensors)
+
+
+def test_a_contexts_tensors_are_held_for_its_stream(held):
+    """What a draft, positions and gains read or write on the context's stream is
+    recorded on it, whatever stream it was made on."""
+    import torch
+    v = B.Verifier.__new__(B.Verifier)
+    v.lib, v.h, v.stream, v.device = _Ok(), 1, object(), torch.device("cpu")
+    v.cfg = W.VerifierConfig(
+        name="held", n_layers=1, d_model=8, n_heads=1, n_kv_heads=1, head_dim=8, d_ff=8, vocab=40,
+        rope_base=1e4, dtype=W.F32, n_prefix=4, n_visual=0, n_cands=2, cand_len=3)
+    v.workspace = torch.empty(16, dtype=torch.uint8)
+    v.gemm_f16, v._has_qk_norm = False, False
+    i32 = lambda *s: torch.ones(s, dtype=torch.int32)  # noqa: E731
+    prompts, out, ws = i32(2, 3), (i32(2, 5), torch.ones(2, 5)), torch.empty(64, dtype=torch.uint8)
+    rules = dict(repetition=torch.ones(2), presence=torch.ones(2), frequency=torch.ones(2),
+                 bias=torch.ones(1, 40), mask=i32(5, 2, 2))
+    v.draft_ruled(prompts, [1, 2], 5, out=out, workspace=ws, **rules)
+    assert _all_held(held, v.stream, [prompts, ws, *out, *rules.values()])
+    pos = i32(1, 4)
+    v.set_positions(B.rotary((4,), 1e4), pos, 4)
+    assert _all_held(held, v.stream, [pos])
+    layer = {k: torch.ones(8) for k in
+             ("attn_norm", "wqkv", "wo", "ffn_norm", "wgu", "wdown", "q_norm", "k_norm")}
+    v.load_weights(dict(embed=torch.ones(8), lm_head=torch.ones(8), final_norm=torch.ones(8),
+                        layers=[layer]))
+    assert _all_held(held, v.stream, [layer["q_norm"], layer["k_norm"]])
+    v.h = None
