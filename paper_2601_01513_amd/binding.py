@@ -545,14 +545,18 @@ def _torch_names():
     return torch
 
 
-def _call(torch, dev, stream, f, args):
+def _call(torch, dev, stream, f, args, tensors=()):
     """f(*args, stream handle) with device index dev current, on `stream` or dev's
-    current stream."""
+    current stream. tensors: what f reads and writes (held for a given stream)."""
     if dev < 0:
         raise VsrError(VSR_EINVAL, "device tensors expected")
     if stream is not None and stream.device_index != dev:
         raise VsrError(VSR_EINVAL, "a stream of the tensors' device expected")
-    st = stream.cuda_stream if stream is not None else _raw_stream(dev)
+    if stream is None:
+        st = _raw_stream(dev)
+    else:
+        st = stream.cuda_stream
+        _hold(stream, *tensors)
     if dev == _device_now():
         rc = f(*args, st)
     else:
@@ -614,8 +618,9 @@ def _rotate(rot, pos, q, k, gains, eps, q_out, k_out, k_rows, stream):
         raise VsrError(VSR_EINVAL, "k_out and k_rows need k")
     head = (ctypes.byref(rot), vsr_dtype, hd, T, pos.data_ptr(), pos_stride)
     tail = (ctypes.byref(qi), ctypes.byref(qo), ki, ko, rows, cap)
+    tensors = (pos, q, k, q_out, k_out, k_rows, *(gains or ()))
     if gains is None:
-        _call(torch, dev, stream, _lib.vsr_rope_axes, head + tail)
+        _call(torch, dev, stream, _lib.vsr_rope_axes, head + tail, tensors)
         return q_out, k_out
     gq, gk = gains
     for g in gains if k is not None else gains[:1]:
@@ -624,7 +629,7 @@ def _rotate(rot, pos, q, k, gains, eps, q_out, k_out, k_rows, stream):
             raise VsrError(VSR_EINVAL, "gains: contiguous [head_dim] tensors of one float dtype "
                                        "expected")
     _call(torch, dev, stream, _lib.vsr_qk_norm_rope,
-          head + (gq.data_ptr(), _ptr(gk), _float_types.get(gq.dtype, -1), eps) + tail)
+          head + (gq.data_ptr(), _ptr(gk), _float_types.get(gq.dtype, -1), eps) + tail, tensors)
     return q_out, k_out
 
 
@@ -758,7 +763,9 @@ def pick_tokens(logits, prompt=None, prompt_len=None, output=None, output_len=No
     _call(torch, dev, stream, lib.vsr_pick_tokens,
           (logits.data_ptr(), dtype, rows, vocab, stride, lists, rules, kept, kept_stride,
            token.data_ptr(), _ptr(logprob), workspace.data_ptr(),
-           workspace.numel() * workspace.element_size()))
+           workspace.numel() * workspace.element_size()),
+          (logits, prompt, prompt_len, output, output_len, repetition, presence, frequency, bias,
+           mask, processed, token, logprob, workspace))
     return token, logprob
 
 

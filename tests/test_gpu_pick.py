@@ -300,3 +300,27 @@ def test_rows_far_apart():
     kept = torch.empty((rows - 1) * stride + V, device="cuda").as_strided((rows, V), (stride, 1))
     token, logprob = B.pick_tokens(far, processed=kept, **kw)
     _check(torch, x, kw, token, logprob, kept)
+
+
+def test_inputs_dropped_behind_another_streams_work():
+    """Picks on a busy stream; their lists, rules and logits dropped after the call
+    and their memory given to others."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    make = lambda: _inputs(torch, 8, 30001, "f32", 51, 300, 100, True, "rows", "rows")  # noqa: E731
+    logits, kw = make()
+    want = B.pick_tokens(logits, **kw)
+    side = torch.cuda.Stream()
+    busy = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    logits, kw = make()
+    shapes = [(t.shape, t.dtype) for t in (logits, *kw.values())]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            torch.mm(busy, busy)
+    got = B.pick_tokens(logits, stream=side, **kw)
+    del logits, kw
+    others = [torch.ones(shape, dtype=dtype, device="cuda") for shape, dtype in shapes]
+    torch.cuda.synchronize()
+    assert all(map(torch.equal, got, want)) and len(others) == len(shapes)

@@ -293,3 +293,40 @@ def test_a_long_cache_and_far_rows():
     torch.cuda.synchronize()
     assert torch.equal(cache[:, :T], plain.transpose(0, 1))
     assert bool((cache[:, T:T + 3] == 7).all())
+
+
+def test_inputs_dropped_behind_another_streams_work():
+    """Heads, positions, gains and slots of a call on a busy stream, dropped after it
+    and their memory given to others."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    T, hd = 300, 128
+    rot = B.rotary((24, 20, 20), 1e6, True)
+
+    def make():
+        g = torch.Generator(device="cuda").manual_seed(61)
+        n = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+        pos = torch.randint(0, 9000, (3, T), generator=g, device="cuda", dtype=torch.int32)
+        slots = torch.randperm(T, generator=g, device="cuda").to(torch.int32)
+        return pos, n(T, 8, hd).half(), n(T, 2, hd).half(), n(hd), n(hd), slots
+
+    def call(made, **kw):
+        pos, q, k, gq, gk, slots = made
+        return B.qk_norm_rope(rot, pos, q, k, gq, gk, 1e-6, k_rows=slots, **kw)
+
+    outs = [[torch.empty((T, n, hd), dtype=torch.float16, device="cuda") for n in (8, 2)]
+            for _ in range(2)]
+    call(make(), q_out=outs[0][0], k_out=outs[0][1])
+    side = torch.cuda.Stream()
+    busy = torch.randn((4096, 4096), device="cuda")
+    made = make()
+    shapes = [(t.shape, t.dtype) for t in made]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            torch.mm(busy, busy)
+    call(made, q_out=outs[1][0], k_out=outs[1][1], stream=side)
+    del made
+    others = [torch.ones(shape, dtype=dtype, device="cuda") for shape, dtype in shapes]
+    torch.cuda.synchronize()
+    assert all(map(torch.equal, *outs)) and len(others) == len(shapes)

@@ -269,3 +269,34 @@ def test_a_contexts_tensors_are_held_for_its_stream(held):
                         layers=[layer]))
     assert _all_held(held, v.stream, [layer["q_norm"], layer["k_norm"]])
     v.h = None
+
+
+def test_calls_on_a_given_stream_hold_their_tensors(held, monkeypatch):
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    B._torch_names()
+    for name, value in (("_lib", _Ok()), ("_device_now", lambda: 0), ("_raw_stream", lambda d: 0)):
+        monkeypatch.setattr(B, name, value)
+    stream = type("Stream", (), {"device_index": 0, "cuda_stream": 0})()
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    q, k, pos, rot = torch.ones(4, 2, 8), torch.ones(4, 1, 8), i32(2, 4), B.rotary((2, 2), 1e4)
+    heads = dict(q_out=q.clone(), k_out=k.clone(), k_rows=i32(4))
+    gains = torch.ones(8), torch.ones(8)
+    x, f32 = torch.ones(3, 100), lambda: torch.ones(3)
+    pick = dict(prompt=i32(3, 5), prompt_len=i32(3), output=i32(3, 5), output_len=i32(3),
+                repetition=f32(), presence=f32(), frequency=f32(), bias=torch.ones(1, 100),
+                mask=i32(1, 4), processed=torch.ones(3, 100),
+                workspace=torch.ones(64, dtype=torch.uint8))
+    out = i32(3), f32()
+    calls = [(lambda s: B.rope_axes(rot, pos, q, k, stream=s, **heads), [pos, q, k, *heads.values()]),
+             (lambda s: B.qk_norm_rope(rot, pos, q, k, *gains, 1e-6, stream=s, **heads),
+              [pos, q, k, *gains, *heads.values()]),
+             (lambda s: B.qk_norm_rope(rot, pos, q, None, gains[0], None, 1e-6, q_out=q, stream=s),
+              [pos, q, gains[0]]),
+             (lambda s: B.pick_tokens(x, stream=s, out=out, **pick), [x, *out, *pick.values()])]
+    for i, (call, tensors) in enumerate(calls):
+        held.clear()
+        call(None)  # (the current stream's own order holds them)
+        assert not held, i
+        call(stream)
+        assert _all_held(held, stream, tensors), i
