@@ -135,6 +135,16 @@ hipError_t launch_draft_rows(const Branches &br, int P, int S, const int32_t *id
                              int32_t *cache_row, int32_t *lm_tgt, hipStream_t s);
 hipError_t launch_draft_step(const Branches &br, int P, int S, int step, int32_t *row_lo,
                              int32_t *row_pos, int32_t *cache_row, hipStream_t s);
+// Runs of value-cache positions that a pass reads but does not write, set to zero.
+struct ClearSlots {
+  int n = 0;
+  struct Run {
+    char *at;           // the first row's first byte
+    long rows, stride;  // bytes from row to row
+    int len;            // bytes a row; all multiples of 16
+  } run[4];
+};
+hipError_t launch_clear_slots(const ClearSlots &c, hipStream_t s);
 template <typename TW, typename TA>
 hipError_t launch_branch_last_norm(const float *x, const Branches &br, const TW *g, int d,
                                    float eps, TA *y, hipStream_t s);

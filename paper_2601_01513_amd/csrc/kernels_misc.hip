@@ -97,6 +97,24 @@ hipError_t launch_draft_rows(const Branches &br, int P, int S, const int32_t *id
   return hipGetLastError();
 }
 
+// A thread writes 16 bytes at a time; grid.y is the run.
+__global__ __launch_bounds__(256) void k_clear_slots(ClearSlots c) {
+  const ClearSlots::Run r = c.run[blockIdx.y];
+  const int chunks = r.len / 16;
+  const long n = r.rows * chunks;
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256)
+    *reinterpret_cast<u32x4 *>(r.at + i / chunks * r.stride + i % chunks * 16) = u32x4{};
+}
+
+hipError_t launch_clear_slots(const ClearSlots &c, hipStream_t s) {
+  long most = 0;
+  for (int i = 0; i < c.n; ++i) most = std::max(most, c.run[i].rows * (c.run[i].len / 16));
+  if (most == 0) return hipSuccess;
+  const unsigned blocks = (unsigned)std::min<long>((most + 255) / 256, 2048);
+  k_clear_slots<<<dim3(blocks, c.n), 256, 0, s>>>(c);
+  return hipGetLastError();
+}
+
 // Decode step s >= 1: row m is new token s - 1 of branch m, at branch offset
 // n_m + s - 1.
 __global__ void k_draft_step(Branches br, int P, int S, int step, int32_t *row_lo,

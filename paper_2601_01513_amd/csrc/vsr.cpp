@@ -786,6 +786,39 @@ int run_layers(vsr_ctx *c, int rows, int mode, const Split &split) {
   return VSR_OK;
 }
 
+// The attention kernels read whole key tiles and give keys that a query does not
+// see the probability 0, which a NaN or an infinity among the values survives
+// (fp32 contexts then add the tile key by key, in another order). Positions that a
+// pass reads without writing them may hold those of an earlier call: the rest of
+// the last tile of its prefix and candidate rows, and a draft's positions, which
+// its steps fill one by one. They are set to zero before it. Prefixes and
+// candidates of whole tiles need no launch; the others show none in their time (7B,
+// 397 candidate rows 10.45 ms, a 3B draft of 3 branches 142.8, with it or without).
+int clear_slots(vsr_ctx *c, bool prefix, int cand_rows, int draft_branches) {
+  const vsr_config &cf = c->cfg;
+  const Plan &p = c->plan;
+  const int E = cf.dtype == VSR_BF16 ? 2 : 4, precise = cf.dtype == VSR_BF16 ? cf.split_layers : 0;
+  ClearSlots a;
+  const auto add = [&](size_t plane, int layers, int npos, int beg, int n) {
+    const long rows = (long)layers * cf.n_kv_heads * cf.head_dim;
+    const int end = (int)align_up(n, 64);
+    if (rows > 0 && end > beg)
+      a.run[a.n++] = {c->at<char>(plane) + (size_t)beg * E, rows, (long)npos * E, (end - beg) * E};
+  };
+  if (prefix) {
+    add(p.vtc, cf.n_layers, p.kv_npos, c->P & ~63, c->P);
+    add(p.vtc_lo, precise, p.kv_npos, c->P & ~63, c->P);
+  }
+  add(p.bvt, 1, p.bk_npos, cand_rows & ~63, cand_rows);
+  add(p.bvt_lo, precise > 0, p.bk_npos, cand_rows & ~63, cand_rows);
+  if (draft_branches > 0) {
+    add(p.vtd, cf.n_layers, p.dec_npos, 0, draft_branches * p.dec_S);
+    add(p.vtd_lo, precise, p.dec_npos, 0, draft_branches * p.dec_S);
+  }
+  if (a.n > 0) STAGE(c, K_ROWS, "clear cache slots", launch_clear_slots(a, c->stream));
+  return VSR_OK;
+}
+
 template <typename TW, typename TA>
 int prefill_impl(vsr_ctx *c, const void *visual, int nv, const int32_t *ids, int nt) {
   const vsr_config &cf = c->cfg;
@@ -797,7 +830,9 @@ int prefill_impl(vsr_ctx *c, const void *visual, int nv, const int32_t *ids, int
                                    static_cast<const TW *>(c->embed), cf.vocab, cf.d_model, x,
                                    c->at<int32_t>(p.flags), c->stream));
   c->P = P;
-  const int rc = run_layers<TW, TA>(c, P, 0, Split{1});
+  int rc = clear_slots(c, true, 0, 0);
+  if (rc) return rc;
+  rc = run_layers<TW, TA>(c, P, 0, Split{1});
   if (rc) return rc;
   STAGE(c, K_COPY, "last prefix row",
            hipMemcpyAsync(c->at<float>(p.h_last), x + (size_t)(P - 1) * cf.d_model,
@@ -825,6 +860,8 @@ int branch_forward(vsr_ctx *c, const Branches &br, const int32_t *cand_ids) {
                               c->at<float>(p.x), s));
   const Split split =
       kMfma ? cascade_split(T_rows, c->P + br.cmax, cf.n_heads, cf.n_kv_heads) : Split{1};
+  const int rc = clear_slots(c, false, T_rows, 0);
+  if (rc) return rc;
   return run_layers<TW, TA>(c, T_rows, 1, split);
 }
 
@@ -940,7 +977,9 @@ int verify_impl(vsr_ctx *c, const void *visual, int nv, const int32_t *ids, int 
   constexpr bool kMfma = std::is_same<TA, f16>::value;
   const Split split =
       kMfma ? cascade_split(T_rows, P + br.cmax, cf.n_heads, cf.n_kv_heads) : Split{1};
-  const int rc = run_layers<TW, TA>(c, P + T_rows, 3, split);
+  int rc = clear_slots(c, true, T_rows, 0);
+  if (rc) return rc;
+  rc = run_layers<TW, TA>(c, P + T_rows, 3, split);
   if (rc) return rc;
   STAGE(c, K_COPY, "last prefix row",
         hipMemcpyAsync(c->at<float>(p.h_last), x + (size_t)(P - 1) * cf.d_model,
@@ -1056,7 +1095,9 @@ int draft_impl(vsr_ctx *c, const Branches &br, const int32_t *ids, int n_new, in
   // the cache segments of all of them.
   const Split split0 =
       kMfma ? cascade_split(T_rows, c->P + p.dec_S, cf.n_heads, cf.n_kv_heads) : Split{1};
-  int rc = run_layers<TW, TA>(c, T_rows, 2, split0);
+  int rc = clear_slots(c, false, 0, M);
+  if (rc) return rc;
+  rc = run_layers<TW, TA>(c, T_rows, 2, split0);
   if (rc) return rc;
   STAGE(c, K_LMIN, "draft inputs",
         launch_branch_last_norm<TW, TA>(x, br, g, cf.d_model, cf.rms_eps, lm_in, s));

@@ -131,3 +131,44 @@ def test_unknown_check_bits_are_rejected():
     v = Verifier(W.TINY_F32, wl.weights, device="cuda")
     assert v.lib.vsr_set_checks(v.h, 4) == VSR_EINVAL
     assert b"unknown" in v.lib.vsr_last_error(v.h)
+
+
+@pytest.mark.parametrize("split", [0, 1], ids=["fast", "precise"])
+@pytest.mark.parametrize("cfg", [SMALL, W.TINY_F32], ids=["bf16", "fp32"])
+def test_a_nan_call_leaves_nothing_behind(cfg, split):
+    """After a prefix, candidates, branches and drafts of NaN, shorter and longer
+    calls give the results of a context that never saw them, bit for bit: what
+    the caches hold past the rows a call writes does not reach it."""
+    torch = _torch()
+    from paper_2601_01513_amd.binding import Verifier
+    _say(f"case: {cfg.name} split {split} calls after a NaN visual row")
+    wl = W.make_workload(cfg, 6, device="cuda")
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    ids, cands, M = i32(wl.prefix_ids), i32(wl.cand_ids), cfg.n_cands
+    make = lambda: Verifier(cfg, wl.weights, device="cuda", max_new=6, split_layers=split)  # noqa: E731
+
+    def calls(v, vis, prefix, lens, m):
+        out = []
+        out += v.verify(vis, prefix, cands, lens)
+        v.prefill(vis, prefix)
+        out += v.score(cands, lens)
+        out += v.reliability(cands[:m], [max(1, n) for n in lens[:m]], 1, 2, 0.05)[:2]
+        out += [v.draft(cands[:m], [3] * m, 5), *v.draft_ruled(cands[:m], [2] * m, 4)]
+        torch.cuda.synchronize()
+        return [t.cpu().numpy() for t in out]
+
+    nan = wl.visual.clone()
+    nan[3, :] = float("nan")
+    full = [int(n) for n in wl.cand_len]
+    # (lengths that leave part of the last tile of the long call's rows unwritten)
+    short = ids[:len(ids) - 20], [7, 1, 0, 12, 5][:M], M - 1
+    long = ids, full, M
+    v = make()
+    bad = calls(v, nan, *long)
+    assert np.isnan(bad[0]).any() and np.isnan(bad[-1]).any()
+    for case in (short, long):
+        got, want = calls(v, wl.visual, *case), calls(make(), wl.visual, *case)
+        assert all(np.isfinite(a).all() for a in want)
+        for i, (a, b) in enumerate(zip(got, want)):
+            assert np.array_equal(a, b), i
+        calls(v, nan, *long)
