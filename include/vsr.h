@@ -510,10 +510,12 @@ int vsr_weights_to_f16(const void *src, void *dst, size_t n, void *hip_stream);
  *                  checked or not, so the results are those of id 0;
  *   VSR_ENONFINITE (VSR_CHECK_FINITE) if a result is NaN or infinite: the
  *                  scores (vsr_score, vsr_verify), the Yes/No log-probs
- *                  (vsr_reliability) or the last prefix row's hidden state
- *                  (vsr_prefill). A NaN or infinite visual row, or an fp16
- *                  activation that overflows (|x| > 65504) on the bf16 path,
- *                  propagates to them.
+ *                  (vsr_reliability), the last prefix row's hidden state
+ *                  (vsr_prefill) or, only if it is NaN, a pick's log-probability
+ *                  (vsr_draft_ruled, also with logprobs NULL; -inf is that of a
+ *                  mask that allows nothing). vsr_draft has none. A NaN or
+ *                  infinite visual row, or an fp16 activation that overflows
+ *                  (|x| > 65504) on the bf16 path, propagates to them.
  * VSR_EID is reported before VSR_ENONFINITE. Either way the outputs are
  * written as in an unchecked call and the prefix state changes as it would
  * on success. checks: an OR of the bits below (0 turns checking off). */

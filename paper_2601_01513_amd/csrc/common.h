@@ -94,8 +94,9 @@ hipError_t launch_rope_table(float2 *cs, int npos, int hd, float base, hipStream
 constexpr int32_t kFlagBadId = 1;
 constexpr int32_t kFlagNonFinite = 2;
 hipError_t launch_flags_clear(int32_t *flags, hipStream_t s);
-// Sets kFlagNonFinite in *flags if any of x[0 .. n) is NaN or infinite.
-hipError_t launch_check_finite(const float *x, long n, int32_t *flags, hipStream_t s);
+// Sets kFlagNonFinite in *flags if any of x[0 .. n) is NaN, or infinite unless nan_only.
+hipError_t launch_check_finite(const float *x, long n, bool nan_only, int32_t *flags,
+                               hipStream_t s);
 
 // Row tables of one score call: for packed row t of candidate m at offset j,
 // row_lo[t] = cu[m] (first row of its candidate), row_pos[t] = P + j,

@@ -199,18 +199,20 @@ hipError_t launch_flags_clear(int32_t *flags, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Sets kFlagNonFinite if any of x[0 .. n) is NaN or infinite.
-__global__ __launch_bounds__(256) void k_check_finite(const float *x, long n, int32_t *flags) {
+// Sets kFlagNonFinite if any of x[0 .. n) is NaN, or infinite unless nan_only.
+__global__ __launch_bounds__(256) void k_check_finite(const float *x, long n, bool nan_only,
+                                                      int32_t *flags) {
   bool bad = false;
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256)
-    bad |= !isfinite(x[i]);
+    bad |= nan_only ? isnan(x[i]) : !isfinite(x[i]);
   if (__any(bad) && (threadIdx.x & 63) == 0) atomicOr(flags, kFlagNonFinite);
 }
 
-hipError_t launch_check_finite(const float *x, long n, int32_t *flags, hipStream_t s) {
+hipError_t launch_check_finite(const float *x, long n, bool nan_only, int32_t *flags,
+                               hipStream_t s) {
   if (n <= 0) return hipSuccess;
   const long blocks = std::min<long>((n + 255) / 256, 1024);
-  k_check_finite<<<(unsigned)blocks, 256, 0, s>>>(x, n, flags);
+  k_check_finite<<<(unsigned)blocks, 256, 0, s>>>(x, n, nan_only, flags);
   return hipGetLastError();
 }
 

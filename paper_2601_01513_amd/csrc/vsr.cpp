@@ -1124,18 +1124,18 @@ int draft_impl(vsr_ctx *c, const Branches &br, const int32_t *ids, int n_new, in
 // Checked calls (vsr_set_checks): the status word is cleared before the
 // call's launches and read once after them (the call then waits for its
 // stream). `vals` (n floats, device) are the call's results whose finiteness
-// is checked.
+// is checked (nan_only: among which infinities are results).
 int checks_begin(vsr_ctx *c) {
   if (!c->checks) return VSR_OK;
   HIPCHECK(c, "checks", launch_flags_clear(c->at<int32_t>(c->plan.flags), c->stream));
   return VSR_OK;
 }
 
-int checks_end(vsr_ctx *c, int rc, const float *vals, long n) {
+int checks_end(vsr_ctx *c, int rc, const float *vals, long n, bool nan_only = false) {
   if (rc != VSR_OK || !c->checks) return rc;
   int32_t *flags = c->at<int32_t>(c->plan.flags);
   if ((c->checks & VSR_CHECK_FINITE) && vals)
-    HIPCHECK(c, "checks", launch_check_finite(vals, n, flags, c->stream));
+    HIPCHECK(c, "checks", launch_check_finite(vals, n, nan_only, flags, c->stream));
   int32_t f = 0;
   HIPCHECK(c, "checks", hipMemcpyAsync(&f, flags, sizeof f, hipMemcpyDeviceToHost, c->stream));
   HIPCHECK(c, "checks", hipStreamSynchronize(c->stream));
@@ -1346,18 +1346,21 @@ int draft_call(vsr_ctx *ctx, const int32_t *prompt_ids, const int32_t *prompt_le
   rc = ctx->cfg.dtype == VSR_BF16
            ? draft_impl<bf16, f16>(ctx, br, prompt_ids, n_new, tokens, ruled)
            : draft_impl<float, float>(ctx, br, prompt_ids, n_new, tokens, ruled);
-  return checks_end(ctx, rc, nullptr, 0);
+  // (A step whose mask allows nothing has the log-probability -inf.)
+  return checks_end(ctx, rc, ruled ? ruled->pick.logprob : nullptr, (long)M * n_new, true);
 }
 
-// Parts of a ruled draft's workspace: logits, branch lengths, the pick's partials.
+// Parts of a ruled draft's workspace: logits, branch lengths, the pick's partials,
+// log-probabilities of a checked call that keeps none.
 struct RuledPlan {
-  size_t prompt_len, pick, total;
+  size_t prompt_len, pick, logprobs, total;
 };
 RuledPlan ruled_plan(const vsr_config &c, int M) {
   RuledPlan p;
   p.prompt_len = align_up((size_t)M * c.vocab * 4, 256);
   p.pick = p.prompt_len + align_up((size_t)M * 4, 256);
-  p.total = align_up(p.pick + pick_workspace_bytes(M, c.vocab), 256);
+  p.logprobs = align_up(p.pick + pick_workspace_bytes(M, c.vocab), 256);
+  p.total = align_up(p.logprobs + (size_t)M * c.max_new * 4, 256);
   return p;
 }
 
@@ -1434,6 +1437,8 @@ extern "C" int vsr_draft_ruled(vsr_ctx *ctx, const int32_t *prompt_ids,
     r.pick.prompt_len = r.prompt_len;
   }
   r.pick.logprob = logprobs;
+  if (!logprobs && (ctx->checks & VSR_CHECK_FINITE))
+    r.pick.logprob = reinterpret_cast<float *>(ws + p.logprobs);
   r.pick.token_stride = n_new;
   return draft_call(ctx, prompt_ids, prompt_len, M, Cmax, n_new, tokens, &r);
 }

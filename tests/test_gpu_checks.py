@@ -172,3 +172,49 @@ def test_a_nan_call_leaves_nothing_behind(cfg, split):
         for i, (a, b) in enumerate(zip(got, want)):
             assert np.array_equal(a, b), i
         calls(v, nan, *long)
+@pytest.mark.parametrize("kept", [True, False], ids=["logprobs", "tokens only"])
+@pytest.mark.parametrize("cfg", [SMALL, W.TINY_F32], ids=["bf16", "fp32"])
+def test_ruled_drafts(cfg, kept):
+    """A ruled draft under both checks: a mask that allows nothing in a step is no
+    error, a NaN prefix and an allowed infinite bias are VSR_ENONFINITE, a prompt id
+    outside the vocabulary is VSR_EID."""
+    torch = _torch()
+    from paper_2601_01513_amd.binding import VSR_EID, VSR_ENONFINITE, Verifier
+    _say(f"case: {cfg.name} ruled drafts, logprobs {kept}")
+    wl = W.make_workload(cfg, 4, device="cuda")
+    v = Verifier(cfg, wl.weights, device="cuda", max_new=3)
+    ids = torch.tensor(wl.prefix_ids, dtype=torch.int32, device="cuda")
+    prompts = torch.tensor(wl.cand_ids, dtype=torch.int32, device="cuda")
+    M, words = cfg.n_cands, (cfg.vocab + 31) // 32
+    mask = torch.full((3, M, words), -1, dtype=torch.int32, device="cuda")
+    mask[1, M - 1] = 0
+
+    def run(p=prompts, **kw):
+        out = (torch.empty((M, 3), dtype=torch.int32, device="cuda"),
+               torch.empty((M, 3), device="cuda") if kept else None)
+        return v.draft_ruled(p, [2] * M, 3, mask=mask, out=out, **kw)
+
+    v.prefill(wl.visual, ids)
+    want, want_lp = run()
+    v.set_checks(ids=True, finite=True)
+    got, got_lp = run()
+    assert torch.equal(got, want) and int(got[M - 1, 1]) == -1
+    if kept:
+        assert torch.equal(got_lp, want_lp) and float(got_lp[M - 1, 1]) == -np.inf
+    bias = torch.zeros((1, cfg.vocab), device="cuda")
+    bias[0, 5] = float("inf")
+    _expect(VSR_ENONFINITE, lambda: run(bias=bias))
+    bad = prompts.clone()
+    bad[1, 1] = cfg.vocab
+    _expect(VSR_EID, lambda: run(bad))
+    v.set_checks(ids=False, finite=False)
+    vis = wl.visual.clone()
+    vis[0, :] = float("nan")
+    v.prefill(vis, ids)
+    v.set_checks(ids=False, finite=True)
+    _expect(VSR_ENONFINITE, run)
+    v.set_checks(ids=False, finite=False)
+    assert bool((run()[0] == -1).all())  # unchecked, as a mask that allows nothing
+    v.prefill(wl.visual, ids)
+    v.set_checks(ids=True, finite=True)
+    assert torch.equal(run()[0], want)
