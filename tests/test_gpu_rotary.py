@@ -330,3 +330,29 @@ def test_inputs_dropped_behind_another_streams_work():
     others = [torch.ones(shape, dtype=dtype, device="cuda") for shape, dtype in shapes]
     torch.cuda.synchronize()
     assert all(map(torch.equal, *outs)) and len(others) == len(shapes)
+
+
+@pytest.mark.parametrize("base", [0.5, 0.01, 1e-4, 1e-30, 1.0, 2.0, 1e12])
+@pytest.mark.parametrize("sections", [(1,), (16, 16), (60, 65)], ids=str)
+def test_bases_below_one_and_far_above(base, sections):
+    """Below 1 the angles grow with the pair, past pos: off by at most 2^-49 of the
+    angle then (a relative error of the steps and of one product, all fp64), by
+    2^-49 of pos otherwise."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    T, hd, half = 60, 250, sum(sections)
+    base = float(np.float32(base))
+    g = torch.Generator(device="cuda").manual_seed(71)
+    x = torch.randn((T, 3, hd), generator=g, device="cuda")
+    pos = torch.randint(-200000, 200000, (len(sections), T), generator=g, device="cuda",
+                        dtype=torch.int32)
+    out, _ = B.rope_axes(B.rotary(sections, base), pos, x)
+    y, p, axis = _np(x), pos.cpu().numpy(), axis_of_pair(sections, False)
+    want = rope(y, p, axis, base)
+    per_pos = np.maximum(base ** (-np.arange(half) / half), 1.0)
+    far = np.abs(p.astype(np.float64)[axis].T * per_pos)[:, None] * 2.0 ** -49
+    h = np.hypot(y[..., :half], y[..., half:2 * half])
+    bound = np.tile((40 * 2.0 ** -24 + far) * h, 2) + EPS["f32"] * np.abs(want[..., :2 * half])
+    got = _np(out)
+    assert np.all(np.abs(got - want)[..., :2 * half] <= bound)
+    assert np.array_equal(got[..., 2 * half:], y[..., 2 * half:])
