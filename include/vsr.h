@@ -267,8 +267,9 @@ typedef struct vsr_heads {
 
 /* Rotates the query heads q_in into q_out and the key heads k_in into k_out.
  *   pos    : device int32, axis x's position of token t at pos[x pos_stride + t]
- *            (any int32; angles are exact to about 2^-50 of pos, with base < 1
- *            of the angle itself, which is then the larger);
+ *            (any int32; angles are exact to about 2^-50 of pos; with base < 1
+ *            they outgrow pos and are exact to about 2^-50 of themselves, times
+ *            |ln base| / 4 where that is more than 1);
  *   k_rows : device [T] int32 or NULL: token t's key goes to row k_rows[t] of
  *            k_out (NULL: t), and nowhere if that lies outside [0, k_cap) (e.g.
  *            -1 for padding). Rows inside it must differ: of two tokens of

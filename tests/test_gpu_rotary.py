@@ -335,9 +335,12 @@ def test_inputs_dropped_behind_another_streams_work():
 @pytest.mark.parametrize("base", [0.5, 0.01, 1e-4, 1e-30, 1.0, 2.0, 1e12])
 @pytest.mark.parametrize("sections", [(1,), (16, 16), (60, 65)], ids=str)
 def test_bases_below_one_and_far_above(base, sections):
-    """Below 1 the angles grow with the pair, past pos: off by at most 2^-49 of the
-    angle then (a relative error of the steps and of one product, all fp64), by
-    2^-49 of pos otherwise."""
+    """At 1 and above the angles are off by at most 2^-49 of pos, as elsewhere. Below 1
+    they grow with the pair, past pos, and so does their error: the exponent of a
+    step, at most |ln base| in natural units, is off by three roundings here and one
+    in the comparison, which are relative errors of the step, and 24 cover the
+    powers, their products and the one with pos: (4 |ln base| + 24) 2^-53 of the
+    angle."""
     torch = _torch()
     from paper_2601_01513_amd import binding as B
     T, hd, half = 60, 250, sum(sections)
@@ -350,7 +353,8 @@ def test_bases_below_one_and_far_above(base, sections):
     y, p, axis = _np(x), pos.cpu().numpy(), axis_of_pair(sections, False)
     want = rope(y, p, axis, base)
     per_pos = np.maximum(base ** (-np.arange(half) / half), 1.0)
-    far = np.abs(p.astype(np.float64)[axis].T * per_pos)[:, None] * 2.0 ** -49
+    rel = 2.0 ** -49 if base >= 1 else (4 * abs(np.log(base)) + 24) * 2.0 ** -53
+    far = np.abs(p.astype(np.float64)[axis].T * per_pos)[:, None] * rel
     h = np.hypot(y[..., :half], y[..., half:2 * half])
     bound = np.tile((40 * 2.0 ** -24 + far) * h, 2) + EPS["f32"] * np.abs(want[..., :2 * half])
     got = _np(out)
