@@ -61,12 +61,12 @@ CASES = [
     (1, 28, 4, 128, (16, 24, 24), False, "bf16"),
     (3, 16, 2, 128, (24, 20, 20), True, "f16"),
     (65, 5, 5, 64, (12, 10, 10), True, "bf16"),
-    (33, 3, 1, 80, (10, 10), False, "f16"),     # a partial rotation, narrow tail
-    (17, 4, 2, 36, (5, 4), True, "f32"),        # 9 pairs and a tail of 9: element by element
+    (33, 3, 1, 80, (10, 10), False, "f16"),     # a partial rotation
+    (17, 4, 2, 36, (5, 4), True, "f32"),        # 9 pairs and a tail of 9
     (9, 2, 2, 6, (1, 1, 1), False, "bf16"),
     (130, 8, 2, 256, (16, 16), False, "f32"),
     (21, 7, 1, 256, (56, 24, 24, 24), True, "f16"),
-    (40, 2, 1, 250, (60, 65), False, "f16"),    # 125 pairs: two chunks a lane
+    (40, 2, 1, 250, (60, 65), False, "f16"),    # 125 pairs
     (700, 14, 2, 128, (64,), False, "bf16"),
     (5000, 6, 2, 64, (10, 0, 22), False, "f16"),  # an axis without pairs, waves of many tokens
 ]
@@ -360,3 +360,56 @@ def test_bases_below_one_and_far_above(base, sections):
     got = _np(out)
     assert np.all(np.abs(got - want)[..., :2 * half] <= bound)
     assert np.array_equal(got[..., 2 * half:], y[..., 2 * half:])
+
+
+def _lanes(hd, rot, esize):
+    """Pairs a lane takes at a time, lanes a head, such chunks a lane: 16 bytes of
+    each half where both parts of the head have the pairs and a wave the lanes."""
+    rh, th = rot // 2, (hd - rot) // 2
+    n = lambda vec: -(-rh // vec) + -(-th // vec)  # noqa: E731
+    vec = 16 // esize
+    while vec > 1 and (rh < vec or 0 < th < vec or n(vec) > 64):
+        vec //= 2
+    lanes = 1
+    while lanes < min(n(vec), 64):
+        lanes *= 2
+    return vec, lanes, -(-n(vec) // lanes)
+
+
+@pytest.mark.parametrize("norm", [False, True], ids=["rope", "norm"])
+@pytest.mark.parametrize("hd,sections,dtype,layout", [
+    (256, (1,), "f16", (1, 64, 2)), (256, (1,), "f32", (1, 64, 2)),
+    (256, (60, 67), "bf16", (1, 64, 2)), (256, (3,), "f16", (1, 64, 2)),
+    (132, (1,), "bf16", (1, 64, 2)), (256, (1, 1), "f16", (2, 64, 1)),
+    (256, (64, 62), "f32", (2, 64, 1)), (256, (2, 3), "f32", (4, 64, 1)),
+    (128, (1,), "f16", (1, 64, 1)), (128, (30, 33), "f32", (1, 64, 1)),
+    (128, (1, 1), "bf16", (2, 32, 1)), (126, (1, 1), "f32", (2, 32, 1)),
+    (64, (1,), "f16", (1, 32, 1)), (62, (30,), "bf16", (1, 32, 1)), (18, (1,), "f32", (1, 16, 1)),
+    (6, (1,), "f16", (1, 4, 1)), (20, (4,), "bf16", (4, 4, 1)), (256, (128,), "f16", (8, 16, 1)),
+    (254, (127,), "f32", (4, 32, 1)), (8, (4,), "f32", (4, 1, 1)),
+], ids=str)
+def test_lane_layouts(hd, sections, dtype, layout, norm):
+    """Every way that a head's pairs fall on lanes: one, two, four or eight at a time,
+    one lane to a whole wave a head, one or two chunks a lane; in place too."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    assert _lanes(hd, 2 * sum(sections), 4 if dtype == "f32" else 2) == layout
+    T, hq, hk = 37, 5, 2
+    g = torch.Generator(device="cuda").manual_seed(hd + sum(sections))
+    n = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    qkv = (n(T, hq + 2 * hk, hd) * 3).to(_dt(dtype))
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:].clone()
+    pos = torch.randint(0, 40000, (len(sections), T), generator=g, device="cuda",
+                        dtype=torch.int32)
+    rot, gq, gk = B.rotary(sections, 1e4), None, None
+    if norm:
+        gq, gk = ((1 + 0.3 * n(hd)).to(_dt(dtype)) for _ in range(2))
+    call = lambda **kw: (B.qk_norm_rope(rot, pos, q, k, gq, gk, 1e-6, **kw) if norm  # noqa: E731
+                         else B.rope_axes(rot, pos, q, k, **kw))
+    qo, ko = call()
+    p = pos.cpu().numpy()
+    _check(qo, q, p, sections, False, 1e4, dtype, gq)
+    _check(ko, k, p, sections, False, 1e4, dtype, gk)
+    call(q_out=q, k_out=k)
+    torch.cuda.synchronize()
+    assert torch.equal(q, qo) and torch.equal(k, ko) and torch.equal(qkv[:, hq + hk:], v)
