@@ -427,3 +427,48 @@ def test_tensors_of_another_stream_dropped_at_once():
     got, _ = run(True)
     torch.cuda.synchronize()
     assert all(map(torch.equal, got, want))
+
+
+@pytest.mark.parametrize("cfg", DRAFTS[:3], ids=lambda c: c.name)
+def test_without_rules_as_vsr_draft_with_bf16_weights(cfg):
+    """The heads that keep their logits on weights that stay bf16."""
+    torch = _torch()
+    wl, v = _case(cfg, 5, True, max_new=6, gemm_weights="bf16")
+    _place(cfg, v, True)
+    v.prefill(wl.visual, _ids(wl.prefix_ids))
+    lens = 1 + np.arange(cfg.n_cands) % cfg.cand_len
+    want = v.draft(_ids(wl.cand_ids), lens, 6)
+    got, logprobs = v.draft_ruled(_ids(wl.cand_ids), lens, 6)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and bool((logprobs < 0).all())
+
+
+@pytest.mark.parametrize("split", [0, 1])
+def test_scoring_and_drafts_with_bf16_weights(split):
+    """Head norms behind the QKV products on bf16 weights: prefix and candidate rows
+    (tiles), few rows, decode steps."""
+    torch = _torch()
+    cfg = SMALL_BF16
+    wl, v = _case(cfg, 17, True, max_new=4, split_layers=split, gemm_weights="bf16")
+    pos, nxt, axis = _place(cfg, v, True)
+    cand, lens = _candidates(cfg, wl)
+    hw, vis = W.host_weights(wl.weights), W.to_host_f32(wl.visual)
+    v.prefill(wl.visual, _ids(wl.prefix_ids))
+    two = v.score(_ids(cand), lens)[0].clone()
+    few = v.score(_ids(cand[:1]), lens[3:4])[0].clone()
+    one = v.verify(wl.visual, _ids(wl.prefix_ids), _ids(cand), lens)[0]
+    tokens, logprobs = v.draft_ruled(_ids(cand), [3] * cfg.n_cands, 4)
+    torch.cuda.synchronize()
+    after = lambda ids: PD.logits_after(cfg, hw, vis, wl.prefix_ids, ids, pos, nxt, axis)  # noqa: E731
+    for m in range(cfg.n_cands):
+        ids = cand[m, :lens[m]]
+        want = _log_softmax(after(ids))[np.arange(len(ids)), ids]
+        for got in (two, one):
+            assert np.all(np.abs(got[m, :lens[m]].cpu().numpy() - want) <= 2e-2), m
+        new = tokens[m].cpu().numpy()
+        lp = _log_softmax(after(np.concatenate([cand[m, :3], new[:-1]]))[3:])
+        assert np.all(lp.max(-1) - lp[np.arange(4), new] <= 4e-2), m
+        assert np.all(np.abs(logprobs[m].cpu().numpy() - lp[np.arange(4), new]) <= 4e-2), m
+    ids = cand[0, :lens[3]]
+    want = _log_softmax(after(ids))[np.arange(len(ids)), ids]
+    assert np.all(np.abs(few[0, :lens[3]].cpu().numpy() - want) <= 2e-2)
