@@ -168,16 +168,29 @@ hipError_t launch_align_select(const float *ent, const float *frames, int M, int
                                const float *rel, float delta, int strategy, float *align,
                                int32_t *choice, hipStream_t s);
 
-// Outputs above this many bytes are gone from the caches (32 MB of L2) before
-// their reader comes.
+// VEC neighbours, at any element's address (the hardware's 16-byte loads and
+// stores take any).
+template <typename T, int VEC>
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
+  T v[VEC];
+};
+
+// Outputs above this many bytes are written past the caches. By itself the write is
+// faster that way from about 40 MB up (rotation of 5120 / 8192 / 16384 tokens of 28
+// + 4 heads, 40 / 64 / 128 MB: 14.1 / 21.4 / 47.4 us against 15.7 / 26.8 / 51.1;
+// kept picks of 64 / 128 / 256 rows of 152064, 37 / 74 / 148 MB: 16.1 / 26.7 / 59
+// against 16.3 / 34 / 63). A reader right after it finds the outputs in the last-level
+// cache up to 80 MB otherwise (with a copy of the queries 62.1 against 57.4 us at
+// 80 MB, 71.2 against 71.5 at 96, 96 against 106 at 128; with a maximum over the picks
+// 75 against 59 at 74 MB, 83 against 87 at 93). A prefill with head norms is the same
+// either way (4 layers, 12288 and 16384 rows: within 0.1%).
 constexpr long kCachedBytes = 64L << 20;
 
 // Rotary positions with several axes (kernels_rotary.hip): pair i < rot / 2
 // turns with the position of its axis, 2 bits of a map (16 pairs a word).
-constexpr int kMaxAxes = 4;
 constexpr int kAxisWords = 8;  // head_dim <= 256: up to 128 pairs
 struct RotaryAxes {
-  int rot, n_axes;
+  int rot;
   uint32_t map[kAxisWords];
 };
 // Heads [tokens][n][head_dim] in and out (may be one and the same), strides in

@@ -76,13 +76,6 @@ __device__ __forceinline__ Best block_best(Best b, Best *red) {
   return b;
 }
 
-// VEC neighbours, at any element's address (the hardware's 16-byte loads and
-// stores take any).
-template <typename T, int VEC>
-struct __attribute__((packed, aligned(sizeof(T)))) Pack {
-  T v[VEC];
-};
-
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
 // Rounded as written (no fused multiply-add): the same values as the same

@@ -37,13 +37,6 @@ namespace vsr {
 
 namespace {
 
-// VEC neighbours, at any element's address (the hardware's 16-byte loads and
-// stores take any).
-template <typename T, int VEC>
-struct __attribute__((packed, aligned(sizeof(T)))) Pack {
-  T v[VEC];
-};
-
 typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
 
 // Sum over groups of lph (a power of two) consecutive lanes, in every lane.

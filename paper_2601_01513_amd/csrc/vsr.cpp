@@ -403,7 +403,6 @@ const char *rotary_axes(const vsr_rotary *r, int head_dim, RotaryAxes *out) {
       if (r->sections[x] > 0 && x + r->n_axes * (r->sections[x] - 1) >= half)
         return "interleaved: an axis has more pairs than its turns";
   out->rot = 2 * half;
-  out->n_axes = r->n_axes;
   for (int i = 0, x = 0, end = r->sections[0]; i < half; ++i) {
     while (i >= end) end += r->sections[++x];
     const int turn = i % r->n_axes;
@@ -1009,12 +1008,7 @@ int reliability_impl(vsr_ctx *c, const Branches &br, const int32_t *ids, int yes
   return VSR_OK;
 }
 
-// Greedy drafts: the prompt rows of every branch through all layers (keys /
-// values kept in the draft cache), then n_new steps of one row per branch.
-// Each step's LM head picks the next token on the device and feeds it to the
-// next step's embedding, so the loop never waits for the host.
-// `ruled` not NULL: the head keeps its logits and the tokens are picked from them
-// under the rules.
+// What a draft under rules adds.
 struct RuledDraft {
   PickArgs pick;    // rules, prompt lists, the first step's outputs and mask
   long mask_step;   // words from one step's mask to the next
@@ -1023,6 +1017,12 @@ struct RuledDraft {
   void *ws;         // of the pick
 };
 
+// Greedy drafts: the prompt rows of every branch through all layers (keys /
+// values kept in the draft cache), then n_new steps of one row per branch.
+// Each step's LM head picks the next token on the device and feeds it to the
+// next step's embedding, so the loop never waits for the host.
+// `ruled` not NULL: the head keeps its logits and the tokens are picked from them
+// under the rules.
 template <typename TW, typename TA>
 int draft_impl(vsr_ctx *c, const Branches &br, const int32_t *ids, int n_new, int32_t *tokens,
                const RuledDraft *ruled) {
@@ -1314,7 +1314,7 @@ extern "C" int vsr_reliability(vsr_ctx *ctx, const int32_t *branch_ids,
 namespace {
 
 // vsr_draft and vsr_draft_ruled: `ruled` (NULL: greedy over the logits) is
-// complete but for its prompt lists and branch lengths.
+// complete but for the branch lengths that prompt_len points to.
 int draft_call(vsr_ctx *ctx, const int32_t *prompt_ids, const int32_t *prompt_len, int32_t M,
                int32_t Cmax, int32_t n_new, int32_t *tokens, RuledDraft *ruled) {
   if (!ctx->prefilled) return ctx->fail(VSR_ESTATE, "draft before a successful prefill");
