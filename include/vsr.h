@@ -317,7 +317,8 @@ int vsr_set_positions(vsr_ctx *ctx, const vsr_rotary *rot, const int32_t *pos,
  * rms_eps) in every layer of every later call: q_norm, k_norm are HOST arrays of
  * n_layers device pointers to [head_dim] gains in the context's dtype (borrowed,
  * like the weights; vsr_load_weights leaves them). Both NULL: no norms. The
- * current prefix is dropped. */
+ * current prefix is dropped. A bf16 context holds the heads in fp16 before they
+ * are normed: raw values past 65504 overflow, and their row's results are NaN. */
 int vsr_load_qk_norms(vsr_ctx *ctx, const void *const *q_norm, const void *const *k_norm);
 
 /* ---- tokens under rules -----------------------------------------------------

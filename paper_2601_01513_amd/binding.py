@@ -427,7 +427,8 @@ class Verifier:
         branch m; its prompt list is the branch's prompt, its output list the
         tokens it got so far). mask: int32 words [1 or M][ceil(vocab/32)], or
         [n_new][1 or M][...] with one mask a step. out: (tokens [M][n_new] int32,
-        logprobs [M][n_new] f32 or None). Returns (tokens, logprobs)."""
+        logprobs [M][n_new] f32 or None). Returns (tokens, logprobs). The inputs must
+        be ready on the context's stream and may be dropped after the call."""
         torch = _torch_names()
         M, cmax = int(prompt_ids.shape[0]), int(prompt_ids.shape[1])
         lens = (ctypes.c_int32 * M)(*[int(x) for x in prompt_len])
@@ -647,8 +648,9 @@ def rope_axes(rot, pos, q, k=None, q_out=None, k_out=None, k_rows=None, stream=N
     device int32 [n_axes][T]; q: [T][Hq][hd] and k: [T][Hk][hd], any token and head
     strides (slices of stacked QKV rows). q_out, k_out: new tensors, or given ones
     (q itself for in place; a key cache [Hk][positions][hd] as its transpose(0, 1),
-    with k_rows [T] int32 its positions, -1 to leave a key out). Returns (q_out,
-    k_out), valid once the stream is synchronised."""
+    with k_rows [T] int32 its positions, -1 to leave a key out). stream: where it
+    runs (None: the current one); the tensors must be ready there and may be dropped
+    after the call. Returns (q_out, k_out), valid once the stream is synchronised."""
     return _rotate(rot, pos, q, k, None, 0.0, q_out, k_out, k_rows, stream)
 
 
@@ -712,14 +714,15 @@ def pick_tokens(logits, prompt=None, prompt_len=None, output=None, output_len=No
                 processed=None, out=None, workspace=None, stream=None):
     """The greedy pick of each row of logits under rules (vsr_pick_tokens).
 
-    logits: device [rows][vocab], float32, bfloat16 or float16, rows at any stride;
+    logits: device [rows][vocab], float32, bfloat16 or float16, rows at any stride
+    from vocab up;
     prompt, output: int32 [rows][n] token lists, *_len int32 [rows] (all n if None);
     repetition, presence, frequency: float32 [rows]; bias: float32 [1 or rows][vocab];
     mask: int32 words [1 or rows][ceil(vocab / 32)], a set bit allows its token;
     processed: float32 [rows][vocab] to keep the logits after the rules (may be
-    logits). Returns (token [rows] int32, logprob [rows] f32), or `out`, whose
-    logprob may be None; valid once the stream is synchronised. token -1, logprob
-    -inf: no token was allowed."""
+    logits); stream as in rope_axes. Returns (token [rows] int32, logprob [rows] f32),
+    or `out`, whose logprob may be None; valid once the stream is synchronised. token
+    -1, logprob -inf: no token was allowed."""
     torch = _torch_names()
     lib = _lib
     dtype = _float_types.get(logits.dtype)

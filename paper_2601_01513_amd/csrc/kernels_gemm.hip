@@ -1431,7 +1431,9 @@ __global__ __launch_bounds__(256) void k_gemm_lmhead_4w(const f16 *__restrict__ 
 
 // LM head that keeps the logits (drafts under rules): the greedy variant's
 // products, stored as logits[token][vocab]. A lane holds 4 neighbouring
-// vocabulary entries of a token at a time.
+// vocabulary entries of a token at a time and stores them one by one, a wave's
+// lanes a row of logits apart: with the 3B drafter's head (622 MB of fp16) 64 rows
+// take 221 us, the greedy variant 224, but 128 rows 253 and 231, 256 rows 308 and 235.
 template <class TL, bool WCVT>
 __global__ __launch_bounds__(NT) void k_gemm_lmlogits(const f16 *__restrict__ Hn,
                                                       const uint16_t *__restrict__ Wlm, int T,

@@ -10,9 +10,10 @@
 //
 // The kernel reads and writes each head once and is bound by that traffic (the
 // counters show no byte more written): 16384 tokens of 40 + 8 bf16 heads, 403 MB, take 71 us
-// (5.6 TB/s; a bare copy of the same rows takes 71.5), 8192 with the norms 37 us, 4096
-// tokens of 28 + 4 heads (in the caches) 12 us. Few tokens are bound by one
-// round trip to memory and the launch: 3.5 us for a decode step's 3 or 8.
+// (5.7 TB/s; a bare copy of the same rows takes 71.5), 8192 with the norms 36 us, 4096
+// tokens of 28 + 4 heads (in the caches) 12 us, 8192 of them in fp32 47 us (5.7 TB/s).
+// Few tokens are bound by one round trip to memory and the launch: 3.1 us for a decode
+// step's 8, 3.7 for 3 with norms.
 //
 // A head is handed to lph consecutive lanes of a wave (8 for head_dim 128 in 16
 // bits): a lane holds VEC consecutive pairs, both halves, so that the rotation and
