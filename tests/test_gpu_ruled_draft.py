@@ -472,3 +472,66 @@ def test_scoring_and_drafts_with_bf16_weights(split):
     ids = cand[0, :lens[3]]
     want = _log_softmax(after(ids))[np.arange(len(ids)), ids]
     assert np.all(np.abs(few[0, :lens[3]].cpu().numpy() - want) <= 2e-2)
+
+
+def _decode64(cfg, w, visual, prefix_ids, branch, pos, next_pos, axis):
+    """Log-probabilities after the last prefix row and every branch token, as
+    plain_decoder.logits_after, in float64 on the GPU (rows by the thousand)."""
+    torch = _torch()
+    dev, hq, hk, hd, F = w["embed"].device, cfg.n_heads, cfg.n_kv_heads, cfg.head_dim, cfg.d_ff
+    norm = lambda x, g: x / (x.square().mean(-1, keepdim=True) + cfg.rms_eps).sqrt() * g  # noqa: E731
+    ids = lambda a: w["embed"][torch.tensor(np.asarray(a, dtype=np.int64), device=dev)].double()  # noqa: E731
+    x = torch.cat([visual.double(), ids(prefix_ids), ids(branch)])
+    n, half = len(x), len(axis)
+    own = np.tile(next_pos + np.arange(len(branch)), (pos.shape[0], 1))
+    p = np.concatenate([pos, own], 1).astype(np.float64)
+    ang = torch.tensor(p[axis].T * cfg.rope_base ** (-np.arange(half) / half), device=dev)[:, None]
+    turn = lambda y: torch.cat([y[..., :half] * ang.cos() - y[..., half:] * ang.sin(),  # noqa: E731
+                                y[..., half:] * ang.cos() + y[..., :half] * ang.sin()], -1)
+    hidden = torch.ones((n, n), dtype=torch.bool, device=dev).triu(1)
+    for lw in w["layers"]:
+        lw = {k: t.double() for k, t in lw.items()}
+        qkv = (norm(x, lw["attn_norm"]) @ lw["wqkv"].T).view(n, hq + 2 * hk, hd)
+        q, k = turn(norm(qkv[:, :hq], lw["q_norm"])), turn(norm(qkv[:, hq:hq + hk], lw["k_norm"]))
+        out = []
+        for h in range(hq):
+            kv = h * hk // hq
+            s = q[:, h].contiguous() @ k[:, kv].T.contiguous() / np.sqrt(hd)
+            out.append(s.masked_fill(hidden, -np.inf).softmax(-1) @ qkv[:, hq + hk + kv].contiguous())
+        x = x + torch.cat(out, -1) @ lw["wo"].T
+        gu = norm(x, lw["ffn_norm"]) @ lw["wgu"].T
+        x = x + (torch.nn.functional.silu(gu[:, :F]) * gu[:, F:]) @ lw["wdown"].T
+    x = norm(x[pos.shape[1] - 1:], w["final_norm"].double())
+    return (x @ w["lm_head"].double().T).log_softmax(-1)
+
+
+@pytest.mark.parametrize("weights", ["f16", "bf16"])
+@pytest.mark.parametrize("model,P", [(W.B1_5, 2048), (W.B7, 1029), (W.B32, 300)],
+                         ids=lambda x: getattr(x, "name", x))
+def test_one_layer_of_the_workloads_models(model, P, weights):
+    """Head norms and axes behind the QKV products of real widths: prefixes and
+    candidates by the thousand rows, few rows, decode steps."""
+    torch = _torch()
+    cfg = model.replace(name="one layer", n_layers=1, vocab=2048, n_prefix=P, n_visual=P // 2,
+                        n_cands=5, cand_len=64)
+    wl, v = _case(cfg, 19, True, max_new=5, split_layers=int(weights == "bf16"),
+                  gemm_weights=weights)
+    pos, nxt, axis = _place(cfg, v, True)
+    cand, lens = _ids(wl.cand_ids), [64, 20, 6, 41, 33]
+    ids = _ids(wl.prefix_ids)
+    v.prefill(wl.visual, ids)
+    got = [v.score(cand, lens)[0].clone()]
+    few = [v.score(cand[m:m + 1], lens[m:m + 1])[0].clone() for m in (1, 2)]
+    got.append(v.verify(wl.visual, ids, cand, lens)[0])
+    tokens, logprobs = v.draft_ruled(cand, [4] * 5, 5)
+    torch.cuda.synchronize()
+    after = lambda b: _decode64(cfg, wl.weights, wl.visual, wl.prefix_ids, b, pos, nxt, axis)  # noqa: E731
+    for m in range(5):
+        b = wl.cand_ids[m, :lens[m]]
+        want = after(b)[torch.arange(len(b)), torch.tensor(b).long()]
+        for lp in got + ([few[m - 1].expand(5, -1)] if m in (1, 2) else []):
+            assert float((lp[m, :lens[m]] - want).abs().max()) <= 2e-2, m
+        new = tokens[m].cpu().long()
+        lp = after(np.concatenate([wl.cand_ids[m, :4], new[:-1]]))[4:]
+        assert float((lp.max(-1).values - lp[torch.arange(5), new]).max()) <= 4e-2, m
+        assert float((logprobs[m] - lp[torch.arange(5), new]).abs().max()) <= 4e-2, m
