@@ -20,7 +20,8 @@
  *
  * Context-free calls on the same stages' tensors: vsr_rope_axes and
  * vsr_qk_norm_rope (positions with several axes, norms of query and key heads),
- * vsr_pick_tokens (a token per row of logits under rules), vsr_align_select,
+ * vsr_pick_tokens (a token per row of logits under rules), vsr_tree_rows and
+ * vsr_tree_attention (drafted trees over a paged cache), vsr_align_select,
  * vsr_keyframes, vsr_retrieve.
  *
  * Each candidate sees the prefix plus its own earlier tokens only (the drafts
@@ -406,6 +407,82 @@ int vsr_draft_ruled(vsr_ctx *ctx, const int32_t *prompt_ids, const int32_t *prom
                     int64_t mask_step, int32_t *tokens, float *logprobs, void *workspace,
                     size_t ws_bytes);
 
+/* ---- drafted trees over a paged key/value cache ------------------------------
+ *
+ * A cache of n_pages pages of page_size positions (a power of two): slot
+ * page * page_size + i of every layer's keys and values is position i of a page.
+ * Sequence s holds held[s] pages: position x of it lies in slot
+ *   table[s table_stride + x / page_size] * page_size + x % page_size;
+ * its first len[s] positions are in use, the rest is room. refs[p] is the number
+ * of sequences that hold page p (0: free); pages held by more than one are full.
+ * All arrays are int32 in device memory and read when the call runs: held outside
+ * [0, max_pages] and len outside its pages count as the nearest value inside,
+ * entries past held are not looked at.
+ * 1 <= n_seqs <= VSR_MAX_SEQS, n_pages >= 1, n_pages page_size < 2^31,
+ * max_pages (columns of table) >= 1, max_pages page_size <= 2^30. */
+#define VSR_MAX_SEQS 4096
+typedef struct vsr_pages {
+  int32_t n_seqs, n_pages, page_size, max_pages;
+  int32_t *table;
+  int64_t table_stride;
+  int32_t *len, *held, *refs;
+} vsr_pages;
+
+/* Rows of drafted trees: sequence s has rows start[s] .. start[s + 1] - 1 (start
+ * device [n_seqs + 1], rising, clamped to [0, T]; NULL: row s alone, T == n_seqs).
+ * Row j of a sequence sits at position len + j of its pages and is a child of its
+ * row parent[j] (device [T], indices within the sequence; -1, or any that is not
+ * below j: a root, a child of the context; parent NULL: of row j - 1).
+ *   shift : device [n_seqs] or NULL (0);
+ *   pos   : device [T] out, len + shift + the row's depth (0: a root), the
+ *           position for vsr_rope_axes;
+ *   slot  : device [T] out, the slot of position len + j (vsr_rope_axes' k_rows),
+ *           -1 where the sequence has no room there;
+ *   mask  : device, rows of mask_words words mask_stride apart, out, or NULL: bit j
+ *           of a row is set for the row itself and every row on its path
+ *           (vsr_tree_attention's mask; rows past 32 mask_words have no bit).
+ * Rows of no sequence get position 0, slot -1 and an empty mask. pages->refs may be
+ * NULL. 0 <= T <= 2^24. Outputs must not overlap inputs. Enqueued on hip_stream,
+ * whose device must be the current one; errors via vsr_last_error(NULL). */
+int vsr_tree_rows(const vsr_pages *pages, int32_t T, const int32_t *start,
+                  const int32_t *parent, const int32_t *shift, int32_t *pos, int32_t *slot,
+                  uint32_t *mask, int64_t mask_stride, int32_t mask_words, void *hip_stream);
+
+/* Bytes of device workspace vsr_tree_attention needs (0 for invalid sizes). */
+size_t vsr_tree_attention_workspace_size(int32_t dtype, int32_t head_dim, int32_t T,
+                                         int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads);
+
+/* Attention of drafted rows over their sequences' pages, the rows' own keys and
+ * values among them (at positions len + j, written before). Row j of a sequence
+ * sees position x < len, and position len + i where bit i of its mask row is set;
+ * with mask NULL where i <= j (a chain: a single token, a piece of a prompt). Query
+ * head h reads key head h / (n_heads / n_kv_heads):
+ *   out = sum_x softmax_x(scale q . k_x) v_x
+ * with fp32 sums; a row that sees nothing gets 0. Positions without room (past
+ * held page_size) are not seen; a table entry outside [0, n_pages) is read as page 0.
+ * What a row does not see does not reach it, NaN and infinity included.
+ *   q, out : [T][n_heads][head_dim]; k, v : [n_pages page_size slots][n_kv_heads]
+ *            [head_dim] of one layer, token_stride from slot to slot;
+ *            all of dtype (VSR_F32, VSR_BF16, VSR_F16; 16-bit ones round the
+ *            probabilities to it), element-aligned; 16-byte aligned keys and values
+ *            with strides and head_dim to match are read faster;
+ *   start  : as vsr_tree_rows; rows of no sequence are left as they are;
+ *   mask   : device rows of mask_words words, mask_stride words apart, or NULL;
+ *   lse    : device float [T][n_heads] out or NULL, log sum_x exp(scale q . k_x),
+ *            -inf for a row that sees nothing;
+ *   workspace : device, >= vsr_tree_attention_workspace_size bytes, 256-byte
+ *            aligned, caller-owned; calls that overlap in time need their own (two
+ *            captured graphs that share one must not replay at once).
+ * out must not overlap q, k, v or itself. n_heads % n_kv_heads == 0, n_heads <= 4096;
+ * 1 <= head_dim <= 256; 0 <= T <= 2^24; scale finite. pages->refs may be NULL.
+ * Enqueued on hip_stream, whose device must be the current one; errors via
+ * vsr_last_error(NULL). */
+int vsr_tree_attention(const vsr_pages *pages, int32_t dtype, int32_t head_dim, int32_t T,
+                       const int32_t *start, const vsr_heads *q, const vsr_heads *k,
+                       const vsr_heads *v, const uint32_t *mask, int64_t mask_stride,
+                       int32_t mask_words, float scale, const vsr_heads *out, float *lse,
+                       void *workspace, size_t ws_bytes, void *hip_stream);
+
 /* Stage 2 and the final choice (Section 3.2, Eq. 14-15; Algorithm 1; the
  * strategies compared in Table 3). No context: the inputs are CLIP
  * embeddings, not verifier state.
@@ -433,7 +510,7 @@ int vsr_align_select(const float *ent, const float *frames, int32_t M, int32_t N
  * ctx == NULL: message of the last failed context-free call on this thread
  * (vsr_create, vsr_align_select, vsr_weights_to_f16, vsr_keyframes,
  * vsr_retrieve, vsr_retrieve_static, vsr_rope_axes, vsr_qk_norm_rope,
- * vsr_pick_tokens). */
+ * vsr_pick_tokens, vsr_tree_rows, vsr_tree_attention). */
 const char *vsr_last_error(const vsr_ctx *ctx);
 
 /* Keyframes of a video (Section 3.1, Eq. 1). Each frame is compared with the

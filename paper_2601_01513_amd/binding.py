@@ -26,7 +26,8 @@ EXPORTS = ["vsr_workspace_size", "vsr_create", "vsr_load_weights", "vsr_prefill"
            "vsr_keyframes", "vsr_retrieve_workspace_size", "vsr_retrieve", "vsr_retrieve_static",
            "vsr_rope_axes", "vsr_qk_norm_rope", "vsr_set_positions", "vsr_load_qk_norms",
            "vsr_pick_workspace_size", "vsr_pick_tokens", "vsr_draft_ruled_workspace_size",
-           "vsr_draft_ruled", "vsr_last_error",
+           "vsr_draft_ruled", "vsr_tree_rows", "vsr_tree_attention_workspace_size",
+           "vsr_tree_attention", "vsr_last_error",
            "vsr_destroy", "vsr_set_checks", "vsr_profile_enable", "vsr_profile_read"]
 
 VSR_SELECT_TWO_STAGE, VSR_SELECT_ADDITION, VSR_SELECT_INVERT = 0, 1, 2
@@ -89,6 +90,13 @@ class VsrTokenLists(ctypes.Structure):
                 ("n_prompt", ctypes.c_int32), ("prompt_len", ctypes.c_void_p),
                 ("output", ctypes.c_void_p), ("output_stride", ctypes.c_int64),
                 ("n_output", ctypes.c_int32), ("output_len", ctypes.c_void_p)]
+
+
+class VsrPages(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("len", ctypes.c_void_p), ("held", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
 
 
 class VsrError(RuntimeError):
@@ -192,6 +200,15 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                                     ctypes.POINTER(VsrTokenRules), i64, ptr, ptr, ptr,
                                     ctypes.c_size_t]
     lib.vsr_draft_ruled.restype = ctypes.c_int
+    lib.vsr_tree_rows.argtypes = [ctypes.POINTER(VsrPages), i32, ptr, ptr, ptr, ptr, ptr, ptr,
+                                  i64, i32, ptr]
+    lib.vsr_tree_rows.restype = ctypes.c_int
+    lib.vsr_tree_attention_workspace_size.argtypes = [i32] * 6
+    lib.vsr_tree_attention_workspace_size.restype = ctypes.c_size_t
+    lib.vsr_tree_attention.argtypes = [ctypes.POINTER(VsrPages), i32, i32, i32, ptr, *heads[:3],
+                                       ptr, i64, i32, ctypes.c_float, heads[0], ptr, ptr,
+                                       ctypes.c_size_t, ptr]
+    lib.vsr_tree_attention.restype = ctypes.c_int
     lib.vsr_last_error.argtypes = [ctypes.c_void_p]
     lib.vsr_last_error.restype = ctypes.c_char_p
     lib.vsr_destroy.argtypes = [ctypes.c_void_p]
@@ -770,6 +787,136 @@ def pick_tokens(logits, prompt=None, prompt_len=None, output=None, output_len=No
           (logits, prompt, prompt_len, output, output_len, repetition, presence, frequency, bias,
            mask, processed, token, logprob, workspace))
     return token, logprob
+
+
+class Pages:
+    """A paged cache's tables (vsr_pages): the tensors and what they hold."""
+
+    def __init__(self, table, len, held, refs, page_size: int):
+        torch = _torch_names()
+        i32, dev = torch.int32, table.get_device()
+        if table.dtype is not i32 or table.dim() != 2 or \
+                (table.shape[1] > 1 and table.stride(1) != 1):
+            raise VsrError(VSR_EINVAL, "table: int32 [n_seqs][max_pages] rows expected")
+        seqs, most = table.shape
+        for t in (len, held):
+            if t.dtype is not i32 or t.shape != (seqs,) or t.stride(0) != 1 and seqs > 1 or \
+                    t.get_device() != dev:
+                raise VsrError(VSR_EINVAL, "len, held: contiguous int32 [n_seqs] on the table's "
+                                           "device expected")
+        if refs.dtype is not i32 or refs.dim() != 1 or not refs.is_contiguous() or \
+                refs.get_device() != dev:
+            raise VsrError(VSR_EINVAL, "refs: contiguous int32 [n_pages] on the table's device "
+                                       "expected")
+        self.table, self.len, self.held, self.refs = table, len, held, refs
+        self.n_seqs, self.max_pages, self.n_pages, self.page_size = seqs, most, refs.shape[0], \
+            int(page_size)
+        self.device_index = dev
+        self.c = VsrPages(seqs, self.n_pages, self.page_size, most, table.data_ptr(),
+                          table.stride(0) if seqs > 1 else most, len.data_ptr(), held.data_ptr(),
+                          refs.data_ptr())
+
+    def tensors(self):
+        return self.table, self.len, self.held, self.refs
+
+
+def pages(table, len, held, refs, page_size: int) -> Pages:
+    """The tables of a paged key/value cache (vsr_pages), device int32: table
+    [n_seqs][max_pages] (row s: the pages sequence s holds, in order), len [n_seqs]
+    positions in use, held [n_seqs] pages held, refs [n_pages] how many sequences hold
+    a page. page_size: positions a page, a power of two; slot page * page_size + i of
+    the cache is position i of a page."""
+    return Pages(table, len, held, refs, page_size)
+
+
+def _int_rows(t, n, dev, what):
+    """Pointer of a contiguous int32 [n] tensor, or None."""
+    if t is None:
+        return None
+    if t.dtype is _torch_names().int32 and t.numel() == n and t.is_contiguous() and \
+            t.get_device() == dev:
+        return t.data_ptr()
+    raise VsrError(VSR_EINVAL, f"{what}: contiguous int32 [{n}] on the pages' device expected")
+
+
+def _mask_rows(mask, T, dev):
+    """(pointer, row stride, words) of int32 [T][words] rows."""
+    if mask is None:
+        return None, 0, 0
+    if mask.dim() == 2 and mask.dtype is _torch_names().int32 and mask.get_device() == dev:
+        n, words = mask.shape
+        stride, step = mask.stride()
+        if n == T and (step == 1 or words == 1):
+            return mask.data_ptr(), stride if n > 1 else words, words
+    raise VsrError(VSR_EINVAL, f"mask: int32 [{T}][words] rows on the pages' device expected")
+
+
+def tree_rows(pages, start, parent=None, shift=None, words: Optional[int] = None, out=None,
+              stream=None):
+    """Positions, cache slots and ancestor masks of drafted rows (vsr_tree_rows).
+
+    start: int32 [n_seqs + 1], sequence s has rows start[s] .. start[s + 1] - 1, or None
+    (a row a sequence); parent: int32 [T], each row's parent within its sequence, -1 a
+    root (None: each row's is the one before it); shift: int32 [n_seqs] added to the
+    positions. out: (pos [T], slot [T], mask [T][words] or None), int32; new ones have
+    `words` words of mask (None: no mask; T comes from parent or is n_seqs).
+    Returns (pos, slot, mask)."""
+    torch = _torch_names()
+    dev = pages.device_index
+    if out is None:
+        T = pages.n_seqs if start is None else None if parent is None else parent.numel()
+        if T is None:
+            raise VsrError(VSR_EINVAL, "tree_rows: parent or out expected with start")
+        new = lambda *s: _empty(torch, s, torch.int32, pages.table.device, stream)  # noqa: E731
+        out = new(T), new(T), new(T, words) if words else None
+    pos, slot, mask = out
+    T = pos.numel()
+    args = (ctypes.byref(pages.c), T, _int_rows(start, pages.n_seqs + 1, dev, "start"),
+            _int_rows(parent, T, dev, "parent"), _int_rows(shift, pages.n_seqs, dev, "shift"),
+            _int_rows(pos, T, dev, "pos"), _int_rows(slot, T, dev, "slot"),
+            *_mask_rows(mask, T, dev))
+    _call(torch, dev, stream, _lib.vsr_tree_rows, args,
+          (*pages.tensors(), start, parent, shift, *out))
+    return pos, slot, mask
+
+
+def tree_attention(pages, q, k, v, scale: float, start=None, mask=None, out=None, lse=None,
+                   workspace=None, stream=None):
+    """Attention of drafted rows over their sequences' pages (vsr_tree_attention).
+
+    q: [T][n_heads][head_dim]; k, v: one layer's slots [n_pages * page_size]
+    [n_kv_heads][head_dim], any slot and head strides; start: as in tree_rows; mask:
+    int32 [T][words], bit i of a row lets it see row i of its sequence's draft (None:
+    every row sees those before it and itself); out: like q (None: new; rows of no
+    sequence are left as they are); lse: float32 [T][n_heads] to fill, or None. Returns
+    out."""
+    torch = _torch_names()
+    dtype, dev = q.dtype, pages.device_index
+    vsr_dtype = _float_types.get(dtype)
+    if vsr_dtype is None or q.dim() != 3 or k.dim() != 3:
+        raise VsrError(VSR_EINVAL, "q, k, v: [rows][n_heads][head_dim] float tensors expected")
+    T, nq, hd = q.shape
+    slots = pages.n_pages * pages.page_size
+    if out is None:
+        out = _empty(torch, (T, nq, hd), dtype, q.device, stream)
+    qh, oh = _heads(q, dtype, hd, dev, T), _heads(out, dtype, hd, dev, T)
+    kh, vh = _heads(k, dtype, hd, dev, slots), _heads(v, dtype, hd, dev, slots)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (T, nq) or
+                            not lse.is_contiguous() or lse.get_device() != dev):
+        raise VsrError(VSR_EINVAL, "lse: contiguous float32 [rows][n_heads] expected")
+    if workspace is None:
+        size = _lib.vsr_tree_attention_workspace_size(vsr_dtype, hd, T, pages.n_seqs, nq,
+                                                      k.shape[1])
+        workspace = _empty(torch, max(size, 256), torch.uint8, q.device, stream)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise VsrError(VSR_EINVAL, "workspace: contiguous tensor on the pages' device expected")
+    _call(torch, dev, stream, _lib.vsr_tree_attention,
+          (ctypes.byref(pages.c), vsr_dtype, hd, T,
+           _int_rows(start, pages.n_seqs + 1, dev, "start"), ctypes.byref(qh), ctypes.byref(kh),
+           ctypes.byref(vh), *_mask_rows(mask, T, dev), scale, ctypes.byref(oh), _ptr(lse) or None,
+           workspace.data_ptr(), workspace.numel() * workspace.element_size()),
+          (*pages.tensors(), q, k, v, start, mask, out, lse, workspace))
+    return out
 
 
 def align_select(ent, frames, rel, delta: float, strategy: str = "two_stage", out=None,

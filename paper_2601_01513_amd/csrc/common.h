@@ -268,6 +268,47 @@ hipError_t launch_pick(PickArgs a, int dtype, void *ws, hipStream_t s);
 // len[m] = length of branch m.
 hipError_t launch_branch_lengths(const Branches &br, int32_t *len, hipStream_t s);
 
+// A paged cache's tables (vsr_pages), in device memory, page_size 2^page_shift.
+struct PageTables {
+  int n_seqs, n_pages, page_shift, max_pages;
+  int32_t *table;
+  long table_stride;
+  int32_t *len, *held, *refs;
+};
+// Positions, slots and ancestor masks of drafted rows (kernels_tree.hip): the fields of
+// vsr_tree_rows.
+struct TreeRowsArgs {
+  PageTables pages;
+  int T;
+  const int32_t *start, *parent, *shift;
+  int32_t *pos, *slot;
+  uint32_t *mask;
+  long mask_stride;
+  int mask_words;
+};
+hipError_t launch_tree_rows(const TreeRowsArgs &a, hipStream_t s);
+// Attention of drafted rows over their sequences' pages (kernels_tree.hip): the fields of
+// vsr_tree_attention, strides in elements.
+struct TreeAttnArgs {
+  PageTables pages;
+  int T, hd, n_heads, n_kv;
+  const int32_t *start;
+  const void *q, *k, *v;
+  void *out;
+  float *lse;
+  long q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs;
+  const uint32_t *mask;
+  long mask_stride;
+  int mask_words;
+  float scale_log2;  // scale * log2(e)
+  // Set by the launcher: partial results, blocks of the grid.
+  float *part;
+  float2 *part_ml;
+  int groups;
+};
+size_t tree_attention_workspace_bytes(int dtype, int hd, int T, int n_seqs, int n_heads, int n_kv);
+hipError_t launch_tree_attention(TreeAttnArgs a, int dtype, void *ws, hipStream_t s);
+
 // Retrieval stage (Eq. 1-3): histograms + keyframes, then per-keyframe top-k
 // and the merged top-K (kernels_retrieval.hip).
 hipError_t launch_keyframes(const uint8_t *frames, int NF, int H, int W, float theta,

@@ -10,6 +10,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <string>
 #include <type_traits>
 #include <vector>
@@ -1832,6 +1833,179 @@ extern "C" int vsr_pick_tokens(const void *logits, int32_t dtype, int32_t rows, 
   a.token_stride = 1;
   const hipError_t e = launch_pick(a, dtype, workspace, static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return refuse(VSR_EHIP, "pick_tokens", hipGetErrorString(e));
+  return VSR_OK;
+}
+
+namespace {
+
+bool float_type(int d) { return d == VSR_F32 || d == VSR_BF16 || d == VSR_F16; }
+
+bool aligned4(std::initializer_list<const void *> ps) {
+  uintptr_t any = 0;
+  for (const void *p : ps) any |= reinterpret_cast<uintptr_t>(p);
+  return !(any & 3);
+}
+
+// A paged cache's tables as a call gives them: its message if they are wrong, else NULL.
+const char *pages_error(const vsr_pages *p, bool refs) {
+  if (!p) return "pages must be non-NULL";
+  if (p->n_seqs < 1 || p->n_seqs > VSR_MAX_SEQS) return "n_seqs must lie in [1, 4096]";
+  if (p->page_size < 1 || (p->page_size & (p->page_size - 1)))
+    return "page_size must be a power of two";
+  if (p->n_pages < 1 || (int64_t)p->n_pages * p->page_size > INT32_MAX)
+    return "n_pages must be >= 1, and n_pages * page_size below 2^31";
+  if (p->max_pages < 1 || (int64_t)p->max_pages * p->page_size > 1 << 30)
+    return "max_pages must be >= 1, and max_pages * page_size at most 2^30";
+  if (p->table_stride < p->max_pages || p->table_stride > 1LL << 40)
+    return "table_stride must be at least max_pages";
+  if (!p->table || !p->len || !p->held || (refs && !p->refs))
+    return "the pages' arrays must be non-NULL";
+  if (!aligned4({p->table, p->len, p->held, p->refs})) return "the pages' arrays must be 4-byte aligned";
+  return nullptr;
+}
+
+PageTables page_tables(const vsr_pages *p) {
+  return {p->n_seqs,        p->n_pages, __builtin_ctz(p->page_size), p->max_pages, p->table,
+          (long)p->table_stride, p->len,    p->held,                     p->refs};
+}
+
+// [a, a + an) and [b, b + bn) in bytes.
+bool ranges_meet(const void *a, size_t an, const void *b, size_t bn) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && an && bn && x < y + bn && y < x + an;
+}
+
+const char *mask_error(const uint32_t *mask, int64_t stride, int32_t words) {
+  if (!mask) return nullptr;
+  if (reinterpret_cast<uintptr_t>(mask) & 3) return "mask must be 4-byte aligned";
+  if (words < 1 || words > 1 << 19) return "mask_words must lie in [1, 2^19]";
+  if (stride < words || stride > 1LL << 40) return "mask_stride must be at least mask_words";
+  return nullptr;
+}
+
+constexpr int kMaxTreeRows = 1 << 24;
+
+size_t mask_bytes(int32_t T, int64_t stride, int32_t words) {
+  return ((size_t)(T - 1) * stride + words) * 4;
+}
+
+}  // namespace
+
+extern "C" int vsr_tree_rows(const vsr_pages *pages, int32_t T, const int32_t *start,
+                             const int32_t *parent, const int32_t *shift, int32_t *pos,
+                             int32_t *slot, uint32_t *mask, int64_t mask_stride,
+                             int32_t mask_words, void *hip_stream) {
+  g_create_error.clear();
+  const auto check = [&]() -> const char * {
+    if (const char *m = pages_error(pages, false)) return m;
+    if (T < 0 || T > kMaxTreeRows) return "T must lie in [0, 2^24]";
+    if (!start && T != pages->n_seqs) return "T must be n_seqs without start";
+    if (!aligned4({start, parent, shift})) return "start, parent and shift must be 4-byte aligned";
+    if (T == 0) return nullptr;
+    if (!pos || !slot || !aligned4({pos, slot})) return "pos and slot must be non-NULL and 4-byte aligned";
+    if (const char *m = mask_error(mask, mask_stride, mask_words)) return m;
+    struct Range {
+      const void *p;
+      size_t n;
+    };
+    const size_t n = pages->n_seqs, rows = (size_t)T * 4;
+    const Range in[] = {{pages->table, ((n - 1) * pages->table_stride + pages->max_pages) * 4},
+                        {pages->len, n * 4}, {pages->held, n * 4}, {start, n * 4 + 4},
+                        {parent, rows}, {shift, n * 4}};
+    const Range out[] = {{pos, rows}, {slot, rows}, {mask, mask ? mask_bytes(T, mask_stride, mask_words) : 0}};
+    for (const Range &o : out)
+      for (const Range &i : in)
+        if (ranges_meet(o.p, o.n, i.p, i.n)) return "an output overlaps an input";
+    for (int i = 0; i < 3; ++i)
+      if (ranges_meet(out[i].p, out[i].n, out[(i + 1) % 3].p, out[(i + 1) % 3].n))
+        return "outputs overlap each other";
+    return nullptr;
+  };
+  if (const char *msg = check()) return refuse(VSR_EINVAL, "tree_rows", msg);
+  if (T == 0) return VSR_OK;
+  const TreeRowsArgs a{page_tables(pages), T,    start, parent,      shift,
+                       pos,                slot, mask,  mask_stride, mask ? mask_words : 0};
+  const hipError_t e = launch_tree_rows(a, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return refuse(VSR_EHIP, "tree_rows", hipGetErrorString(e));
+  return VSR_OK;
+}
+
+extern "C" size_t vsr_tree_attention_workspace_size(int32_t dtype, int32_t head_dim, int32_t T,
+                                                    int32_t n_seqs, int32_t n_heads,
+                                                    int32_t n_kv_heads) {
+  if (!float_type(dtype) || head_dim < 1 || head_dim > 256 || T < 0 || T > kMaxTreeRows ||
+      n_seqs < 1 || n_seqs > VSR_MAX_SEQS || n_kv_heads < 1 || n_heads < 1 || n_heads > 4096 ||
+      n_heads % n_kv_heads)
+    return 0;
+  return align_up(tree_attention_workspace_bytes(dtype, head_dim, T, n_seqs, n_heads, n_kv_heads),
+                  256);
+}
+
+extern "C" int vsr_tree_attention(const vsr_pages *pages, int32_t dtype, int32_t head_dim,
+                                  int32_t T, const int32_t *start, const vsr_heads *q,
+                                  const vsr_heads *k, const vsr_heads *v, const uint32_t *mask,
+                                  int64_t mask_stride, int32_t mask_words, float scale,
+                                  const vsr_heads *out, float *lse, void *workspace,
+                                  size_t ws_bytes, void *hip_stream) {
+  g_create_error.clear();
+  const size_t esize = dtype == VSR_F32 ? 4 : 2;
+  const auto check = [&]() -> const char * {
+    if (const char *m = pages_error(pages, false)) return m;
+    if (!float_type(dtype)) return "dtype must be VSR_F32, VSR_BF16 or VSR_F16";
+    if (head_dim < 1 || head_dim > 256) return "head_dim must lie in [1, 256]";
+    if (T < 0 || T > kMaxTreeRows) return "T must lie in [0, 2^24]";
+    if (!start && T != pages->n_seqs) return "T must be n_seqs without start";
+    if (!std::isfinite(scale)) return "scale must be finite";
+    if (!q || !k || !v || !out) return "q, k, v and out must be non-NULL";
+    if (T == 0) return nullptr;
+    if (!aligned4({start, lse})) return "start and lse must be 4-byte aligned";
+    const long slots = (long)pages->n_pages * pages->page_size;
+    if (const char *m = heads_error(q, esize, false, head_dim, T)) return m;
+    if (const char *m = heads_error(out, esize, true, head_dim, T)) return m;
+    if (const char *m = heads_error(k, esize, false, head_dim, slots)) return m;
+    if (const char *m = heads_error(v, esize, false, head_dim, slots)) return m;
+    if (q->n_heads != out->n_heads) return "q and out differ in n_heads";
+    if (k->n_heads != v->n_heads || q->n_heads % k->n_heads)
+      return "k and v need one n_heads that divides q's";
+    if (heads_clash(out, T, q, T, head_dim, esize)) return "out overlaps q";
+    if (heads_clash(out, T, k, slots, head_dim, esize)) return "out overlaps k";
+    if (heads_clash(out, T, v, slots, head_dim, esize)) return "out overlaps v";
+    if (const char *m = mask_error(mask, mask_stride, mask_words)) return m;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))
+      return "workspace must be non-NULL and 256-byte aligned";
+    if (ws_bytes < vsr_tree_attention_workspace_size(dtype, head_dim, T, pages->n_seqs, q->n_heads,
+                                                     k->n_heads))
+      return "workspace smaller than vsr_tree_attention_workspace_size";
+    return nullptr;
+  };
+  if (const char *msg = check()) return refuse(VSR_EINVAL, "tree_attention", msg);
+  if (T == 0) return VSR_OK;
+  TreeAttnArgs a{};
+  a.pages = page_tables(pages);
+  a.T = T;
+  a.hd = head_dim;
+  a.n_heads = q->n_heads;
+  a.n_kv = k->n_heads;
+  a.start = start;
+  a.q = q->data;
+  a.k = k->data;
+  a.v = v->data;
+  a.out = out->data;
+  a.lse = lse;
+  a.q_ts = q->token_stride;
+  a.q_hs = q->head_stride;
+  a.k_ts = k->token_stride;
+  a.k_hs = k->head_stride;
+  a.v_ts = v->token_stride;
+  a.v_hs = v->head_stride;
+  a.o_ts = out->token_stride;
+  a.o_hs = out->head_stride;
+  a.mask = mask;
+  a.mask_stride = mask_stride;
+  a.mask_words = mask_words;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  const hipError_t e = launch_tree_attention(a, dtype, workspace, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return refuse(VSR_EHIP, "tree_attention", hipGetErrorString(e));
   return VSR_OK;
 }
 
