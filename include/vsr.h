@@ -21,8 +21,8 @@
  * Context-free calls on the same stages' tensors: vsr_rope_axes and
  * vsr_qk_norm_rope (positions with several axes, norms of query and key heads),
  * vsr_pick_tokens (a token per row of logits under rules), vsr_tree_rows and
- * vsr_tree_attention (drafted trees over a paged cache), vsr_align_select,
- * vsr_keyframes, vsr_retrieve.
+ * vsr_tree_attention (drafted trees over a paged cache), vsr_pages_update and
+ * vsr_pages_keep (that cache's pages), vsr_align_select, vsr_keyframes, vsr_retrieve.
  *
  * Each candidate sees the prefix plus its own earlier tokens only (the drafts
  * are scored independently, Eq. 6); candidate token j sits at position P + j.
@@ -483,6 +483,62 @@ int vsr_tree_attention(const vsr_pages *pages, int32_t dtype, int32_t head_dim, 
                        int32_t mask_words, float scale, const vsr_heads *out, float *lse,
                        void *workspace, size_t ws_bytes, void *hip_stream);
 
+/* Keys and values of a paged cache in every layer: k and v each
+ * [n_layers][n_pages page_size slots][n_heads][head_dim] of dtype, head_dim
+ * consecutive, strides in elements and the same for both. */
+typedef struct vsr_cache {
+  void *k, *v;
+  int32_t dtype, n_layers, n_heads, head_dim;
+  int64_t layer_stride, slot_stride, head_stride;
+} vsr_cache;
+
+/* Bytes of device workspace vsr_pages_update needs (0 for invalid sizes). */
+size_t vsr_pages_update_workspace_size(int32_t n_seqs);
+
+/* Sequences forked, dropped and given room, in two steps.
+ * 1. Every sequence d becomes what sequence source[d] was before the call: its len
+ *    positions, without room. -1: it becomes empty; any other value outside
+ *    [0, n_seqs), or source NULL: it stays, with its room. The full pages are
+ *    shared. Of a partly filled last page one sequence goes on with the page itself:
+ *    the source if it stays, else the lowest-numbered of those that become it; the
+ *    others get a page of their own and the rows are copied, in every layer. Pages
+ *    that nobody holds any more are free.
+ * 2. Every sequence gets pages for room[d] positions past its len (device [n_seqs],
+ *    below 0 or NULL: 0), beyond those it holds.
+ * New pages are the free ones (refs 0) of lowest number, handed out in the order of
+ * sequences, to each first that of its copy, then those of its room. A sequence whose
+ * pages and those of the sequences before it are more than there are gets none (a
+ * copy then ends at its last full page), and none of its room if that is
+ * more than max_pages pages.
+ *   source, room : device [n_seqs] or NULL;
+ *   ok     : device [n_seqs] out or NULL: 1 where a sequence got all of it, else 0;
+ *   cache  : HOST struct; may be NULL with source NULL;
+ *   workspace : device, >= vsr_pages_update_workspace_size(n_seqs) bytes, 16-byte
+ *            aligned, caller-owned (used with source alone, else it may be NULL).
+ * Table entries past held are left as they are. A table entry outside [0, n_pages)
+ * is neither counted nor copied. Arrays must not overlap. Enqueued on hip_stream,
+ * whose device must be the current one; errors via vsr_last_error(NULL). */
+int vsr_pages_update(const vsr_pages *pages, const int32_t *source, const int32_t *room,
+                     const vsr_cache *cache, int32_t *ok, void *workspace, size_t ws_bytes,
+                     void *hip_stream);
+
+/* The kept rows of every sequence's draft moved together, in every layer: the row at
+ * position len + kept[i] goes to position len + i, for i < n_kept; then the length
+ * is len + n_kept.
+ *   kept   : device [n_seqs][max_kept], rows kept_stride apart: rising, each within
+ *            the sequence's pages; a sequence's list ends before the first entry that
+ *            does not rise or lies outside them;
+ *   n_kept : device [n_seqs], clamped to [0, max_kept], or NULL (max_kept each);
+ *   len_out : device [n_seqs] out, the new lengths; pages->len, or an array of its own
+ *            (pages->len then stays);
+ *   release : nonzero: pages past the new length are given back (refs, held).
+ * 0 <= max_kept <= 2^20. Arrays must not overlap, but for len_out as above.
+ * pages->refs may be NULL without release. Enqueued on hip_stream, whose device must
+ * be the current one; errors via vsr_last_error(NULL). */
+int vsr_pages_keep(const vsr_pages *pages, const int32_t *kept, int64_t kept_stride,
+                   int32_t max_kept, const int32_t *n_kept, const vsr_cache *cache,
+                   int32_t *len_out, int32_t release, void *hip_stream);
+
 /* Stage 2 and the final choice (Section 3.2, Eq. 14-15; Algorithm 1; the
  * strategies compared in Table 3). No context: the inputs are CLIP
  * embeddings, not verifier state.
@@ -510,7 +566,8 @@ int vsr_align_select(const float *ent, const float *frames, int32_t M, int32_t N
  * ctx == NULL: message of the last failed context-free call on this thread
  * (vsr_create, vsr_align_select, vsr_weights_to_f16, vsr_keyframes,
  * vsr_retrieve, vsr_retrieve_static, vsr_rope_axes, vsr_qk_norm_rope,
- * vsr_pick_tokens, vsr_tree_rows, vsr_tree_attention). */
+ * vsr_pick_tokens, vsr_tree_rows, vsr_tree_attention,
+ * vsr_pages_update, vsr_pages_keep). */
 const char *vsr_last_error(const vsr_ctx *ctx);
 
 /* Keyframes of a video (Section 3.1, Eq. 1). Each frame is compared with the

@@ -27,7 +27,8 @@ EXPORTS = ["vsr_workspace_size", "vsr_create", "vsr_load_weights", "vsr_prefill"
            "vsr_rope_axes", "vsr_qk_norm_rope", "vsr_set_positions", "vsr_load_qk_norms",
            "vsr_pick_workspace_size", "vsr_pick_tokens", "vsr_draft_ruled_workspace_size",
            "vsr_draft_ruled", "vsr_tree_rows", "vsr_tree_attention_workspace_size",
-           "vsr_tree_attention", "vsr_last_error",
+           "vsr_tree_attention", "vsr_pages_update_workspace_size", "vsr_pages_update",
+           "vsr_pages_keep", "vsr_last_error",
            "vsr_destroy", "vsr_set_checks", "vsr_profile_enable", "vsr_profile_read"]
 
 VSR_SELECT_TWO_STAGE, VSR_SELECT_ADDITION, VSR_SELECT_INVERT = 0, 1, 2
@@ -97,6 +98,13 @@ class VsrPages(ctypes.Structure):
                 ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
                 ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
                 ("len", ctypes.c_void_p), ("held", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
+class VsrCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("n_layers", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("layer_stride", ctypes.c_int64),
+                ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class VsrError(RuntimeError):
@@ -209,6 +217,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                                        ptr, i64, i32, ctypes.c_float, heads[0], ptr, ptr,
                                        ctypes.c_size_t, ptr]
     lib.vsr_tree_attention.restype = ctypes.c_int
+    lib.vsr_pages_update_workspace_size.argtypes = [i32]
+    lib.vsr_pages_update_workspace_size.restype = ctypes.c_size_t
+    lib.vsr_pages_update.argtypes = [ctypes.POINTER(VsrPages), ptr, ptr, ctypes.POINTER(VsrCache),
+                                     ptr, ptr, ctypes.c_size_t, ptr]
+    lib.vsr_pages_update.restype = ctypes.c_int
+    lib.vsr_pages_keep.argtypes = [ctypes.POINTER(VsrPages), ptr, i64, i32, ptr,
+                                   ctypes.POINTER(VsrCache), ptr, i32, ptr]
+    lib.vsr_pages_keep.restype = ctypes.c_int
     lib.vsr_last_error.argtypes = [ctypes.c_void_p]
     lib.vsr_last_error.restype = ctypes.c_char_p
     lib.vsr_destroy.argtypes = [ctypes.c_void_p]
@@ -917,6 +933,76 @@ def tree_attention(pages, q, k, v, scale: float, start=None, mask=None, out=None
            workspace.data_ptr(), workspace.numel() * workspace.element_size()),
           (*pages.tensors(), q, k, v, start, mask, out, lse, workspace))
     return out
+
+
+def _cache(pages, k, v):
+    """vsr_cache of k and v, [n_layers][slots][n_kv_heads][head_dim]."""
+    dtype = _float_types.get(k.dtype)
+    if dtype is not None and v.dtype is k.dtype and k.dim() == 4 and v.shape == k.shape and \
+            v.stride() == k.stride() and k.get_device() == v.get_device() == pages.device_index:
+        L, slots, heads, hd = k.shape
+        ls, ss, hs, ds = k.stride()
+        if (ds == 1 or hd == 1) and slots == pages.n_pages * pages.page_size:
+            return VsrCache(k.data_ptr(), v.data_ptr(), dtype, L, heads, hd, ls, ss, hs)
+    raise VsrError(VSR_EINVAL, "k, v: [n_layers][n_pages * page_size][n_kv_heads][head_dim] "
+                               "tensors of one float dtype and the same strides, head_dim "
+                               "contiguous, on the pages' device expected")
+
+
+def pages_update(pages, source=None, room=None, k=None, v=None, ok=None, workspace=None,
+                 stream=None):
+    """Sequences forked, dropped and given room (vsr_pages_update): sequence d becomes
+    what source[d] was (-1: empty; None: all stay) and then has pages for room[d]
+    positions more. source, room: int32 [n_seqs]; k, v: the cache in every layer,
+    [n_layers][n_pages * page_size][n_kv_heads][head_dim] (needed with source: partly
+    filled pages are copied). Returns ok, int32 [n_seqs]: 1 where a sequence got all of
+    it."""
+    torch = _torch_names()
+    dev, n = pages.device_index, pages.n_seqs
+    if ok is None:
+        ok = _empty(torch, n, torch.int32, pages.table.device, stream)
+    cache, size = None, 0
+    if source is not None:
+        if k is None or v is None:
+            raise VsrError(VSR_EINVAL, "pages_update: source needs k and v")
+        cache = ctypes.byref(_cache(pages, k, v))
+        if workspace is None:
+            size = _lib.vsr_pages_update_workspace_size(n)
+            workspace = _empty(torch, size, torch.uint8, pages.table.device, stream)
+    if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise VsrError(VSR_EINVAL, "workspace: contiguous tensor on the pages' device expected")
+        size = workspace.numel() * workspace.element_size()
+    _call(torch, dev, stream, _lib.vsr_pages_update,
+          (ctypes.byref(pages.c), _int_rows(source, n, dev, "source"),
+           _int_rows(room, n, dev, "room"), cache, _int_rows(ok, n, dev, "ok"),
+           _ptr(workspace) or None, size),
+          (*pages.tensors(), source, room, k, v, ok, workspace))
+    return ok
+
+
+def pages_keep(pages, kept, n_kept, k, v, len_out=None, release: bool = True, stream=None):
+    """The kept rows of every sequence's draft moved together in every layer
+    (vsr_pages_keep): the row at position len + kept[s][i] goes to len + i for i <
+    n_kept[s], and the length becomes len + n_kept. kept: int32 [n_seqs][max_kept],
+    rising; n_kept: int32 [n_seqs], or None (max_kept); k, v as in pages_update; len_out:
+    where the new lengths go (None: pages.len); release: give back the pages past them.
+    Returns the new lengths."""
+    torch = _torch_names()
+    dev, n = pages.device_index, pages.n_seqs
+    if len_out is None:
+        len_out = pages.len
+    if kept.dim() != 2 or kept.dtype is not torch.int32 or kept.shape[0] != n or \
+            (kept.shape[1] > 1 and kept.stride(1) != 1) or kept.get_device() != dev:
+        raise VsrError(VSR_EINVAL, f"kept: int32 [{n}][max_kept] rows on the pages' device expected")
+    most = kept.shape[1]
+    cache = _cache(pages, k, v)
+    _call(torch, dev, stream, _lib.vsr_pages_keep,
+          (ctypes.byref(pages.c), kept.data_ptr() if most else None,
+           kept.stride(0) if n > 1 and most else most, most, _int_rows(n_kept, n, dev, "n_kept"),
+           ctypes.byref(cache), _int_rows(len_out, n, dev, "len_out"), bool(release)),
+          (*pages.tensors(), kept, n_kept, k, v, len_out))
+    return len_out
 
 
 def align_select(ent, frames, rel, delta: float, strategy: str = "two_stage", out=None,

@@ -309,6 +309,50 @@ struct TreeAttnArgs {
 size_t tree_attention_workspace_bytes(int dtype, int hd, int T, int n_seqs, int n_heads, int n_kv);
 hipError_t launch_tree_attention(TreeAttnArgs a, int dtype, void *ws, hipStream_t s);
 
+// A paged cache's keys and values in every layer (vsr_cache), strides in bytes.
+struct CacheRows {
+  char *k, *v;
+  int n_layers, n_heads;
+  long row;  // bytes of a position's row of one head
+  long layer_stride, slot_stride, head_stride;
+};
+// Sequences become copies of others, then get room (kernels_pages.hip): the fields of
+// vsr_pages_update. source NULL: everyone stays.
+struct PagesUpdateArgs {
+  PageTables pages;
+  const int32_t *source, *room;
+  int32_t *ok;
+  CacheRows cache;
+};
+size_t pages_update_workspace_bytes(int n_seqs);
+hipError_t launch_pages_update(const PagesUpdateArgs &a, void *ws, hipStream_t s);
+// Kept rows of drafts moved together (kernels_pages.hip): the fields of vsr_pages_keep.
+struct PagesKeepArgs {
+  PageTables pages;
+  const int32_t *kept;
+  long kept_stride;
+  const int32_t *n_kept;
+  int most;
+  int32_t *len_out;
+  int release;
+  CacheRows cache;
+};
+hipError_t launch_pages_keep(const PagesKeepArgs &a, hipStream_t s);
+
+// Log-probabilities of given tokens (kernels_logprobs.hip): the fields of
+// vsr_token_logprobs.
+struct LogprobArgs {
+  const void *logits;
+  long stride;
+  int rows, vocab, top;
+  const int32_t *tokens;
+  float *logprob, *entropy;
+  int32_t *rank, *top_id;
+  float *top_logprob;
+};
+size_t logprobs_workspace_bytes(int dtype, int rows, int vocab, int top);
+hipError_t launch_logprobs(const LogprobArgs &a, int dtype, void *ws, hipStream_t s);
+
 // Retrieval stage (Eq. 1-3): histograms + keyframes, then per-keyframe top-k
 // and the merged top-K (kernels_retrieval.hip).
 hipError_t launch_keyframes(const uint8_t *frames, int NF, int H, int W, float theta,

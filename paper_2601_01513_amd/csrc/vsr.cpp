@@ -2009,6 +2009,122 @@ extern "C" int vsr_tree_attention(const vsr_pages *pages, int32_t dtype, int32_t
   return VSR_OK;
 }
 
+namespace {
+
+struct IntArray {
+  const void *p;
+  size_t n;
+};
+
+// Whether arrays of a call that changes pages meet each other or the pages' own.
+const char *overlapping(const vsr_pages *p, std::initializer_list<IntArray> given) {
+  const size_t n = p->n_seqs;
+  IntArray all[8] = {{p->table, (n - 1) * p->table_stride + p->max_pages},
+                     {p->len, n}, {p->held, n}, {p->refs, (size_t)p->n_pages}};
+  size_t count = 4;
+  for (const IntArray &g : given) all[count++] = g;
+  for (size_t i = 0; i < count; ++i)
+    for (size_t j = 0; j < i; ++j)
+      if (ranges_meet(all[i].p, all[i].n * 4, all[j].p, all[j].n * 4)) return "arrays overlap";
+  return nullptr;
+}
+
+// A cache as a call gives it: its message if it is wrong, else NULL.
+const char *cache_error(const vsr_cache *c, long slots) {
+  if (!c) return "cache must be non-NULL";
+  if (!float_type(c->dtype)) return "dtype must be VSR_F32, VSR_BF16 or VSR_F16";
+  if (c->head_dim < 1 || c->head_dim > 256) return "head_dim must lie in [1, 256]";
+  if (c->n_layers < 1 || c->n_layers > 4096) return "n_layers must lie in [1, 4096]";
+  const size_t esize = c->dtype == VSR_F32 ? 4 : 2;
+  const vsr_heads k{c->k, c->n_heads, c->slot_stride, c->head_stride},
+      v{c->v, c->n_heads, c->slot_stride, c->head_stride};
+  if (const char *m = heads_error(&k, esize, true, c->head_dim, slots)) return m;
+  if (const char *m = heads_error(&v, esize, true, c->head_dim, slots)) return m;
+  const int64_t layer = (slots - 1) * c->slot_stride + (c->n_heads - 1) * c->head_stride + c->head_dim;
+  if (c->n_layers > 1 && c->layer_stride < layer) return "layer_stride must be at least a layer";
+  if ((double)c->layer_stride * c->n_layers > 0x1p46 || c->layer_stride < 0)
+    return "heads span more than 2^46 elements";
+  // Keys and values may lie side by side, in columns of the same slots or layer by layer:
+  // values against the layers of keys around them.
+  const int64_t step = c->n_layers > 1 ? c->layer_stride * (int64_t)esize : 0;
+  const int64_t gap = static_cast<char *>(c->v) - static_cast<char *>(c->k);
+  for (int64_t i = step ? gap / step - 1 : 0, end = step ? i + 2 : 0; i <= end; ++i) {
+    if (std::abs(i) >= c->n_layers) continue;
+    const vsr_heads near{static_cast<char *>(c->k) + i * step, c->n_heads, c->slot_stride,
+                         c->head_stride};
+    if (heads_clash(&near, slots, &v, slots, c->head_dim, esize)) return "k overlaps v";
+  }
+  return nullptr;
+}
+
+CacheRows cache_rows(const vsr_cache *c) {
+  const long esize = c->dtype == VSR_F32 ? 4 : 2;
+  return {static_cast<char *>(c->k),
+          static_cast<char *>(c->v),
+          c->n_layers,
+          c->n_heads,
+          c->head_dim * esize,
+          c->n_layers > 1 ? (long)c->layer_stride * esize : 0,
+          (long)c->slot_stride * esize,
+          c->n_heads > 1 ? (long)c->head_stride * esize : 0};
+}
+
+}  // namespace
+
+extern "C" size_t vsr_pages_update_workspace_size(int32_t n_seqs) {
+  return n_seqs < 1 || n_seqs > VSR_MAX_SEQS ? 0 : pages_update_workspace_bytes(n_seqs);
+}
+
+extern "C" int vsr_pages_update(const vsr_pages *pages, const int32_t *source,
+                                const int32_t *room, const vsr_cache *cache, int32_t *ok,
+                                void *workspace, size_t ws_bytes, void *hip_stream) {
+  g_create_error.clear();
+  const auto check = [&]() -> const char * {
+    if (const char *m = pages_error(pages, true)) return m;
+    const size_t n = pages->n_seqs;
+    if (!aligned4({source, room, ok})) return "source, room and ok must be 4-byte aligned";
+    if (const char *m = overlapping(pages, {{source, n}, {room, n}, {ok, n}})) return m;
+    if (!source) return nullptr;
+    if (const char *m = cache_error(cache, (long)pages->n_pages * pages->page_size)) return m;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))
+      return "workspace must be non-NULL and 16-byte aligned";
+    if (ws_bytes < pages_update_workspace_bytes(pages->n_seqs))
+      return "workspace smaller than vsr_pages_update_workspace_size";
+    return nullptr;
+  };
+  if (const char *msg = check()) return refuse(VSR_EINVAL, "pages_update", msg);
+  PagesUpdateArgs a{page_tables(pages), source, room, ok, CacheRows{}};
+  if (source) a.cache = cache_rows(cache);
+  const hipError_t e = launch_pages_update(a, workspace, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return refuse(VSR_EHIP, "pages_update", hipGetErrorString(e));
+  return VSR_OK;
+}
+
+extern "C" int vsr_pages_keep(const vsr_pages *pages, const int32_t *kept, int64_t kept_stride,
+                              int32_t max_kept, const int32_t *n_kept, const vsr_cache *cache,
+                              int32_t *len_out, int32_t release, void *hip_stream) {
+  g_create_error.clear();
+  const auto check = [&]() -> const char * {
+    if (const char *m = pages_error(pages, release != 0)) return m;
+    if (max_kept < 0 || max_kept > 1 << 20) return "max_kept must lie in [0, 2^20]";
+    if (max_kept > 0 && !kept) return "kept must be non-NULL";
+    if (kept_stride < max_kept || kept_stride > 1LL << 40)
+      return "kept_stride must be at least max_kept";
+    if (!len_out) return "len_out must be non-NULL";
+    if (!aligned4({kept, n_kept, len_out})) return "kept, n_kept and len_out must be 4-byte aligned";
+    const size_t n = pages->n_seqs, list = max_kept ? (n - 1) * kept_stride + max_kept : 0;
+    const int32_t *own_len = len_out == pages->len ? nullptr : len_out;
+    if (const char *m = overlapping(pages, {{kept, list}, {n_kept, n}, {own_len, n}})) return m;
+    return cache_error(cache, (long)pages->n_pages * pages->page_size);
+  };
+  if (const char *msg = check()) return refuse(VSR_EINVAL, "pages_keep", msg);
+  const PagesKeepArgs a{page_tables(pages), kept,    (long)kept_stride, n_kept, max_kept,
+                        len_out,            release, cache_rows(cache)};
+  const hipError_t e = launch_pages_keep(a, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return refuse(VSR_EHIP, "pages_keep", hipGetErrorString(e));
+  return VSR_OK;
+}
+
 extern "C" int vsr_set_checks(vsr_ctx *ctx, int checks) {
   if (!ctx) return VSR_EINVAL;
   if (checks & ~(VSR_CHECK_IDS | VSR_CHECK_FINITE))

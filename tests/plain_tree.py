@@ -74,3 +74,80 @@ def attention(q, k, v, table, length, held, page, start, mask, scale):
                     mass[b + j, h] = p @ np.abs(vv)
                     size[b + j, h] = abs(scale) * (np.abs(kk) @ np.abs(qq)).max()
     return out, lse, mass, size
+
+
+def pages_update(table, length, held, refs, page, source, room, k, v):
+    """vsr_pages_update in place, one sequence after the other; returns ok. k, v:
+    [layers][slots][...]."""
+    n, most = table.shape
+    was = [list(table[s, :held[s]]) for s in range(n)]
+    lens = [int(x) for x in length]
+    src = [d if source is None else int(source[d]) for d in range(n)]
+    src = [d if not -1 <= s < n else s for d, s in enumerate(src)]
+    heir = {s: s if src[s] == s else min([d for d in range(n) if src[d] == s], default=None)
+            for s in range(n)}
+    mine, copy = [], []
+    for d, s in enumerate(src):
+        if s == d:
+            mine.append(was[d])
+            copy.append(None)
+            continue
+        for p in was[d]:
+            refs[p] -= 1
+        if s < 0:
+            mine.append([])
+            copy.append(None)
+            length[d] = 0
+            continue
+        full, part = divmod(lens[s], page)
+        pages = was[s][:full + (part > 0)]
+        table[d, :len(pages)] = pages
+        length[d] = lens[s]
+        copy.append(pages.pop() if part and heir[s] != d else None)
+        for p in pages:
+            refs[p] += 1
+        mine.append(pages)
+    free = [p for p in range(len(refs)) if refs[p] == 0]
+    ok, before = np.zeros(n, np.int32), 0
+    for d in range(n):
+        have = len(mine[d]) + (copy[d] is not None)
+        want = -(-(int(length[d]) + (0 if room is None else max(0, int(room[d])))) // page)
+        need = (copy[d] is not None) + (max(0, want - have) if want <= most else 0)
+        before += need
+        served = need == 0 or before <= len(free)
+        ok[d] = served and want <= most
+        held[d] = len(mine[d]) + (need if served else 0)
+        if served:
+            new = free[before - need:before]
+            at = len(mine[d])
+            table[d, at:at + need] = new
+            for p in new:
+                refs[p] = 1
+            if copy[d] is not None:
+                r = np.arange(int(length[d]) % page)
+                for x in (k, v):
+                    x[:, new[0] * page + r] = x[:, copy[d] * page + r]
+        elif copy[d] is not None:
+            length[d] = int(length[d]) // page * page
+    return ok
+
+
+def pages_keep(table, length, held, refs, page, kept, n_kept, k, v, release):
+    """vsr_pages_keep in place; returns the new lengths."""
+    new = length.copy()
+    for s in range(len(length)):
+        n = kept.shape[1] if n_kept is None else min(max(int(n_kept[s]), 0), kept.shape[1])
+        room, last, i = int(held[s]) * page - int(length[s]), -1, 0
+        while i < n and last < kept[s, i] < room:
+            last = int(kept[s, i])
+            x, y = int(length[s]) + last, int(length[s]) + i
+            x, y = (int(table[s, p // page]) * page + p % page for p in (x, y))
+            k[:, y], v[:, y] = k[:, x].copy(), v[:, x].copy()
+            i += 1
+        new[s] += i
+        if release:
+            left = -(-int(new[s]) // page)
+            for c in range(left, int(held[s])):
+                refs[table[s, c]] -= 1
+            held[s] = left
+    return new

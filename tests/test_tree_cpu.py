@@ -102,6 +102,73 @@ def test_tree_attention_refuses(kw, word):
     _message("tree_attention", _attend(**kw), word)
 
 
+def _cache(**kw):
+    a = dict(k=16 * MB, v=32 * MB, dtype=B.VSR_F16, n_layers=2, n_heads=2, head_dim=64,
+             layer_stride=1600 * 128, slot_stride=128, head_stride=64)
+    a.update({x: v for x, v in kw.items() if x in a})
+    return B.VsrCache(**a)
+
+
+BAD_CACHES = [
+    (dict(cache=None), "cache"), (dict(dtype=7), "dtype"), (dict(head_dim=0), "head_dim"),
+    (dict(head_dim=300), "head_dim"), (dict(n_layers=0), "n_layers"), (dict(n_layers=4097), "n_layers"),
+    (dict(k=None), "non-NULL"), (dict(v=32 * MB + 1), "aligned"), (dict(n_heads=0), "n_heads"),
+    (dict(slot_stride=127), "themselves"), (dict(head_stride=63), "themselves"),
+    (dict(slot_stride=-128), "strides"), (dict(layer_stride=1600 * 128 - 1), "layer_stride"),
+    (dict(layer_stride=1 << 60), "2^46"), (dict(v=16 * MB), "k overlaps v"),
+    (dict(v=16 * MB + 4096), "k overlaps v"),
+    (dict(v=16 * MB + 2 * 1600 * 128), "k overlaps v"),            # the second layer's keys
+    (dict(k=32 * MB + 2 * 1600 * 128 + 512), "k overlaps v"),
+]
+
+
+def _update(pages="own", cache="own", **kw):
+    lib = _lib()
+    a = dict(source=2 * MB, room=2 * MB + 64, ok=2 * MB + 128, ws=3 * MB,
+             wsb=lib.vsr_pages_update_workspace_size(4))
+    a.update({k: v for k, v in kw.items() if k in a})
+    p, c = _pages(**kw) if pages == "own" else pages, _cache(**kw) if cache == "own" else cache
+    ref = lambda s: ctypes.byref(s) if s is not None else None  # noqa: E731
+    return lib.vsr_pages_update(ref(p), a["source"], a["room"], ref(c), a["ok"], a["ws"], a["wsb"],
+                                None)
+
+
+@pytest.mark.parametrize("kw,word", BAD_PAGES + BAD_CACHES + [
+    (dict(pages=None), "pages"), (dict(refs=None), "non-NULL"), (dict(source=2 * MB + 1), "aligned"),
+    (dict(ok=2 * MB + 130), "aligned"), (dict(room=2 * MB), "overlap"), (dict(ok=MB + 4096), "overlap"),
+    (dict(source=MB + 8), "overlap"), (dict(room=MB + 8192 + 396), "overlap"), (dict(len=MB + 156), "overlap"),
+    (dict(ws=None), "workspace"), (dict(ws=3 * MB + 8), "workspace"), (dict(wsb=79), "smaller"),
+])
+def test_pages_update_refuses(kw, word):
+    _message("pages_update", _update(**kw), word)
+
+
+def _keep(pages="own", cache="own", **kw):
+    a = dict(kept=2 * MB, stride=5, most=5, n_kept=2 * MB + 512, out=2 * MB + 1024, release=1)
+    a.update({k: v for k, v in kw.items() if k in a})
+    p, c = _pages(**kw) if pages == "own" else pages, _cache(**kw) if cache == "own" else cache
+    ref = lambda s: ctypes.byref(s) if s is not None else None  # noqa: E731
+    return _lib().vsr_pages_keep(ref(p), a["kept"], a["stride"], a["most"], a["n_kept"], ref(c),
+                                 a["out"], a["release"], None)
+
+
+@pytest.mark.parametrize("kw,word", BAD_PAGES + BAD_CACHES + [
+    (dict(pages=None), "pages"), (dict(refs=None), "non-NULL"), (dict(most=-1), "max_kept"),
+    (dict(most=(1 << 20) + 1, stride=1 << 21), "max_kept"), (dict(kept=None), "kept"),
+    (dict(stride=4), "kept_stride"), (dict(out=None), "len_out"), (dict(kept=2 * MB + 2), "aligned"),
+    (dict(n_kept=2 * MB + 76), "overlap"), (dict(out=2 * MB + 516), "overlap"),
+    (dict(out=MB + 4100), "overlap"), (dict(kept=MB + 100), "overlap"),
+])
+def test_pages_keep_refuses(kw, word):
+    _message("pages_keep", _keep(**kw), word)
+
+
+def test_page_workspaces():
+    lib = _lib()
+    assert [lib.vsr_pages_update_workspace_size(n) for n in (0, -1, 4097)] == [0] * 3
+    assert 16 < lib.vsr_pages_update_workspace_size(4096) < 1 << 18
+
+
 def test_nothing_to_do_and_sizes():
     lib = _lib()
     assert _rows(T=0, pos=None, slot=None) == B.VSR_OK
@@ -125,7 +192,7 @@ def test_the_binding_refuses_what_the_library_cannot_see():
     i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
     p = B.pages(**t, page_size=8)
     q, k = torch.zeros(4, 2, 8), torch.zeros(160, 1, 8)
-    start = i32(4)
+    start, kv = i32(4), torch.zeros(2, 160, 1, 8)
     att = lambda **kw: lambda: B.tree_attention(p, **dict(dict(q=q, k=k, v=k, scale=1.0, start=start), **kw))  # noqa: E731
     bad = [lambda kw=kw: B.pages(**dict(dict(t, page_size=8), **kw)) for kw in (
         dict(table=i32(3, 5).long()), dict(table=i32(5)), dict(table=i32(5, 3).t()), dict(len=i32(2)),
@@ -136,6 +203,18 @@ def test_the_binding_refuses_what_the_library_cannot_see():
             lambda: B.tree_rows(p, start, i32(4), out=(i32(4), i32(4), i32(3, 1))),
             lambda: B.tree_rows(p, start, i32(4)),               # host tensors
             att(), att(q=q.double()), att(q=q[0]), att(k=k.half()), att(k=k[:159]), att(v=k[:, :, :4]),
+            lambda: B.pages_update(p, i32(3)), lambda: B.pages_update(p, i32(2), k=kv, v=kv),
+            lambda: B.pages_update(p, room=i32(3).long()), lambda: B.pages_update(p, room=i32(3)),
+            lambda: B.pages_update(p, i32(3), k=kv, v=kv[:, :, :, ::2]),
+            lambda: B.pages_update(p, i32(3), k=kv[0], v=kv[0]),
+            lambda: B.pages_update(p, i32(3), k=kv[:, :99], v=kv[:, :99]),
+            lambda: B.pages_update(p, i32(3), k=kv, v=kv, ok=i32(4)),
+            lambda: B.pages_keep(p, i32(2, 4), None, kv, kv), lambda: B.pages_keep(p, i32(3), None, kv, kv),
+            lambda: B.pages_keep(p, i32(4, 3).t(), None, kv, kv),
+            lambda: B.pages_keep(p, i32(3, 4), i32(4), kv, kv),
+            lambda: B.pages_keep(p, i32(3, 4), None, kv, kv.half()),
+            lambda: B.pages_keep(p, i32(3, 4), None, kv, kv, i32(2)),
+            lambda: B.pages_keep(p, i32(3, 4), None, kv, kv),      # host tensors
             att(start=i32(5)), att(start=start.long()), att(mask=i32(3, 1)), att(mask=i32(4, 1).long()),
             att(mask=i32(2, 4).t()), att(out=q[:3]), att(out=q.half()), att(lse=torch.zeros(4, 3)),
             att(lse=torch.zeros(2, 4).t()), att(q=q.transpose(1, 2))]
