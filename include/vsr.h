@@ -20,7 +20,8 @@
  *
  * Context-free calls on the same stages' tensors: vsr_rope_axes and
  * vsr_qk_norm_rope (positions with several axes, norms of query and key heads),
- * vsr_pick_tokens (a token per row of logits under rules), vsr_tree_rows and
+ * vsr_pick_tokens (a token per row of logits under rules), vsr_token_logprobs
+ * (given tokens' log-probabilities), vsr_tree_rows and
  * vsr_tree_attention (drafted trees over a paged cache), vsr_pages_update and
  * vsr_pages_keep (that cache's pages), vsr_align_select, vsr_keyframes, vsr_retrieve.
  *
@@ -386,6 +387,39 @@ int vsr_pick_tokens(const void *logits, int32_t dtype, int32_t rows, int32_t voc
                     float *processed, int64_t processed_stride, int32_t *token, float *logprob,
                     void *workspace, size_t ws_bytes, void *hip_stream);
 
+/* Bytes of device workspace vsr_token_logprobs needs (0 for invalid sizes). */
+size_t vsr_token_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t top);
+
+/* Log-probabilities of given tokens under each row of logits, with the token's rank,
+ * the distribution's entropy and its most likely tokens; outputs may be NULL (not
+ * wanted):
+ *   logits  : device [rows][vocab] of dtype (VSR_F32, VSR_BF16, VSR_F16), rows
+ *             stride elements apart (>= vocab);
+ *   tokens  : device [rows] int32; NULL: none given;
+ *   logprob : device [rows] float out, log softmax at the token; -inf for a token
+ *             outside [0, vocab) (as vsr_pick_tokens' -1);
+ *   rank    : device [rows] int32 out, the number of tokens with a larger logit, or the
+ *             same and a lower index (0: the likeliest); -1 for a token outside or
+ *             whose logit is NaN;
+ *   entropy : device [rows] float out, -sum p log p in nats;
+ *   top_id, top_logprob : device [rows][top] int32 and float out, the `top` likeliest
+ *             tokens by falling logit (the same: by rising index) and their
+ *             log-probabilities; -1 and -inf where there are no more above -inf;
+ *   workspace : device, >= vsr_token_logprobs_workspace_size(rows, vocab, top) bytes,
+ *             16-byte aligned, caller-owned; calls that overlap in time need their own
+ *             (two captured graphs that share one must not replay at once).
+ * A NaN or +inf in a row makes its log-probabilities and entropy NaN (NaN is never
+ * among the likeliest). A row of -inf alone: log-probabilities -inf, entropy 0.
+ * Statistics in fp32, those of the likeliest token to its relative accuracy. Outputs
+ * must not overlap inputs or each other. 0 <= rows <= 65535 (0: nothing is done), 1 <=
+ * vocab <= 2^24, 0 <= top <= VSR_MAX_TOP. Enqueued on hip_stream, whose device must be
+ * the current one; errors via vsr_last_error(NULL). */
+#define VSR_MAX_TOP 64
+int vsr_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,
+                       int64_t stride, const int32_t *tokens, int32_t top, float *logprob,
+                       int32_t *rank, float *entropy, int32_t *top_id, float *top_logprob,
+                       void *workspace, size_t ws_bytes, void *hip_stream);
+
 /* Bytes of device workspace vsr_draft_ruled needs for M branches (0 for an
  * invalid config or M). */
 size_t vsr_draft_ruled_workspace_size(const vsr_config *cfg, int32_t M);
@@ -567,7 +601,7 @@ int vsr_align_select(const float *ent, const float *frames, int32_t M, int32_t N
  * (vsr_create, vsr_align_select, vsr_weights_to_f16, vsr_keyframes,
  * vsr_retrieve, vsr_retrieve_static, vsr_rope_axes, vsr_qk_norm_rope,
  * vsr_pick_tokens, vsr_tree_rows, vsr_tree_attention,
- * vsr_pages_update, vsr_pages_keep). */
+ * vsr_pages_update, vsr_pages_keep, vsr_token_logprobs). */
 const char *vsr_last_error(const vsr_ctx *ctx);
 
 /* Keyframes of a video (Section 3.1, Eq. 1). Each frame is compared with the

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Dict, Optional, Sequence
+from typing import Dict, NamedTuple, Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libvsr.so")
@@ -28,7 +28,8 @@ EXPORTS = ["vsr_workspace_size", "vsr_create", "vsr_load_weights", "vsr_prefill"
            "vsr_pick_workspace_size", "vsr_pick_tokens", "vsr_draft_ruled_workspace_size",
            "vsr_draft_ruled", "vsr_tree_rows", "vsr_tree_attention_workspace_size",
            "vsr_tree_attention", "vsr_pages_update_workspace_size", "vsr_pages_update",
-           "vsr_pages_keep", "vsr_last_error",
+           "vsr_pages_keep", "vsr_token_logprobs_workspace_size", "vsr_token_logprobs",
+           "vsr_last_error",
            "vsr_destroy", "vsr_set_checks", "vsr_profile_enable", "vsr_profile_read"]
 
 VSR_SELECT_TWO_STAGE, VSR_SELECT_ADDITION, VSR_SELECT_INVERT = 0, 1, 2
@@ -225,6 +226,11 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.vsr_pages_keep.argtypes = [ctypes.POINTER(VsrPages), ptr, i64, i32, ptr,
                                    ctypes.POINTER(VsrCache), ptr, i32, ptr]
     lib.vsr_pages_keep.restype = ctypes.c_int
+    lib.vsr_token_logprobs_workspace_size.argtypes = [i32] * 3
+    lib.vsr_token_logprobs_workspace_size.restype = ctypes.c_size_t
+    lib.vsr_token_logprobs.argtypes = [ptr, i32, i32, i32, i64, ptr, i32, ptr, ptr, ptr, ptr, ptr,
+                                       ptr, ctypes.c_size_t, ptr]
+    lib.vsr_token_logprobs.restype = ctypes.c_int
     lib.vsr_last_error.argtypes = [ctypes.c_void_p]
     lib.vsr_last_error.restype = ctypes.c_char_p
     lib.vsr_destroy.argtypes = [ctypes.c_void_p]
@@ -803,6 +809,62 @@ def pick_tokens(logits, prompt=None, prompt_len=None, output=None, output_len=No
           (logits, prompt, prompt_len, output, output_len, repetition, presence, frequency, bias,
            mask, processed, token, logprob, workspace))
     return token, logprob
+
+
+class TokenLogprobs(NamedTuple):
+    """What token_logprobs returns; None where it was not asked for."""
+    logprob: object
+    rank: object
+    entropy: object
+    top_id: object
+    top_logprob: object
+
+
+def token_logprobs(logits, tokens=None, top: int = 0, out=None, workspace=None, stream=None):
+    """Log-probabilities of given tokens, one a row (vsr_token_logprobs).
+
+    logits: device [rows][vocab], float32, bfloat16 or float16, rows at any stride from
+    vocab up; tokens: int32 [rows], or None; top: how many of the likeliest tokens to
+    list. Returns TokenLogprobs of logprob [rows], rank [rows] int32, entropy [rows],
+    top_id [rows][top] int32, top_logprob [rows][top] (new ones, or `out`, whose members
+    may be None)."""
+    torch = _torch_names()
+    dtype = _float_types.get(logits.dtype)
+    if dtype is None or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise VsrError(VSR_EINVAL, "logits: float rows [rows][vocab] expected")
+    rows, vocab = logits.shape
+    dev, i32, f32 = logits.get_device(), torch.int32, torch.float32
+    if out is None:
+        one, two = (rows,), (rows, top)
+        new = lambda shape, dt, given: _empty(torch, shape, dt, logits.device, stream) \
+            if given else None  # noqa: E731
+        out = TokenLogprobs(new(one, f32, tokens is not None), new(one, i32, tokens is not None),
+                            new(one, f32, True), new(two, i32, top), new(two, f32, top))
+    else:
+        out = TokenLogprobs(*out)
+    ptrs = []
+    for name, t, dt, n in (("tokens", tokens, i32, rows), ("logprob", out.logprob, f32, rows),
+                           ("rank", out.rank, i32, rows), ("entropy", out.entropy, f32, rows),
+                           ("top_id", out.top_id, i32, rows * top),
+                           ("top_logprob", out.top_logprob, f32, rows * top)):
+        if t is None:
+            ptrs.append(None)
+        elif t.dtype is dt and t.numel() == n and t.is_contiguous() and t.get_device() == dev:
+            ptrs.append(t.data_ptr())
+        else:
+            raise VsrError(VSR_EINVAL, f"{name}: contiguous {dt} of {n} on the logits' device "
+                                       "expected")
+    if workspace is None:
+        size = _lib.vsr_token_logprobs_workspace_size(rows, vocab, top)
+        workspace = _empty(torch, max(size, 16), torch.uint8, logits.device, stream)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise VsrError(VSR_EINVAL, "workspace: contiguous tensor on the logits' device expected")
+    # (A single row's stride is not looked at.)
+    _call(torch, dev, stream, _lib.vsr_token_logprobs,
+          (logits.data_ptr(), dtype, rows, vocab, logits.stride(0) if rows > 1 else vocab, ptrs[0],
+           top, *ptrs[1:], workspace.data_ptr(), workspace.numel() * workspace.element_size()),
+          (logits, tokens, *out, workspace))
+    return out
 
 
 class Pages:

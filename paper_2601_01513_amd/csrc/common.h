@@ -350,7 +350,7 @@ struct LogprobArgs {
   int32_t *rank, *top_id;
   float *top_logprob;
 };
-size_t logprobs_workspace_bytes(int dtype, int rows, int vocab, int top);
+size_t logprobs_workspace_bytes(int rows, int vocab, int top);
 hipError_t launch_logprobs(const LogprobArgs &a, int dtype, void *ws, hipStream_t s);
 
 // Retrieval stage (Eq. 1-3): histograms + keyframes, then per-keyframe top-k

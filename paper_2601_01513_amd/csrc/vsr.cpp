@@ -2125,6 +2125,55 @@ extern "C" int vsr_pages_keep(const vsr_pages *pages, const int32_t *kept, int64
   return VSR_OK;
 }
 
+extern "C" size_t vsr_token_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t top) {
+  if (rows < 1 || rows > kMaxPickRows || vocab < 1 || vocab > kMaxPickVocab || top < 0 ||
+      top > VSR_MAX_TOP)
+    return 0;
+  return align_up(logprobs_workspace_bytes(rows, vocab, top), 16);
+}
+
+extern "C" int vsr_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,
+                                  int64_t stride, const int32_t *tokens, int32_t top,
+                                  float *logprob, int32_t *rank, float *entropy, int32_t *top_id,
+                                  float *top_logprob, void *workspace, size_t ws_bytes,
+                                  void *hip_stream) {
+  g_create_error.clear();
+  const auto check = [&]() -> const char * {
+    if (!float_type(dtype)) return "dtype must be VSR_F32, VSR_BF16 or VSR_F16";
+    if (rows < 0 || rows > kMaxPickRows) return "rows must lie in [0, 65535]";
+    if (vocab < 1 || vocab > kMaxPickVocab) return "vocab must lie in [1, 2^24]";
+    if (top < 0 || top > VSR_MAX_TOP) return "top must lie in [0, 64]";
+    if (rows == 0) return nullptr;
+    const uintptr_t esize = dtype == VSR_F32 ? 4 : 2;
+    if (!logits || !workspace) return "NULL argument";
+    if (reinterpret_cast<uintptr_t>(logits) % esize) return "logits must be aligned to their element";
+    if (stride < vocab || stride > (1LL << 40)) return "stride must be at least vocab";
+    if (!tokens && (logprob || rank)) return "logprob and rank need tokens";
+    if (!aligned4({tokens, logprob, rank, entropy, top_id, top_logprob}))
+      return "tokens and outputs must be 4-byte aligned";
+    const size_t n = (size_t)rows * 4, many = n * top;
+    const struct {
+      const void *p;
+      size_t n;
+    } all[] = {{logprob, n},          {rank, n},   {entropy, n}, {top_id, many}, {top_logprob, many},
+               {tokens, n}, {logits, ((size_t)(rows - 1) * stride + vocab) * esize}};
+    for (int i = 0; i < 5; ++i)
+      for (int j = i + 1; j < 7; ++j)
+        if (ranges_meet(all[i].p, all[i].n, all[j].p, all[j].n)) return "an output overlaps another array";
+    if (reinterpret_cast<uintptr_t>(workspace) & 15) return "workspace must be 16-byte aligned";
+    if (ws_bytes < logprobs_workspace_bytes(rows, vocab, top))
+      return "workspace smaller than vsr_token_logprobs_workspace_size";
+    return nullptr;
+  };
+  if (const char *msg = check()) return refuse(VSR_EINVAL, "token_logprobs", msg);
+  if (rows == 0) return VSR_OK;
+  const LogprobArgs a{logits, (long)stride, rows, vocab, top_id || top_logprob ? top : 0, tokens,
+                      logprob, entropy, rank, top_id, top_logprob};
+  const hipError_t e = launch_logprobs(a, dtype, workspace, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return refuse(VSR_EHIP, "token_logprobs", hipGetErrorString(e));
+  return VSR_OK;
+}
+
 extern "C" int vsr_set_checks(vsr_ctx *ctx, int checks) {
   if (!ctx) return VSR_EINVAL;
   if (checks & ~(VSR_CHECK_IDS | VSR_CHECK_FINITE))
