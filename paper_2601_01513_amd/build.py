@@ -21,6 +21,7 @@ LIB = os.path.join(HERE, "libvsr.so")
 SOURCES = ["vsr.cpp", "kernels_misc.hip", "kernels_f32.hip", "kernels_gemm.hip",
            "kernels_attn.hip", "kernels_retrieval.hip", "kernels_skinny.hip",
            "kernels_rotary.hip", "kernels_pick.hip", "kernels_tree.hip",
+           "kernels_tree_f32.hip", "kernels_tree_bf16.hip", "kernels_tree_f16.hip",
            "kernels_pages.hip", "kernels_logprobs.hip"]
 
 # -packed-fp32-ops: keep hipcc from emitting packed fp32 VALU instructions.

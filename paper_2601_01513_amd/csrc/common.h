@@ -300,14 +300,16 @@ struct TreeAttnArgs {
   const uint32_t *mask;
   long mask_stride;
   int mask_words;
-  float scale_log2;  // scale * log2(e)
-  // Set by the launcher: partial results, blocks of the grid.
+  float scale_log2;  // |scale| log2(e), not 0
+  int negate;        // scale < 0: queries change their sign
+  // Set by the launcher: partial results, what joins them, blocks of the grid.
   float *part;
   float2 *part_ml;
+  struct TreeJoin *joins;
   int groups;
 };
-size_t tree_attention_workspace_bytes(int dtype, int hd, int T, int n_seqs, int n_heads, int n_kv);
-hipError_t launch_tree_attention(TreeAttnArgs a, int dtype, void *ws, hipStream_t s);
+size_t tree_attention_workspace_bytes(int hd, int T, int n_seqs, int n_heads, int n_kv);
+hipError_t launch_tree_attention(const TreeAttnArgs &a, int dtype, void *ws, hipStream_t s);
 
 // A paged cache's keys and values in every layer (vsr_cache), strides in bytes.
 struct CacheRows {

@@ -1937,7 +1937,7 @@ extern "C" size_t vsr_tree_attention_workspace_size(int32_t dtype, int32_t head_
       n_seqs < 1 || n_seqs > VSR_MAX_SEQS || n_kv_heads < 1 || n_heads < 1 || n_heads > 4096 ||
       n_heads % n_kv_heads)
     return 0;
-  return align_up(tree_attention_workspace_bytes(dtype, head_dim, T, n_seqs, n_heads, n_kv_heads),
+  return align_up(tree_attention_workspace_bytes(head_dim, T, n_seqs, n_heads, n_kv_heads),
                   256);
 }
 
@@ -2003,7 +2003,9 @@ extern "C" int vsr_tree_attention(const vsr_pages *pages, int32_t dtype, int32_t
   a.mask = mask;
   a.mask_stride = mask_stride;
   a.mask_words = mask_words;
-  a.scale_log2 = scale * 1.4426950408889634f;
+  // (A scale of 0 as the least that keeps unseen scores at -inf.)
+  a.scale_log2 = std::max(std::fabs(scale) * 1.4426950408889634f, 1.17549435e-38f);
+  a.negate = scale < 0.f;
   const hipError_t e = launch_tree_attention(a, dtype, workspace, static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return refuse(VSR_EHIP, "tree_attention", hipGetErrorString(e));
   return VSR_OK;
