@@ -81,6 +81,7 @@ struct Mat<float> {
 };
 
 constexpr int kTreeThreads = 256;
+constexpr int kAllLoads = 0x0f70;  // s_waitcnt's word for "no load is on its way"
 
 // Shape of a block: 4 waves, WM along the rows (each RT tiles of 16) and WK along the
 // keys of a tile of BK; LDS rows of CH 16-byte chunks.
@@ -227,6 +228,7 @@ struct Rows {
   Q q[S::RT][QN];
   int j[S::RT];         // row of the draft
   float m[S::RT], l[S::RT];
+  bool any;             // whether the wave has a row
   f32x4 o[S::RT][S::HD / 16];
 };
 
@@ -241,6 +243,7 @@ __device__ __forceinline__ void load_rows(const TreeAttnArgs &a, const Work &w, 
   typedef typename S::T T;
   const int lane = threadIdx.x & 63, g4 = lane >> 4, wm = (threadIdx.x >> 6) % S::WM;
   const int G = a.n_heads / a.n_kv;
+  R.any = __builtin_amdgcn_readfirstlane((long)tile * S::BM + wm * S::RT * 16 < (long)w.n * G);
 #pragma unroll
   for (int rt = 0; rt < S::RT; ++rt) {
     const long r = (long)tile * S::BM + (wm * S::RT + rt) * 16 + (lane & 15);
@@ -278,7 +281,7 @@ __device__ __forceinline__ void load_rows(const TreeAttnArgs &a, const Work &w, 
   }
 }
 
-// Pages of the keys that a thread loads, of the tile at kb.
+// Pages of the keys that a thread loads, of the tile at kb (past the keys: the last one's).
 template <class S>
 __device__ __forceinline__ void load_pages(const TreeAttnArgs &a, const Work &w, int kb,
                                            int32_t *page) {
@@ -286,8 +289,16 @@ __device__ __forceinline__ void load_pages(const TreeAttnArgs &a, const Work &w,
 #pragma unroll
   for (int i = 0; i < S::NL; ++i) {
     const int p = kb + (i * kTreeThreads + (int)threadIdx.x) / S::CH;
-    page[i] = p < w.keys ? table[p >> a.pages.page_shift] : -1;
+    page[i] = table[min(p, w.keys - 1) >> a.pages.page_shift];
   }
+}
+
+// Chunk of the row that a thread's load i brings (it lands in chunk tid % CH of the row).
+template <class S>
+__device__ __forceinline__ int load_chunk(int i) {
+  constexpr int STEP = kTreeThreads / S::CH;  // rows from load to load
+  const int tid = threadIdx.x, c = (tid % S::CH) ^ swz<S::CH>(tid / S::CH);
+  return S::CH >= 16 ? c ^ (i * STEP & 15) : c;
 }
 
 // Key tile kb of both matrices on its way into an LDS stage: rows past the sequence's
@@ -303,20 +314,20 @@ __device__ __forceinline__ void load_tile(const TreeAttnArgs &a, const Work &w, 
   const bool all = kb + S::BK <= w.keys && a.hd == S::HD;
 #pragma unroll
   for (int i = 0; i < S::NL; ++i) {
-    const int at = i * kTreeThreads + tid, r = at / S::CH, c = (at % S::CH) ^ swz<S::CH>(r);
-    const int p = kb + r;
+    const int r = i * (kTreeThreads / S::CH) + tid / S::CH, p = kb + r, c = load_chunk<S>(i);
     const uint32_t pg = (uint32_t)page[i] < (uint32_t)a.pages.n_pages ? page[i] : 0;
     const uint32_t slot = pg << shift | ((uint32_t)p & ((1u << shift) - 1));
     if constexpr (VEC) {
       const uint32_t kt = (uint32_t)(a.k_ts * sizeof(T)), vt = (uint32_t)(a.v_ts * sizeof(T));
-      const char *kp = reinterpret_cast<const char *>(k) + ((uint64_t)slot * kt + c * 16);
-      const char *vp = reinterpret_cast<const char *>(v) + ((uint64_t)slot * vt + c * 16);
+      const char *kp = reinterpret_cast<const char *>(k) + c * 16 + (uint64_t)slot * kt;
+      const char *vp = reinterpret_cast<const char *>(v) + c * 16 + (uint64_t)slot * vt;
       if (!all && (p >= w.keys || c * S::EC >= a.hd))
         kp = vp = reinterpret_cast<const char *>(&g_zeros);
       u32x4 *to = stage + i * kTreeThreads + (tid & ~63);
       __builtin_amdgcn_global_load_lds(kp, to, 16, 0, 0);
       __builtin_amdgcn_global_load_lds(vp, to + S::TILE, 16, 0, 0);
     } else {
+      const int at = i * kTreeThreads + tid;
       const T *kp = k + slot * a.k_ts + c * S::EC, *vp = v + slot * a.v_ts + c * S::EC;
       const bool real = p < w.keys && c * S::EC < a.hd;
       Pack<T, S::EC> x{}, y{};
@@ -336,20 +347,55 @@ __device__ __forceinline__ void load_tile(const TreeAttnArgs &a, const Work &w, 
   }
 }
 
-// Four V elements of column (dt 16 + lane % 16), keys 4 (lane / 16) .. + 3 of the 16
-// from row k0 on.
+// Byte offsets in a tile of what a lane reads of its first 16 keys, for chunk 0 (keys) and
+// column tile 0 (values). Others differ by an exclusive or (a swizzled row's chunks c and
+// c0 ^ c) and by whole rows. The compiler is kept from working them out ahead of the
+// loops: it took a register for each, spilled them, and waited for the reloads.
 template <class S>
-__device__ __forceinline__ typename Mat<typename S::T>::x4 v_frag(const u32x4 *vs, int k0, int dt) {
+__device__ __forceinline__ int key_offset() {
+  const int l = threadIdx.x & 15, g4 = (threadIdx.x & 63) >> 4;
+  int at = l * S::CH * 16 + ((g4 ^ swz<S::CH>(l)) << 4);
+  asm volatile("" : "+v"(at));
+  return at;
+}
+template <class S>
+__device__ __forceinline__ int value_offset() {
+  const int l = threadIdx.x & 15, g4 = (threadIdx.x & 63) >> 4;
+  int at;
+  if constexpr (S::F32) {
+    at = 4 * g4 * S::CH * 16 + ((l >> 2 ^ swz<S::CH>(4 * g4)) << 4) + (l & 3) * 4;
+  } else {
+    const int r = 4 * g4 + (l >> 2);
+    at = r * S::CH * 16 + (((l & 3) >> 1 ^ swz<S::CH>(r)) << 4) + (l & 1) * 8;
+  }
+  asm volatile("" : "+v"(at));
+  return at;
+}
+
+// Four V elements of column d 16 + lane % 16, keys 4 (lane / 16) .. + 3 of the 16 from
+// row k0 on: a transposing read of four rows by 16 lanes.
+template <class S>
+__device__ __forceinline__ typename Mat<typename S::T>::x4 v_frag(const u32x4 *vs, int at, int k0,
+                                                                  int d) {
   typedef short s16x4 __attribute__((ext_vector_type(4)));
-  const int lane = threadIdx.x & 63, i = lane & 15;
-  const int r = k0 + 4 * (lane >> 4) + (i >> 2);
-  const int c = (dt * 2 + ((i & 3) >> 1)) ^ swz<S::CH>(r);
-  const char *p = reinterpret_cast<const char *>(vs + r * S::CH + c) + (i & 1) * 8;
+  const char *p = reinterpret_cast<const char *>(vs) + (at ^ d * 32) + k0 * S::CH * 16;
   return __builtin_bit_cast(
       typename Mat<typename S::T>::x4,
       __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (__attribute__((address_space(3))) s16x4 *)const_cast<char *>(p)));
 }
+
+// The V operands of VG columns of 16 from column tile d0 on, for a wave's keys.
+template <class S, int VG>
+struct VFrag {
+  typename Mat<typename S::T>::x4 v[VG][S::KW];
+  __device__ __forceinline__ void read(const u32x4 *vs, int at, int key0, int d0) {
+#pragma unroll
+    for (int n = 0; n < VG; ++n)
+#pragma unroll
+      for (int t = 0; t < S::KW; ++t) v[n][t] = v_frag<S>(vs, at, key0 + t * 16, d0 + n);
+  }
+};
 
 template <typename T>
 __device__ __forceinline__ bool not_finite(T x) {
@@ -383,38 +429,57 @@ __device__ __forceinline__ bool clear_odd(u32x4 *vs, int context) {
   return any;
 }
 
+// Keeps the compiler from moving anything across: groups of LDS reads stay a group of
+// products ahead of their use (left to itself it puts each read right before its
+// product, and a tile waits for 28 of them).
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
 // One key tile against a wave's rows. DRAFT: the tile has keys past len.
 template <class S, bool DRAFT>
 __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, int kb,
-                                          u32x4 *st, Rows<S> &R, int *met_odd) {
+                                          const u32x4 *st, Rows<S> &R) {
   typedef typename S::T T;
   typedef Mat<T> M;
   const int lane = threadIdx.x & 63, g4 = lane >> 4, wk = (threadIdx.x >> 6) / S::WM;
-  const u32x4 *ks = st;
-  u32x4 *vs = st + S::TILE;
+  const u32x4 *ks = st, *vs = st + S::TILE;
   const int key0 = wk * S::KW * 16;
   f32x4 x[S::RT][S::KW];
+  constexpr int KC = S::CH / 4;  // 16-byte chunks a lane reads of a key tile
+  const int k_at = key_offset<S>(), v_at = value_offset<S>();
+  const auto read_keys = [&](int t, u32x4 *kf) {
+    const char *p = reinterpret_cast<const char *>(ks) + (key0 + t * 16) * S::CH * 16;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) kf[c] = *reinterpret_cast<const u32x4 *>(p + (k_at ^ c * 64));
+  };
+  u32x4 kf[2][KC];
+  read_keys(0, kf[0]);
 #pragma unroll
   for (int t = 0; t < S::KW; ++t) {
+    in_order();
+    if (t + 1 < S::KW) read_keys(t + 1, kf[(t + 1) & 1]);
+    in_order();
 #pragma unroll
     for (int rt = 0; rt < S::RT; ++rt) x[rt][t] = f32x4{};
-    const int r = key0 + t * 16 + (lane & 15);
 #pragma unroll
-    for (int c = 0; c < S::CH / 4; ++c) {
-      const u32x4 kf = ks[r * S::CH + ((4 * c + g4) ^ swz<S::CH>(r))];
+    for (int c = 0; c < KC; ++c)
 #pragma unroll
       for (int rt = 0; rt < S::RT; ++rt) {
         if constexpr (S::F32) {
-          const f32x4 kv = __builtin_bit_cast(f32x4, kf);
+          const f32x4 kv = __builtin_bit_cast(f32x4, kf[t & 1][c]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[rt][t] = M::mul(kv[i], R.q[rt][c * 4 + i], x[rt][t]);
         } else {
-          x[rt][t] = M::mul(__builtin_bit_cast(typename M::x8, kf),
+          x[rt][t] = M::mul(__builtin_bit_cast(typename M::x8, kf[t & 1][c]),
                             __builtin_bit_cast(typename M::x8, R.q[rt][c]), x[rt][t]);
         }
       }
-    }
   }
+  in_order();
+  // The first values are on their way during the softmax.
+  constexpr int VG = S::F32 ? 1 : 2;  // columns of 16 a group of value reads
+  struct None {};
+  typename std::conditional<S::F32, None, VFrag<S, VG>>::type vf[2];
+  if constexpr (!S::F32) vf[0].read(vs, v_at, key0, 0);
   if constexpr (DRAFT) {
 #pragma unroll
     for (int rt = 0; rt < S::RT; ++rt) {
@@ -439,8 +504,6 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
         }
       }
     }
-    if (clear_odd<S>(vs, w.len - kb)) *met_odd = 1;
-    __syncthreads();
   }
   const float c = a.scale_log2;
 #pragma unroll
@@ -473,6 +536,7 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
           const float y = x[rt][t][i] * c;
           x[rt][t][i] = y - ref;
         }
+      asm volatile("");  // (or the products are taken out of the branch)
     } else {
 #pragma unroll
       for (int t = 0; t < S::KW; ++t)
@@ -495,12 +559,10 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
     for (int t = 0; t < S::KW; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = key0 + t * 16 + 4 * g4 + i;
+        const char *row = reinterpret_cast<const char *>(vs) + (key0 + t * 16 + i) * S::CH * 16;
 #pragma unroll
         for (int d = 0; d < S::HD / 16; ++d) {
-          const int col = d * 16 + (lane & 15);
-          const float v = reinterpret_cast<const float *>(
-              vs + r * S::CH + ((col >> 2) ^ swz<S::CH>(r)))[col & 3];
+          const float v = *reinterpret_cast<const float *>(row + (v_at ^ (d * 64 ^ i * 16)));
 #pragma unroll
           for (int rt = 0; rt < S::RT; ++rt) R.o[rt][d] = M::mul(v, x[rt][t][i], R.o[rt][d]);
         }
@@ -515,25 +577,30 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
       for (int t = 0; t < S::KW; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[rt][t][i] = from_f32<T>(x[rt][t][i]);
+    constexpr int NG = S::HD / 16 / VG;
 #pragma unroll
-    for (int d = 0; d < S::HD / 16; ++d) {
-      x4 v[S::KW];
+    for (int g = 0; g < NG; ++g) {
+      in_order();
+      if (g + 1 < NG) vf[(g + 1) & 1].read(vs, v_at, key0, (g + 1) * VG);
+      in_order();
 #pragma unroll
-      for (int t = 0; t < S::KW; ++t) v[t] = v_frag<S>(vs, key0 + t * 16, d);
+      for (int n = 0; n < VG; ++n) {
+        const x4 *v = vf[g & 1].v[n];
+        const int d = g * VG + n;
 #pragma unroll
-      for (int rt = 0; rt < S::RT; ++rt) {
-        if constexpr (S::KW == 1) {
-          R.o[rt][d] = M::mul(v[0], p[rt][0], R.o[rt][d]);
-        } else {
-          // The 32 keys of two tiles: a lane's first four k are tile t's, the others t + 1's,
-          // in both operands.
+        for (int t = 0; t < S::KW; t += 2)
 #pragma unroll
-          for (int t = 0; t < S::KW; t += 2) {
-            const x8 vv = __builtin_shufflevector(v[t], v[t + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-            const x8 pp = __builtin_shufflevector(p[rt][t], p[rt][t + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-            R.o[rt][d] = M::mul(vv, pp, R.o[rt][d]);
+          for (int rt = 0; rt < S::RT; ++rt) {
+            if constexpr (S::KW == 1) {
+              R.o[rt][d] = M::mul(v[0], p[rt][0], R.o[rt][d]);
+            } else {
+              // The 32 keys of two tiles: a lane's first four k are tile t's, the others
+              // t + 1's, in both operands.
+              const x8 vv = __builtin_shufflevector(v[t], v[t + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+              const x8 pp = __builtin_shufflevector(p[rt][t], p[rt][t + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+              R.o[rt][d] = M::mul(vv, pp, R.o[rt][d]);
+            }
           }
-        }
       }
     }
   }
@@ -579,7 +646,7 @@ __device__ __forceinline__ f32x4 odd_values(const TreeAttnArgs &a, const Work &w
 // result `which` of block g.
 template <class S>
 __device__ __forceinline__ void store_rows(const TreeAttnArgs &a, const Work &w, int kvh, int tile,
-                                           Rows<S> &R, u32x4 *lds, float2 *ml, long which,
+                                           Rows<S> &R, u32x4 *lds0, u32x4 *lds1, float2 *ml, long which,
                                            const int *met_odd, int from, int to) {
   typedef typename S::T T;
   const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4;
@@ -594,7 +661,11 @@ __device__ __forceinline__ void store_rows(const TreeAttnArgs &a, const Work &w,
       ml[wk * S::BM + (wm * S::RT + rt) * 16 + lane] = make_float2(R.m[rt], R.l[rt]);
   }
   __syncthreads();
-  f32x4 *o = reinterpret_cast<f32x4 *>(lds);
+  // (The join takes both stages.)
+  const auto o = [&](int i) -> f32x4 & {
+    u32x4 *at = i < 2 * S::TILE ? lds0 + i : lds1 + (i - 2 * S::TILE);
+    return *reinterpret_cast<f32x4 *>(at);
+  };
 #pragma unroll
   for (int rt = 0; rt < S::RT; ++rt) {
     const int r = (wm * S::RT + rt) * 16 + (lane & 15);
@@ -604,7 +675,7 @@ __device__ __forceinline__ void store_rows(const TreeAttnArgs &a, const Work &w,
     const float f = R.m[rt] == -INFINITY ? (top == -INFINITY ? 1.f : 0.f)
                                          : __builtin_amdgcn_exp2f(R.m[rt] - top);
 #pragma unroll
-    for (int d = 0; d < S::HD / 16; ++d) o[join_at<S>(wk, r, d * 4 + g4)] = R.o[rt][d] * f;
+    for (int d = 0; d < S::HD / 16; ++d) o(join_at<S>(wk, r, d * 4 + g4)) = R.o[rt][d] * f;
   }
   __syncthreads();
   for (int i = tid; i < S::BM * (S::HD / 4); i += kTreeThreads) {
@@ -619,7 +690,7 @@ __device__ __forceinline__ void store_rows(const TreeAttnArgs &a, const Work &w,
     for (int k = 0; k < S::WK; ++k) {
       const float2 x = ml[k * S::BM + r];
       l += x.x == -INFINITY ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - top);
-      y += o[join_at<S>(k, r, c)];
+      y += o(join_at<S>(k, r, c));
     }
     const int j = (int)gr / G, h = kvh * G + (int)gr % G;
     if (*met_odd) y += odd_values<S>(a, w, kvh, j, c, from, last);
@@ -650,7 +721,7 @@ __device__ __forceinline__ void store_rows(const TreeAttnArgs &a, const Work &w,
 
 template <class S, bool VEC>
 __global__ __launch_bounds__(kTreeThreads, S::PER_CU) void k_tree_attn(TreeAttnArgs a) {
-  __shared__ u32x4 ring[4 * S::TILE];
+  __shared__ u32x4 ring0[2 * S::TILE], ring1[2 * S::TILE];
   __shared__ float2 ml[S::WK * S::BM];
   __shared__ long sums[kTreeThreads / 64], found[2];
   __shared__ int met_odd;
@@ -681,34 +752,51 @@ __global__ __launch_bounds__(kTreeThreads, S::PER_CU) void k_tree_attn(TreeAttnA
     const int b2 = min(b1, (int)((upto + S::BK - 1) / S::BK));
     load_rows<S>(a, w, kvh, tile, R);
     if (b0 < b2) {
+      int32_t page[S::NL];
+      load_pages<S>(a, w, b0 * S::BK, page);
+      load_tile<S, VEC>(a, w, kvh, b0 * S::BK, page, ring0);
+      load_pages<S>(a, w, (b0 + 1) * S::BK, page);
+      // Tile b, in `cur`, against the rows, while tile b + 1 is on its way into `nxt`.
+      // The stages are arrays of their own so that the compiler knows that reads of one
+      // need not wait for loads into the other.
+      const auto step = [&](auto draft, int b, u32x4 *cur, u32x4 *nxt) {
+        __builtin_amdgcn_s_waitcnt(kAllLoads);
+        __syncthreads();  // tile b is there for every wave, the other stage is free
+        if (b + 1 < b2) {
+          load_tile<S, VEC>(a, w, kvh, (b + 1) * S::BK, page, nxt);
+          load_pages<S>(a, w, (b + 2) * S::BK, page);
+        }
+        if constexpr (draft.value) {
+          if (clear_odd<S>(cur + S::TILE, w.len - b * S::BK)) met_odd = 1;
+          __syncthreads();
+        }
+        if (R.any) tile_step<S, draft.value>(a, w, b * S::BK, cur, R);
+      };
       // Tiles of the context first, in a loop of their own: with one loop around both kinds
       // the kernel spilled registers inside it, and a reload from scratch waits for
       // every load before it, the next tile's among them.
-      int32_t page[S::NL];
-      load_pages<S>(a, w, b0 * S::BK, page);
-      load_tile<S, VEC>(a, w, kvh, b0 * S::BK, page, ring);
-      load_pages<S>(a, w, (b0 + 1) * S::BK, page);
-      int b = b0, stage = 0;
+      const std::integral_constant<bool, false> context;
+      const std::integral_constant<bool, true> draft;
       const int plain = min(b2, w.len / S::BK);
-      for (; b < plain; ++b, stage ^= 2 * S::TILE) {
-        __syncthreads();  // tile b is there, the other stage is free
-        if (b + 1 < b2) {
-          load_tile<S, VEC>(a, w, kvh, (b + 1) * S::BK, page, ring + (stage ^ 2 * S::TILE));
-          load_pages<S>(a, w, (b + 2) * S::BK, page);
+      int b = b0;
+      bool second = false;
+      for (; b < plain; ++b) {
+        step(context, b, ring0, ring1);
+        if (++b >= plain) {
+          second = true;
+          break;
         }
-        tile_step<S, false>(a, w, b * S::BK, ring + stage, R, &met_odd);
+        step(context, b, ring1, ring0);
       }
-      for (; b < b2; ++b, stage ^= 2 * S::TILE) {
-        __syncthreads();
-        if (b + 1 < b2) {
-          load_tile<S, VEC>(a, w, kvh, (b + 1) * S::BK, page, ring + (stage ^ 2 * S::TILE));
-          load_pages<S>(a, w, (b + 2) * S::BK, page);
-        }
-        tile_step<S, true>(a, w, b * S::BK, ring + stage, R, &met_odd);
+      for (; b < b2; ++b, second = !second) {
+        if (second)
+          step(draft, b, ring1, ring0);
+        else
+          step(draft, b, ring0, ring1);
       }
     }
     const bool whole = b0 == 0 && b1 == w.nb;
-    store_rows<S>(a, w, kvh, tile, R, ring, ml, whole ? -1 : 2L * g + (b0 == 0), &met_odd,
+    store_rows<S>(a, w, kvh, tile, R, ring0, ring1, ml, whole ? -1 : 2L * g + (b0 == 0), &met_odd,
                   b0 * S::BK, b2 * S::BK);
     if (threadIdx.x == 0) met_odd = 0;
     at += b1 - b0;
