@@ -15,10 +15,10 @@
 
 namespace vsr {
 
-// A join of partial results: rows of item (b, n, kvh, tile) from blocks first .. last
+// A join of partial results: those of item (b, n, kvh, tile) from blocks first .. last
 // (last < 0: none).
 struct TreeJoin {
-  int b, n, kvh, tile, last;
+  int b, n, kvh, tile, step, last;
 };
 
 hipError_t launch_tree_f32(const TreeAttnArgs &a, void *ws, hipStream_t s);
@@ -80,26 +80,27 @@ struct Mat<float> {
   }
 };
 
-constexpr int kTreeThreads = 256;
 constexpr int kAllLoads = 0x0f70;  // s_waitcnt's word for "no load is on its way"
 
-// Shape of a block: 4 waves, WM along the rows (each RT tiles of 16) and WK along the
+// Shape of a block: NW waves, WM along the rows (each RT tiles of 16) and WK along the
 // keys of a tile of BK; LDS rows of CH 16-byte chunks.
-template <typename T_, int HD_, int RT_, int WM_>
+template <typename T_, int HD_, int NW_, int RT_, int WM_>
 struct TreeShape {
   typedef T_ T;
-  static constexpr int HD = HD_, RT = RT_, WM = WM_, WK = 4 / WM_;
+  static constexpr int HD = HD_, NW = NW_, RT = RT_, WM = WM_, WK = NW / WM;
+  static constexpr int NT = NW * 64;
   static constexpr bool F32 = sizeof(T) == 4;
   static constexpr int BK = F32 && HD == 256 ? 32 : 64;
   static constexpr int BM = WM * RT * 16;
-  static constexpr int KW = BK / 16 / WK;   // 16-key tiles of a wave
+  static constexpr int KW = BK / 16 / WK;    // 16-key tiles of a wave
   static constexpr int EC = 16 / sizeof(T);  // elements a chunk
   static constexpr int CH = HD / EC;
-  static constexpr int NL = BK * CH / kTreeThreads;  // chunks of K a thread loads
-  static constexpr int TILE = BK * CH;               // chunks of a K or V tile
-  static constexpr int PER_CU = 4 * TILE * 16 <= 72 << 10 ? 2 : 1;  // blocks (by LDS)
-  static_assert(KW >= 1 && NL >= 1, "each wave has keys");
-  static_assert((size_t)WK * BM * HD * 4 <= (size_t)4 * TILE * 16, "the join fits the ring");
+  static constexpr int NL = BK * CH / NT;    // chunks of K a thread loads
+  static constexpr int TILE = BK * CH;       // chunks of a K or V tile
+  // Blocks a CU: by LDS, and two waves a SIMD.
+  static constexpr int PER_CU = NW == 4 && 4 * TILE * 16 <= 72 << 10 ? 2 : 1;
+  static_assert(KW >= 1 && NL >= 1, "each wave has keys, each thread a load");
+  static_assert(WK == 1 || WK * BM * HD * 4 <= 4 * TILE * 16, "waves along the keys join in the ring");
 };
 
 // LDS gives 256 bytes to 16 lanes at once: chunk c of row r lies where 16 rows' chunks
@@ -109,14 +110,19 @@ __device__ __forceinline__ int swz(int r) {
   return CH >= 16 ? r & 15 : (r >> 1) & 7;
 }
 
-// The walk of all blocks over all work: item (sequence, key head, tile of rows, tiles
-// innermost) has as many units as its sequence has key tiles; block g of `eff` takes
-// units [total g / eff, total (g + 1) / eff).
+// The walk of all blocks over all work. An item is (sequence, key head, tile of rows),
+// tiles innermost, the sequence's rows shared evenly by its tiles; its key tiles cost what
+// they take: loads and waits about as much as kTileCost of the waves that have rows.
+// Block g of `eff` takes the key tiles that begin in [total g / eff, total (g + 1) / eff)
+// of the summed costs.
+constexpr int kTileCost = 3;
+
 struct Work {
-  int s, b, n;       // a sequence and its rows
-  int len, keys;     // positions before the draft, and with it
-  int tiles, nb;     // row tiles, key tiles
-  long base;         // units before it
+  int s, b, n;      // a sequence and its rows
+  int len, keys;    // positions before the draft, and with it
+  int tiles, step;  // row tiles, rows of each
+  int nb, cost;     // key tiles of an item, cost of each
+  long base;        // cost of the items before the sequence's
 };
 
 template <class S>
@@ -127,16 +133,20 @@ __device__ __forceinline__ void work_of(const TreeAttnArgs &a, int s, Work &w) {
   w.n = e - w.b;
   w.len = seq_len(a.pages, s);
   w.keys = (int)min((long)w.len + w.n, (long)seq_room(a.pages, s));
-  const int G = a.n_heads / a.n_kv;
-  w.tiles = (int)(((long)w.n * G + S::BM - 1) / S::BM);
+  const long rows = (long)w.n * (a.n_heads / a.n_kv);
+  w.tiles = (int)((rows + S::BM - 1) / S::BM);
+  // (The least multiple of 16 that `tiles` of cover the rows.)
+  w.step = w.tiles ? ((int)((rows + w.tiles - 1) / w.tiles) + 15) / 16 * 16 : 16;
   w.nb = max(1, (int)(((long)w.keys + S::BK - 1) / S::BK));
+  w.cost = kTileCost + (w.step + 16 * S::RT - 1) / (16 * S::RT);
 }
 
-__device__ __forceinline__ long work_units(const TreeAttnArgs &a, const Work &w) {
-  return (long)a.n_kv * w.tiles * w.nb;
+__device__ __forceinline__ long work_cost(const TreeAttnArgs &a, const Work &w) {
+  return (long)a.n_kv * w.tiles * w.nb * w.cost;
 }
 
-// Units before each thread's run of sequences, and their total, in LDS.
+// Exclusive prefix sum over a block's NT threads, and the total.
+template <int NT>
 __device__ __forceinline__ long block_scan(long mine, long *sums, long &total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   long v = mine;
@@ -150,7 +160,7 @@ __device__ __forceinline__ long block_scan(long mine, long *sums, long &total) {
   long before = 0;
   total = 0;
 #pragma unroll
-  for (int i = 0; i < kTreeThreads / 64; ++i) {
+  for (int i = 0; i < NT / 64; ++i) {
     if (i < w) before += sums[i];
     total += sums[i];
   }
@@ -158,10 +168,12 @@ __device__ __forceinline__ long block_scan(long mine, long *sums, long &total) {
   return before + v - mine;
 }
 
-constexpr int kMinUnits = 2;  // the least units worth a block
-
+// A block takes two of the dearest key tiles at least (one that lies between an item's
+// first and last block then has one of its tiles).
+template <class S>
 __device__ __forceinline__ int blocks_used(long total, int groups) {
-  return (int)max(1L, min((total + kMinUnits - 1) / kMinUnits, (long)groups));
+  constexpr int least = 2 * (kTileCost + S::WM);
+  return (int)max(1L, min(total / least, (long)groups));
 }
 // Blocks of one XCD take neighbouring ranges (tiles that share keys), unless there are
 // fewer of them than the grid has.
@@ -173,13 +185,13 @@ __device__ __forceinline__ int logical_block(int b, int eff, int groups) {
 template <class S>
 __device__ __forceinline__ void find_unit(const TreeAttnArgs &a, long first, long at, long *found,
                                           Work &w) {
-  const int per = (a.pages.n_seqs + kTreeThreads - 1) / kTreeThreads;
+  const int per = (a.pages.n_seqs + S::NT - 1) / S::NT;
   const int s0 = threadIdx.x * per;
   long base = first;
   for (int i = 0; i < per && s0 + i < a.pages.n_seqs; ++i) {
     Work x;
     work_of<S>(a, s0 + i, x);
-    const long u = work_units(a, x);
+    const long u = work_cost(a, x);
     if (at >= base && at < base + u) {
       found[0] = s0 + i;
       found[1] = base;
@@ -194,15 +206,15 @@ __device__ __forceinline__ void find_unit(const TreeAttnArgs &a, long first, lon
 }
 
 template <class S>
-__device__ __forceinline__ long my_units(const TreeAttnArgs &a) {
-  const int per = (a.pages.n_seqs + kTreeThreads - 1) / kTreeThreads;
+__device__ __forceinline__ long my_cost(const TreeAttnArgs &a) {
+  const int per = (a.pages.n_seqs + S::NT - 1) / S::NT;
   long u = 0;
   for (int i = 0; i < per; ++i) {
     const int s = threadIdx.x * per + i;
     if (s >= a.pages.n_seqs) break;
     Work x;
     work_of<S>(a, s, x);
-    u += work_units(a, x);
+    u += work_cost(a, x);
   }
   return u;
 }
@@ -243,17 +255,17 @@ __device__ __forceinline__ void load_rows(const TreeAttnArgs &a, const Work &w, 
   typedef typename S::T T;
   const int lane = threadIdx.x & 63, g4 = lane >> 4, wm = (threadIdx.x >> 6) % S::WM;
   const int G = a.n_heads / a.n_kv;
-  R.any = __builtin_amdgcn_readfirstlane((long)tile * S::BM + wm * S::RT * 16 < (long)w.n * G);
+  const int rows = (int)min((long)w.step, (long)w.n * G - (long)tile * w.step);
+  R.any = __builtin_amdgcn_readfirstlane(wm * S::RT * 16 < rows);
 #pragma unroll
   for (int rt = 0; rt < S::RT; ++rt) {
-    const long r = (long)tile * S::BM + (wm * S::RT + rt) * 16 + (lane & 15);
-    const bool real = r < (long)w.n * G;
-    const int rc = real ? (int)r : 0;
-    R.j[rt] = rc / G;
+    const int r = (wm * S::RT + rt) * 16 + (lane & 15);
+    const long rc = r < rows ? (long)tile * w.step + r : 0;
+    R.j[rt] = (int)(rc / G);
     R.m[rt] = -INFINITY;
     R.l[rt] = 0.f;
     const T *q = static_cast<const T *>(a.q) + (w.b + R.j[rt]) * a.q_ts +
-                 (long)(kvh * G + rc % G) * a.q_hs;
+                 (long)(kvh * G + (int)(rc % G)) * a.q_hs;
     constexpr int V = S::F32 ? 4 : 8;
 #pragma unroll
     for (int c = 0; c < Rows<S>::QN / (S::F32 ? 4 : 1); ++c) {
@@ -288,7 +300,7 @@ __device__ __forceinline__ void load_pages(const TreeAttnArgs &a, const Work &w,
   const int32_t *table = a.pages.table + w.s * a.pages.table_stride;
 #pragma unroll
   for (int i = 0; i < S::NL; ++i) {
-    const int p = kb + (i * kTreeThreads + (int)threadIdx.x) / S::CH;
+    const int p = kb + (i * S::NT + (int)threadIdx.x) / S::CH;
     page[i] = table[min(p, w.keys - 1) >> a.pages.page_shift];
   }
 }
@@ -296,7 +308,7 @@ __device__ __forceinline__ void load_pages(const TreeAttnArgs &a, const Work &w,
 // Chunk of the row that a thread's load i brings (it lands in chunk tid % CH of the row).
 template <class S>
 __device__ __forceinline__ int load_chunk(int i) {
-  constexpr int STEP = kTreeThreads / S::CH;  // rows from load to load
+  constexpr int STEP = S::NT / S::CH;  // rows from load to load
   const int tid = threadIdx.x, c = (tid % S::CH) ^ swz<S::CH>(tid / S::CH);
   return S::CH >= 16 ? c ^ (i * STEP & 15) : c;
 }
@@ -314,7 +326,7 @@ __device__ __forceinline__ void load_tile(const TreeAttnArgs &a, const Work &w, 
   const bool all = kb + S::BK <= w.keys && a.hd == S::HD;
 #pragma unroll
   for (int i = 0; i < S::NL; ++i) {
-    const int r = i * (kTreeThreads / S::CH) + tid / S::CH, p = kb + r, c = load_chunk<S>(i);
+    const int r = i * (S::NT / S::CH) + tid / S::CH, p = kb + r, c = load_chunk<S>(i);
     const uint32_t pg = (uint32_t)page[i] < (uint32_t)a.pages.n_pages ? page[i] : 0;
     const uint32_t slot = pg << shift | ((uint32_t)p & ((1u << shift) - 1));
     if constexpr (VEC) {
@@ -323,11 +335,11 @@ __device__ __forceinline__ void load_tile(const TreeAttnArgs &a, const Work &w, 
       const char *vp = reinterpret_cast<const char *>(v) + c * 16 + (uint64_t)slot * vt;
       if (!all && (p >= w.keys || c * S::EC >= a.hd))
         kp = vp = reinterpret_cast<const char *>(&g_zeros);
-      u32x4 *to = stage + i * kTreeThreads + (tid & ~63);
+      u32x4 *to = stage + i * S::NT + (tid & ~63);
       __builtin_amdgcn_global_load_lds(kp, to, 16, 0, 0);
       __builtin_amdgcn_global_load_lds(vp, to + S::TILE, 16, 0, 0);
     } else {
-      const int at = i * kTreeThreads + tid;
+      const int at = i * S::NT + tid;
       const T *kp = k + slot * a.k_ts + c * S::EC, *vp = v + slot * a.v_ts + c * S::EC;
       const bool real = p < w.keys && c * S::EC < a.hd;
       Pack<T, S::EC> x{}, y{};
@@ -412,7 +424,7 @@ __device__ __forceinline__ bool clear_odd(u32x4 *vs, int context) {
   bool any = false;
 #pragma unroll 1
   for (int i = 0; i < S::NL; ++i) {
-    const int n = i * kTreeThreads + threadIdx.x;
+    const int n = i * S::NT + threadIdx.x;
     if (n / S::CH < context) continue;
     u32x4 *at = vs + n;
     Pack<T, S::EC> x = __builtin_bit_cast(Pack<T, S::EC>, *at);
@@ -606,12 +618,6 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
   }
 }
 
-// Float chunk c (of HD / 4) of row r in the join's LDS area.
-template <class S>
-__device__ __forceinline__ int join_at(int wk, int r, int c) {
-  return (wk * S::BM + r) * (S::HD / 4) + (c ^ (r & 15));
-}
-
 // Whether row j sees position len + d of its draft.
 __device__ __forceinline__ bool sees(const TreeAttnArgs &a, const Work &w, int j, int d) {
   if (!a.mask) return d <= j;
@@ -642,93 +648,118 @@ __device__ __forceinline__ f32x4 odd_values(const TreeAttnArgs &a, const Work &w
   return y;
 }
 
-// The waves' shares of an item joined and stored: out and lse, or (which >= 0) partial
-// result `which` of block g.
+// Columns 4 c .. + 3 of a row of the item: its sum y over a sum of probabilities l, scores
+// relative to `top`; into out and lse, or (which >= 0) partial result `which`.
+template <class S>
+__device__ __forceinline__ void put_row(const TreeAttnArgs &a, const Work &w, int kvh, int tile,
+                                        int r, int c, f32x4 y, float l, float top, long which) {
+  typedef typename S::T T;
+  if (which >= 0) {
+    reinterpret_cast<f32x4 *>(a.part)[(which * S::BM + r) * (S::HD / 4) + c] = y;
+    if (c == 0) a.part_ml[which * S::BM + r] = make_float2(top, l);
+    return;
+  }
+  const int G = a.n_heads / a.n_kv;
+  const long gr = (long)tile * w.step + r;
+  const int j = (int)(gr / G), h = kvh * G + (int)(gr % G);
+  // (A row that saw nothing has l = 0 and y = 0; NaN stays.)
+  const float inv = l == 0.f ? 1.f : 1.f / l;
+  T *out = static_cast<T *>(a.out) + (w.b + j) * a.o_ts + h * a.o_hs + 4 * c;
+  Pack<T, 4> t;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) t.v[e] = from_f32<T>(y[e] * inv);
+  if (4 * c + 4 <= a.hd) {
+    *reinterpret_cast<Pack<T, 4> *>(out) = t;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (4 * c + e < a.hd) out[e] = t.v[e];
+  }
+  if (c == 0 && a.lse)
+    a.lse[(long)(w.b + j) * a.n_heads + h] =
+        l == 0.f ? -INFINITY : (top + __builtin_log2f(l)) * 0.69314718055994531f;
+}
+
+// An item's rows stored (put_row). Waves along the keys join their shares first, in the
+// ring's two stages.
 template <class S>
 __device__ __forceinline__ void store_rows(const TreeAttnArgs &a, const Work &w, int kvh, int tile,
-                                           Rows<S> &R, u32x4 *lds0, u32x4 *lds1, float2 *ml, long which,
-                                           const int *met_odd, int from, int to) {
-  typedef typename S::T T;
+                                           Rows<S> &R, u32x4 *lds0, u32x4 *lds1, float2 *ml,
+                                           long which, const int *met_odd, int from, int to) {
   const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4;
   const int wm = (tid >> 6) % S::WM, wk = (tid >> 6) / S::WM;
   const int G = a.n_heads / a.n_kv;
-  __syncthreads();  // the ring is free
+  const int rows = (int)min((long)w.step, (long)w.n * G - (long)tile * w.step);
   const int last = min(to, w.keys);
+  __syncthreads();  // the ring is free, and met_odd what it will be
+  const bool odd = *met_odd;
 #pragma unroll
-  for (int rt = 0; rt < S::RT; ++rt) {
-    R.l[rt] = over_groups_sum(R.l[rt]);
-    if (g4 == 0)
-      ml[wk * S::BM + (wm * S::RT + rt) * 16 + lane] = make_float2(R.m[rt], R.l[rt]);
-  }
-  __syncthreads();
-  // (The join takes both stages.)
-  const auto o = [&](int i) -> f32x4 & {
-    u32x4 *at = i < 2 * S::TILE ? lds0 + i : lds1 + (i - 2 * S::TILE);
-    return *reinterpret_cast<f32x4 *>(at);
-  };
+  for (int rt = 0; rt < S::RT; ++rt) R.l[rt] = over_groups_sum(R.l[rt]);
+  if constexpr (S::WK == 1) {
 #pragma unroll
-  for (int rt = 0; rt < S::RT; ++rt) {
-    const int r = (wm * S::RT + rt) * 16 + (lane & 15);
-    float top = -INFINITY;
+    for (int rt = 0; rt < S::RT; ++rt) {
+      const int r = (wm * S::RT + rt) * 16 + (lane & 15);
+      if (r >= rows) continue;
 #pragma unroll
-    for (int i = 0; i < S::WK; ++i) top = fmaxf(top, ml[i * S::BM + r].x);
-    const float f = R.m[rt] == -INFINITY ? (top == -INFINITY ? 1.f : 0.f)
-                                         : __builtin_amdgcn_exp2f(R.m[rt] - top);
-#pragma unroll
-    for (int d = 0; d < S::HD / 16; ++d) o(join_at<S>(wk, r, d * 4 + g4)) = R.o[rt][d] * f;
-  }
-  __syncthreads();
-  for (int i = tid; i < S::BM * (S::HD / 4); i += kTreeThreads) {
-    const int r = i / (S::HD / 4), c = i % (S::HD / 4);
-    const long gr = (long)tile * S::BM + r;
-    if (gr >= (long)w.n * G) break;
-    float top = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int k = 0; k < S::WK; ++k) top = fmaxf(top, ml[k * S::BM + r].x);
-    f32x4 y{};
-#pragma unroll
-    for (int k = 0; k < S::WK; ++k) {
-      const float2 x = ml[k * S::BM + r];
-      l += x.x == -INFINITY ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - top);
-      y += o(join_at<S>(k, r, c));
+      for (int d = 0; d < S::HD / 16; ++d) {
+        f32x4 y = R.o[rt][d];
+        if (odd) y += odd_values<S>(a, w, kvh, R.j[rt], d * 4 + g4, from, last);
+        put_row<S>(a, w, kvh, tile, r, d * 4 + g4, y, R.l[rt], R.m[rt], which);
+      }
     }
-    const int j = (int)gr / G, h = kvh * G + (int)gr % G;
-    if (*met_odd) y += odd_values<S>(a, w, kvh, j, c, from, last);
-    if (which >= 0) {
-      reinterpret_cast<f32x4 *>(a.part)[(which * S::BM + r) * (S::HD / 4) + c] = y;
-      if (c == 0) a.part_ml[which * S::BM + r] = make_float2(top, l);
-      continue;
-    }
-    // (A row that saw nothing has l = 0 and y = 0; NaN stays.)
-    const float inv = l == 0.f ? 1.f : 1.f / l;
-    T *out = static_cast<T *>(a.out) + (w.b + j) * a.o_ts + h * a.o_hs + 4 * c;
-    Pack<T, 4> t;
+  } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) t.v[e] = from_f32<T>(y[e] * inv);
-    if (4 * c + 4 <= a.hd) {
-      *reinterpret_cast<Pack<T, 4> *>(out) = t;
-    } else {
+    for (int rt = 0; rt < S::RT; ++rt)
+      if (g4 == 0)
+        ml[wk * S::BM + (wm * S::RT + rt) * 16 + lane] = make_float2(R.m[rt], R.l[rt]);
+    __syncthreads();
+    // Float chunk c (of HD / 4) of row r, wave k along the keys.
+    const auto at = [&](int k, int r, int c) -> f32x4 & {
+      const int i = (k * S::BM + r) * (S::HD / 4) + (c ^ (r & 15));
+      u32x4 *p = i < 2 * S::TILE ? lds0 + i : lds1 + (i - 2 * S::TILE);
+      return *reinterpret_cast<f32x4 *>(p);
+    };
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (4 * c + e < a.hd) out[e] = t.v[e];
+    for (int rt = 0; rt < S::RT; ++rt) {
+      const int r = (wm * S::RT + rt) * 16 + (lane & 15);
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < S::WK; ++i) top = fmaxf(top, ml[i * S::BM + r].x);
+      const float f = R.m[rt] == -INFINITY ? (top == -INFINITY ? 1.f : 0.f)
+                                           : __builtin_amdgcn_exp2f(R.m[rt] - top);
+#pragma unroll
+      for (int d = 0; d < S::HD / 16; ++d) at(wk, r, d * 4 + g4) = R.o[rt][d] * f;
     }
-    if (c == 0 && a.lse)
-      a.lse[(long)(w.b + j) * a.n_heads + h] =
-          l == 0.f ? -INFINITY : (top + __builtin_log2f(l)) * 0.69314718055994531f;
+    __syncthreads();
+    for (int i = tid; i < rows * (S::HD / 4); i += S::NT) {
+      const int r = i / (S::HD / 4), c = i % (S::HD / 4);
+      float top = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int k = 0; k < S::WK; ++k) top = fmaxf(top, ml[k * S::BM + r].x);
+      f32x4 y{};
+#pragma unroll
+      for (int k = 0; k < S::WK; ++k) {
+        const float2 x = ml[k * S::BM + r];
+        l += x.x == -INFINITY ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - top);
+        y += at(k, r, c);
+      }
+      if (odd) y += odd_values<S>(a, w, kvh, (int)(((long)tile * w.step + r) / G), c, from, last);
+      put_row<S>(a, w, kvh, tile, r, c, y, l, top, which);
+    }
   }
   __syncthreads();  // LDS may be filled again
 }
 
 template <class S, bool VEC>
-__global__ __launch_bounds__(kTreeThreads, S::PER_CU) void k_tree_attn(TreeAttnArgs a) {
+__global__ __launch_bounds__(S::NT, S::PER_CU) void k_tree_attn(TreeAttnArgs a) {
   __shared__ u32x4 ring0[2 * S::TILE], ring1[2 * S::TILE];
   __shared__ float2 ml[S::WK * S::BM];
-  __shared__ long sums[kTreeThreads / 64], found[2];
+  __shared__ long sums[S::NT / 64], found[2];
   __shared__ int met_odd;
   if (threadIdx.x == 0) met_odd = 0;
   long total;
-  const long first = block_scan(my_units<S>(a), sums, total);
-  const int eff = blocks_used(total, a.groups);
+  const long first = block_scan<S::NT>(my_cost<S>(a), sums, total);
+  const int eff = blocks_used<S>(total, a.groups);
   const int g = logical_block(blockIdx.x, eff, a.groups);
   if (total == 0 || g >= eff) {
     if (threadIdx.x == 0) a.joins[g].last = -1;
@@ -741,16 +772,17 @@ __global__ __launch_bounds__(kTreeThreads, S::PER_CU) void k_tree_attn(TreeAttnA
   const int G = a.n_heads / a.n_kv;
   Rows<S> R;
   for (;;) {
-    const long local = at - w.base;
-    const int item = __builtin_amdgcn_readfirstlane((int)(local / w.nb));
-    const int b0 = __builtin_amdgcn_readfirstlane((int)(local - (long)item * w.nb));
+    const long local = at - w.base, each = (long)w.nb * w.cost;
+    const int item = __builtin_amdgcn_readfirstlane((int)(local / each));
+    const long off = local - item * each, off_end = min(each, off + (end - at));
+    const int b0 = __builtin_amdgcn_readfirstlane((int)((off + w.cost - 1) / w.cost));
+    const int b1 = __builtin_amdgcn_readfirstlane((int)((off_end + w.cost - 1) / w.cost));
     const int kvh = item / w.tiles, tile = item - kvh * w.tiles;
-    const int b1 = (int)min((long)w.nb, b0 + (end - at));
     // Without masks, key tiles past the last row's own position are seen by none.
-    const int last = min(w.n - 1, (int)min((long)INT32_MAX, ((long)(tile + 1) * S::BM - 1) / G));
+    const int last = (int)min((long)w.n - 1, ((long)(tile + 1) * w.step - 1) / G);
     const long upto = a.mask ? w.keys : min((long)w.keys, (long)w.len + last + 1);
     const int b2 = min(b1, (int)((upto + S::BK - 1) / S::BK));
-    load_rows<S>(a, w, kvh, tile, R);
+    if (b0 < b1) load_rows<S>(a, w, kvh, tile, R);
     if (b0 < b2) {
       int32_t page[S::NL];
       load_pages<S>(a, w, b0 * S::BK, page);
@@ -795,44 +827,49 @@ __global__ __launch_bounds__(kTreeThreads, S::PER_CU) void k_tree_attn(TreeAttnA
           step(draft, b, ring0, ring1);
       }
     }
-    const bool whole = b0 == 0 && b1 == w.nb;
-    store_rows<S>(a, w, kvh, tile, R, ring0, ring1, ml, whole ? -1 : 2L * g + (b0 == 0), &met_odd,
-                  b0 * S::BK, b2 * S::BK);
-    if (threadIdx.x == 0) met_odd = 0;
-    at += b1 - b0;
+    if (b0 < b1) {
+      const bool whole = b0 == 0 && b1 == w.nb;
+      store_rows<S>(a, w, kvh, tile, R, ring0, ring1, ml, whole ? -1 : 2L * g + (b0 == 0),
+                    &met_odd, b0 * S::BK, b2 * S::BK);
+      if (threadIdx.x == 0) met_odd = 0;
+    }
+    at += off_end - off;
     if (at >= end) {
-      // An item that begins here and ends in another block is joined afterwards.
+      // An item that begins here and ends in another block is joined afterwards, with the
+      // blocks up to that in which its last key tile begins.
       if (threadIdx.x == 0) {
         int last = -1;
-        if (b0 == 0 && b1 < w.nb) {
-          const long iend = w.base + (long)item * w.nb + w.nb;
-          for (last = g + 1; total * (last + 1) / eff < iend;) ++last;
+        if (b0 == 0 && b1 > 0 && b1 < w.nb) {
+          const long begins = w.base + (item + 1) * each - w.cost;
+          for (last = g + 1; total * (last + 1) / eff <= begins;) ++last;
         }
-        a.joins[g] = {w.b, w.n, kvh, tile, last};
+        a.joins[g] = {w.b, w.n, kvh, tile, w.step, last};
       }
       return;
     }
-    while (at >= w.base + work_units(a, w)) {
-      const long base = w.base + work_units(a, w);
+    while (at >= w.base + work_cost(a, w)) {
+      const long base = w.base + work_cost(a, w);
       work_of<S>(a, w.s + 1, w);
       w.base = base;
     }
   }
 }
 
+constexpr int kJoinThreads = 256;
+
 // Joins the items that more than one block has walked. Block (x, y): the item that
 // attention block x begins and another ends (each has one at most), rows y RB .. + RB.
 template <class S>
-__global__ __launch_bounds__(kTreeThreads) void k_tree_join(TreeAttnArgs a) {
+__global__ __launch_bounds__(kJoinThreads) void k_tree_join(TreeAttnArgs a) {
   typedef typename S::T T;
-  constexpr int CF = S::HD / 4, RB = kTreeThreads / CF;
+  constexpr int CF = S::HD / 4, RB = kJoinThreads / CF;
   const int g = blockIdx.x;
   const TreeJoin i = a.joins[g];
   if (i.last < 0) return;
   const int G = a.n_heads / a.n_kv;
   const int r = blockIdx.y * RB + threadIdx.x / CF, c = threadIdx.x % CF;
-  const long gr = (long)i.tile * S::BM + r;
-  if (gr >= (long)i.n * G) return;
+  const long gr = (long)i.tile * i.step + r;
+  if (r >= i.step || gr >= (long)i.n * G) return;
   const auto at = [&](int b) { return (2L * b + (b == g)) * S::BM + r; };
   float top = -INFINITY, l = 0.f;
   for (int b = g; b <= i.last; ++b) top = fmaxf(top, a.part_ml[at(b)].x);
@@ -846,7 +883,7 @@ __global__ __launch_bounds__(kTreeThreads) void k_tree_join(TreeAttnArgs a) {
     l += x.y * f;
     y += o * f;
   }
-  const int j = (int)gr / G, h = i.kvh * G + (int)gr % G;
+  const int j = (int)(gr / G), h = i.kvh * G + (int)(gr % G);
   const float inv = l == 0.f ? 1.f : 1.f / l;
   T *out = static_cast<T *>(a.out) + (i.b + j) * a.o_ts + h * a.o_hs + 4 * c;
 #pragma unroll
@@ -876,11 +913,11 @@ hipError_t launch_tree_shape(TreeAttnArgs a, void *ws, hipStream_t s) {
   a.part = static_cast<float *>(ws);
   a.part_ml = reinterpret_cast<float2 *>(a.part + (size_t)2 * a.groups * S::BM * S::HD);
   a.joins = reinterpret_cast<TreeJoin *>(a.part_ml + (size_t)2 * a.groups * S::BM);
-  k_tree_attn<S, VEC><<<a.groups, kTreeThreads, 0, s>>>(a);
+  k_tree_attn<S, VEC><<<a.groups, S::NT, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  constexpr int RB = kTreeThreads / (S::HD / 4);
-  k_tree_join<S><<<dim3(a.groups, (S::BM + RB - 1) / RB), kTreeThreads, 0, s>>>(a);
+  constexpr int RB = kJoinThreads / (S::HD / 4);
+  k_tree_join<S><<<dim3(a.groups, (S::BM + RB - 1) / RB), kJoinThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -889,23 +926,27 @@ inline int tree_rows_of(int T, int n_seqs, int n_heads, int n_kv) {
 }
 
 // Rows of a block by the rows that a mean sequence has for a key head.
-inline int tree_block_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+inline int tree_block_rows(int rows) {
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+}
 
 template <typename T, int HD>
 hipError_t launch_tree_type(const TreeAttnArgs &a, void *ws, hipStream_t s) {
   constexpr bool wide = sizeof(T) == 4 && HD == 256;  // (its tiles of 32 keys feed two waves)
   if (!tree_aligned<T>(a))
-    return launch_tree_shape<TreeShape<T, HD, wide ? 1 : 2, wide ? 2 : 1>, false>(a, ws, s);
+    return launch_tree_shape<TreeShape<T, HD, 4, wide ? 1 : 2, wide ? 2 : 1>, false>(a, ws, s);
   switch (tree_block_rows(tree_rows_of(a.T, a.pages.n_seqs, a.n_heads, a.n_kv))) {
     case 16:
-      if constexpr (!wide) return launch_tree_shape<TreeShape<T, HD, 1, 1>, true>(a, ws, s);
+      if constexpr (!wide) return launch_tree_shape<TreeShape<T, HD, 4, 1, 1>, true>(a, ws, s);
       [[fallthrough]];
     case 32:
-      return launch_tree_shape<TreeShape<T, HD, wide ? 1 : 2, wide ? 2 : 1>, true>(a, ws, s);
+      return launch_tree_shape<TreeShape<T, HD, 4, wide ? 1 : 2, wide ? 2 : 1>, true>(a, ws, s);
     case 64:
-      return launch_tree_shape<TreeShape<T, HD, 2, 2>, true>(a, ws, s);
+      return launch_tree_shape<TreeShape<T, HD, 4, 2, 2>, true>(a, ws, s);
+    case 128:
+      return launch_tree_shape<TreeShape<T, HD, 4, 2, 4>, true>(a, ws, s);
     default:
-      return launch_tree_shape<TreeShape<T, HD, 2, 4>, true>(a, ws, s);
+      return launch_tree_shape<TreeShape<T, HD, 8, HD == 256 ? 1 : 2, 8>, true>(a, ws, s);
   }
 }
 
