@@ -302,7 +302,11 @@ struct TreeAttnArgs {
   int mask_words;
   float scale_log2;  // |scale| log2(e), not 0
   int negate;        // scale < 0: queries change their sign
-  // Set by the launcher: partial results, what joins them, blocks of the grid.
+  // Set by the launcher: query heads a key head and r / group as a product and a shift
+  // (r < 2^31), partial results, what joins them, blocks of the grid.
+  int group;
+  uint32_t group_mul;
+  int group_shift;
   float *part;
   float2 *part_ml;
   struct TreeJoin *joins;

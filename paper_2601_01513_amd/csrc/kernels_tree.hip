@@ -96,7 +96,14 @@ size_t tree_attention_workspace_bytes(int hd, int T, int n_seqs, int n_heads, in
   return (size_t)kTreeGroups * (2 * rows * (HD * sizeof(float) + sizeof(float2)) + sizeof(TreeJoin));
 }
 
-hipError_t launch_tree_attention(const TreeAttnArgs &a, int dtype, void *ws, hipStream_t s) {
+hipError_t launch_tree_attention(const TreeAttnArgs &given, int dtype, void *ws, hipStream_t s) {
+  TreeAttnArgs a = given;
+  a.group = a.n_heads / a.n_kv;
+  // With 2^b >= group, ceil(2^(31 + b) / group) times r < 2^31 is off by less than 2^(31 + b) / group.
+  int b = 0;
+  while (1 << b < a.group) ++b;
+  a.group_shift = 31 + b;
+  a.group_mul = (uint32_t)(((1ull << a.group_shift) + a.group - 1) / a.group);
   if (dtype == 0) return launch_tree_f32(a, ws, s);
   if (dtype == 1) return launch_tree_bf16(a, ws, s);
   return launch_tree_f16(a, ws, s);

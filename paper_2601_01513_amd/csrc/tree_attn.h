@@ -100,7 +100,7 @@ struct TreeShape {
   // Blocks a CU: by LDS, and two waves a SIMD.
   static constexpr int PER_CU = NW == 4 && 4 * TILE * 16 <= 72 << 10 ? 2 : 1;
   static_assert(KW >= 1 && NL >= 1, "each wave has keys, each thread a load");
-  static_assert(WK == 1 || WK * BM * HD * 4 <= 4 * TILE * 16, "waves along the keys join in the ring");
+  static_assert(NW * 16 * HD * 4 <= 4 * TILE * 16, "a row group of each wave fits the ring");
 };
 
 // LDS gives 256 bytes to 16 lanes at once: chunk c of row r lies where 16 rows' chunks
@@ -111,12 +111,9 @@ __device__ __forceinline__ int swz(int r) {
 }
 
 // The walk of all blocks over all work. An item is (sequence, key head, tile of rows),
-// tiles innermost, the sequence's rows shared evenly by its tiles; its key tiles cost what
-// they take: loads and waits about as much as kTileCost of the waves that have rows.
-// Block g of `eff` takes the key tiles that begin in [total g / eff, total (g + 1) / eff)
-// of the summed costs.
-constexpr int kTileCost = 3;
-
+// tiles innermost, the sequence's rows shared evenly by its tiles, a tile's 16-row groups
+// by the waves. Its key tiles cost what they take, about 1 / 4 + the most groups that a
+// SIMD has (2.33 us for 3, 3.09 for 4), here in quarters. Block g takes the key tiles that begin in [g per, (g + 1) per) of the summed costs.
 struct Work {
   int s, b, n;      // a sequence and its rows
   int len, keys;    // positions before the draft, and with it
@@ -132,17 +129,38 @@ __device__ __forceinline__ void work_of(const TreeAttnArgs &a, int s, Work &w) {
   w.s = s;
   w.n = e - w.b;
   w.len = seq_len(a.pages, s);
-  w.keys = (int)min((long)w.len + w.n, (long)seq_room(a.pages, s));
-  const long rows = (long)w.n * (a.n_heads / a.n_kv);
-  w.tiles = (int)((rows + S::BM - 1) / S::BM);
+  w.keys = min(w.len + w.n, seq_room(a.pages, s));
+  const int rows = w.n * a.group;
+  w.tiles = (rows + S::BM - 1) / S::BM;
   // (The least multiple of 16 that `tiles` of cover the rows.)
-  w.step = w.tiles ? ((int)((rows + w.tiles - 1) / w.tiles) + 15) / 16 * 16 : 16;
-  w.nb = max(1, (int)(((long)w.keys + S::BK - 1) / S::BK));
-  w.cost = kTileCost + (w.step + 16 * S::RT - 1) / (16 * S::RT);
+  w.step = w.tiles <= 1 ? max(16, (rows + 15) / 16 * 16)
+                        : ((rows + w.tiles - 1) / w.tiles + 15) / 16 * 16;
+  w.nb = max(1, (w.keys + S::BK - 1) / S::BK);
+  w.cost = 1 + (w.step / 16 * S::WK + 3) / 4 * 4;
 }
 
 __device__ __forceinline__ long work_cost(const TreeAttnArgs &a, const Work &w) {
-  return (long)a.n_kv * w.tiles * w.nb * w.cost;
+  return (long)a.n_kv * w.tiles * (w.nb * w.cost);
+}
+
+// a / b, 0 <= a < 2^52, 0 < b < 2^31, by a reciprocal put right (a 64-bit division is 1 KB
+// of code, and a kernel's first steps wait for their code as well).
+__device__ __forceinline__ int quotient(long a, int b) {
+  long q = (long)((double)a * __builtin_amdgcn_rcp((double)b));
+  long r = a - q * b;
+  while (r < 0) {
+    --q;
+    r += b;
+  }
+  while (r >= b) {
+    ++q;
+    r -= b;
+  }
+  return (int)q;
+}
+// r / group.
+__device__ __forceinline__ int token_of(const TreeAttnArgs &a, int r) {
+  return (int)(((uint64_t)(uint32_t)r * a.group_mul) >> a.group_shift);
 }
 
 // Exclusive prefix sum over a block's NT threads, and the total.
@@ -168,55 +186,118 @@ __device__ __forceinline__ long block_scan(long mine, long *sums, long &total) {
   return before + v - mine;
 }
 
+__device__ __forceinline__ long lane_value(long v, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int)v, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
+  return (long)((uint64_t)hi << 32 | lo);
+}
+
+// Inclusive prefix sum over the lanes of a wave (wave_scan's steps).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ long scan_step(long v) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xF, false);
+  return v + (long)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ long wave_scan_long(long v) {
+  v = scan_step<0x111, 0xF>(v);
+  v = scan_step<0x112, 0xF>(v);
+  v = scan_step<0x114, 0xF>(v);
+  v = scan_step<0x118, 0xF>(v);
+  v = scan_step<0x142, 0xA>(v);
+  return scan_step<0x143, 0xC>(v);
+}
+
+// The sequences' costs in order. Up to 64 sequences every wave holds them all, one a lane;
+// more are held by the block, runs of them a thread, and read again where they are needed.
+template <class S>
+struct Plan {
+  Work mine;   // a lane's sequence
+  long cost, upto;
+  long total, first;
+  bool few;
+
+  __device__ __forceinline__ Plan(const TreeAttnArgs &a, long *sums) {
+    few = a.pages.n_seqs <= 64;
+    if (few) {
+      const int lane = threadIdx.x & 63;
+      cost = 0;
+      if (lane < a.pages.n_seqs) {
+        work_of<S>(a, lane, mine);
+        cost = work_cost(a, mine);
+      }
+      upto = wave_scan_long(cost);
+      total = lane_value(upto, 63);
+    } else {
+      const int per = (a.pages.n_seqs + S::NT - 1) / S::NT;
+      cost = 0;
+      for (int i = 0; i < per; ++i) {
+        const int s = threadIdx.x * per + i;
+        if (s >= a.pages.n_seqs) break;
+        work_of<S>(a, s, mine);
+        cost += work_cost(a, mine);
+      }
+      first = block_scan<S::NT>(cost, sums, total);
+      total = lane_value(total, 0);
+    }
+  }
+
+  // The sequence in whose cost `at` lies.
+  __device__ __forceinline__ void find(const TreeAttnArgs &a, long at, long *found, Work &w) {
+    if (few) {
+      const int s = __builtin_ctzll(__ballot(at < upto && at >= upto - cost));
+      const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, s); };
+      w = {s, of(mine.b), of(mine.n), of(mine.len), of(mine.keys), of(mine.tiles), of(mine.step),
+           of(mine.nb), of(mine.cost), lane_value(upto - cost, s)};
+      return;
+    }
+    const int per = (a.pages.n_seqs + S::NT - 1) / S::NT;
+    const int s0 = threadIdx.x * per;
+    long base = first;
+    if (at >= first && at < first + cost) {
+      for (int i = 0; i < per && s0 + i < a.pages.n_seqs; ++i) {
+        Work x;
+        work_of<S>(a, s0 + i, x);
+        const long u = work_cost(a, x);
+        if (at >= base && at < base + u) {
+          found[0] = s0 + i;
+          found[1] = base;
+        }
+        base += u;
+      }
+    }
+    __syncthreads();
+    const int s = __builtin_amdgcn_readfirstlane((int)found[0]);
+    work_of<S>(a, s, w);
+    w.base = lane_value(found[1], 0);
+    __syncthreads();
+  }
+
+  // From a sequence's end, `at`, to the next that has rows.
+  __device__ __forceinline__ void next(const TreeAttnArgs &a, long at, Work &w) {
+    if (few) {
+      find(a, at, nullptr, w);
+      return;
+    }
+    while (at >= w.base + work_cost(a, w)) {
+      const long base = w.base + work_cost(a, w);
+      work_of<S>(a, w.s + 1, w);
+      w.base = base;
+    }
+  }
+};
+
 // A block takes two of the dearest key tiles at least (one that lies between an item's
 // first and last block then has one of its tiles).
 template <class S>
 __device__ __forceinline__ int blocks_used(long total, int groups) {
-  constexpr int least = 2 * (kTileCost + S::WM);
+  constexpr int least = 2 * (1 + S::RT * S::NW / 4 * 4);
   return (int)max(1L, min(total / least, (long)groups));
 }
 // Blocks of one XCD take neighbouring ranges (tiles that share keys), unless there are
 // fewer of them than the grid has.
 __device__ __forceinline__ int logical_block(int b, int eff, int groups) {
   return eff < groups ? b : b % 8 * (groups / 8) + b / 8;
-}
-
-// Finds the sequence that holds unit `at` (and its Work): every thread gets it.
-template <class S>
-__device__ __forceinline__ void find_unit(const TreeAttnArgs &a, long first, long at, long *found,
-                                          Work &w) {
-  const int per = (a.pages.n_seqs + S::NT - 1) / S::NT;
-  const int s0 = threadIdx.x * per;
-  long base = first;
-  for (int i = 0; i < per && s0 + i < a.pages.n_seqs; ++i) {
-    Work x;
-    work_of<S>(a, s0 + i, x);
-    const long u = work_cost(a, x);
-    if (at >= base && at < base + u) {
-      found[0] = s0 + i;
-      found[1] = base;
-    }
-    base += u;
-  }
-  __syncthreads();
-  const int s = __builtin_amdgcn_readfirstlane((int)found[0]);
-  work_of<S>(a, s, w);
-  w.base = found[1];
-  __syncthreads();
-}
-
-template <class S>
-__device__ __forceinline__ long my_cost(const TreeAttnArgs &a) {
-  const int per = (a.pages.n_seqs + S::NT - 1) / S::NT;
-  long u = 0;
-  for (int i = 0; i < per; ++i) {
-    const int s = threadIdx.x * per + i;
-    if (s >= a.pages.n_seqs) break;
-    Work x;
-    work_of<S>(a, s, x);
-    u += work_cost(a, x);
-  }
-  return u;
 }
 
 __device__ __forceinline__ float over_groups_max(float x) {
@@ -240,7 +321,7 @@ struct Rows {
   Q q[S::RT][QN];
   int j[S::RT];         // row of the draft
   float m[S::RT], l[S::RT];
-  bool any;             // whether the wave has a row
+  int n;                // of the wave's row groups, those that have rows
   f32x4 o[S::RT][S::HD / 16];
 };
 
@@ -249,43 +330,59 @@ __device__ __forceinline__ T load_part(const T *p, int i, int hd) {
   return i < hd ? p[i] : T(0.f);
 }
 
+// Row groups of 16 of the item's `rows` that wave wm of S::WM has: n of them from first on.
+struct Groups {
+  int first, n;
+};
+template <class S>
+__device__ __forceinline__ Groups groups_of(int rows, int wm) {
+  const int all = (rows + 15) / 16, each = all / S::WM, more = all % S::WM;
+  return {wm * each + min(wm, more), each + (wm < more)};
+}
+
+__device__ __forceinline__ int item_rows(const TreeAttnArgs &a, const Work &w, int tile) {
+  return min(w.step, w.n * a.group - tile * w.step);
+}
+
 template <class S>
 __device__ __forceinline__ void load_rows(const TreeAttnArgs &a, const Work &w, int kvh, int tile,
                                           Rows<S> &R) {
   typedef typename S::T T;
+  constexpr int V = 16 / sizeof(T);  // elements a load
+  typedef Pack<T, V> P;
   const int lane = threadIdx.x & 63, g4 = lane >> 4, wm = (threadIdx.x >> 6) % S::WM;
-  const int G = a.n_heads / a.n_kv;
-  const int rows = (int)min((long)w.step, (long)w.n * G - (long)tile * w.step);
-  R.any = __builtin_amdgcn_readfirstlane(wm * S::RT * 16 < rows);
+  const int rows = item_rows(a, w, tile);
+  const Groups mine = groups_of<S>(rows, wm);
+  R.n = __builtin_amdgcn_readfirstlane(mine.n);
 #pragma unroll
   for (int rt = 0; rt < S::RT; ++rt) {
-    const int r = (wm * S::RT + rt) * 16 + (lane & 15);
-    const long rc = r < rows ? (long)tile * w.step + r : 0;
-    R.j[rt] = (int)(rc / G);
+    const int r = (mine.first + rt) * 16 + (lane & 15);
+    const int rc = tile * w.step + (rt < mine.n && r < rows ? r : 0);
+    R.j[rt] = token_of(a, rc);
     R.m[rt] = -INFINITY;
     R.l[rt] = 0.f;
     const T *q = static_cast<const T *>(a.q) + (w.b + R.j[rt]) * a.q_ts +
-                 (long)(kvh * G + (int)(rc % G)) * a.q_hs;
-    constexpr int V = S::F32 ? 4 : 8;
+                 (long)(kvh * a.group + rc - R.j[rt] * a.group) * a.q_hs;
+    P x[S::CH / 4];
+    if (a.hd == S::HD) {
 #pragma unroll
-    for (int c = 0; c < Rows<S>::QN / (S::F32 ? 4 : 1); ++c) {
-      const int at = c * 4 * V + g4 * V;
-      Pack<T, V> x;
-      if (at + V <= a.hd) {
-        x = *reinterpret_cast<const Pack<T, V> *>(q + at);
-      } else {
+      for (int c = 0; c < S::CH / 4; ++c)
+        x[c] = *reinterpret_cast<const P *>(q + (4 * c + g4) * V);
+    } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) x.v[i] = load_part(q, at + i, a.hd);
-      }
-      if (a.negate) {
+      for (int c = 0; c < S::CH / 4; ++c)
 #pragma unroll
-        for (int i = 0; i < V; ++i) x.v[i] = -x.v[i];
-      }
+        for (int i = 0; i < V; ++i) x[c].v[i] = load_part(q, (4 * c + g4) * V + i, a.hd);
+    }
+#pragma unroll
+    for (int c = 0; c < S::CH / 4; ++c) {
+      u32x4 bits = __builtin_bit_cast(u32x4, x[c]);
+      if (a.negate) bits ^= S::F32 ? 0x80000000u : 0x80008000u;
       if constexpr (S::F32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) R.q[rt][c * 4 + i] = x.v[i];
+        for (int i = 0; i < 4; ++i) R.q[rt][c * 4 + i] = __uint_as_float(bits[i]);
       } else {
-        R.q[rt][c] = __builtin_bit_cast(u32x4, x);
+        R.q[rt][c] = bits;
       }
     }
 #pragma unroll
@@ -293,23 +390,33 @@ __device__ __forceinline__ void load_rows(const TreeAttnArgs &a, const Work &w, 
   }
 }
 
+// The thread's number, of which the compiler knows nothing: what follows from it is worked
+// out again for each tile. Kept in registers over the loops it was spilled, and the
+// reloads stood ahead of the loads.
+__device__ __forceinline__ int thread_again() {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  return tid;
+}
+
 // Pages of the keys that a thread loads, of the tile at kb (past the keys: the last one's).
 template <class S>
 __device__ __forceinline__ void load_pages(const TreeAttnArgs &a, const Work &w, int kb,
                                            int32_t *page) {
   const int32_t *table = a.pages.table + w.s * a.pages.table_stride;
+  const int tid = thread_again();
 #pragma unroll
   for (int i = 0; i < S::NL; ++i) {
-    const int p = kb + (i * S::NT + (int)threadIdx.x) / S::CH;
+    const int p = kb + i * (S::NT / S::CH) + tid / S::CH;
     page[i] = table[min(p, w.keys - 1) >> a.pages.page_shift];
   }
 }
 
 // Chunk of the row that a thread's load i brings (it lands in chunk tid % CH of the row).
 template <class S>
-__device__ __forceinline__ int load_chunk(int i) {
+__device__ __forceinline__ int load_chunk(int tid, int i) {
   constexpr int STEP = S::NT / S::CH;  // rows from load to load
-  const int tid = threadIdx.x, c = (tid % S::CH) ^ swz<S::CH>(tid / S::CH);
+  const int c = (tid % S::CH) ^ swz<S::CH>(tid / S::CH);
   return S::CH >= 16 ? c ^ (i * STEP & 15) : c;
 }
 
@@ -320,13 +427,13 @@ template <class S, bool VEC>
 __device__ __forceinline__ void load_tile(const TreeAttnArgs &a, const Work &w, int kvh, int kb,
                                           const int32_t *page, u32x4 *stage) {
   typedef typename S::T T;
-  const int tid = threadIdx.x, shift = a.pages.page_shift;
+  const int tid = thread_again(), wave = threadIdx.x & ~63, shift = a.pages.page_shift;
   const T *k = static_cast<const T *>(a.k) + kvh * a.k_hs;
   const T *v = static_cast<const T *>(a.v) + kvh * a.v_hs;
   const bool all = kb + S::BK <= w.keys && a.hd == S::HD;
 #pragma unroll
   for (int i = 0; i < S::NL; ++i) {
-    const int r = i * (S::NT / S::CH) + tid / S::CH, p = kb + r, c = load_chunk<S>(i);
+    const int r = i * (S::NT / S::CH) + tid / S::CH, p = kb + r, c = load_chunk<S>(tid, i);
     const uint32_t pg = (uint32_t)page[i] < (uint32_t)a.pages.n_pages ? page[i] : 0;
     const uint32_t slot = pg << shift | ((uint32_t)p & ((1u << shift) - 1));
     if constexpr (VEC) {
@@ -335,7 +442,7 @@ __device__ __forceinline__ void load_tile(const TreeAttnArgs &a, const Work &w, 
       const char *vp = reinterpret_cast<const char *>(v) + c * 16 + (uint64_t)slot * vt;
       if (!all && (p >= w.keys || c * S::EC >= a.hd))
         kp = vp = reinterpret_cast<const char *>(&g_zeros);
-      u32x4 *to = stage + i * S::NT + (tid & ~63);
+      u32x4 *to = stage + i * S::NT + wave;
       __builtin_amdgcn_global_load_lds(kp, to, 16, 0, 0);
       __builtin_amdgcn_global_load_lds(vp, to + S::TILE, 16, 0, 0);
     } else {
@@ -421,24 +528,32 @@ __device__ __forceinline__ bool not_finite(T x) {
 template <class S>
 __device__ __forceinline__ bool clear_odd(u32x4 *vs, int context) {
   typedef typename S::T T;
-  bool any = false;
+  // (An exponent of ones carries into the sign's place.)
+  constexpr uint32_t MASK = S::F32 ? 0x7f800000u : std::is_same<T, bf16>::value ? 0x7f807f80u : 0x7c007c00u;
+  constexpr uint32_t ONE = S::F32 ? 0x00800000u : std::is_same<T, bf16>::value ? 0x00800080u : 0x04000400u;
+  constexpr uint32_t TOP = S::F32 ? 0x80000000u : 0x80008000u;
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < S::NL; ++i) {
+    const int n = i * S::NT + threadIdx.x;
+    const u32x4 x = vs[n];
+    uint32_t odd = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) odd |= ((x[e] & MASK) + ONE) & TOP;
+    any |= n / S::CH < context ? 0 : odd;
+  }
+  if (!__any(any != 0)) return false;
 #pragma unroll 1
   for (int i = 0; i < S::NL; ++i) {
     const int n = i * S::NT + threadIdx.x;
     if (n / S::CH < context) continue;
-    u32x4 *at = vs + n;
-    Pack<T, S::EC> x = __builtin_bit_cast(Pack<T, S::EC>, *at);
-    bool odd = false;
+    Pack<T, S::EC> x = __builtin_bit_cast(Pack<T, S::EC>, vs[n]);
 #pragma unroll
     for (int e = 0; e < S::EC; ++e)
-      if (not_finite(x.v[e])) {
-        x.v[e] = from_f32<T>(0.f);
-        odd = true;
-      }
-    if (odd) *at = __builtin_bit_cast(u32x4, x);
-    any |= odd;
+      if (not_finite(x.v[e])) x.v[e] = from_f32<T>(0.f);
+    vs[n] = __builtin_bit_cast(u32x4, x);
   }
-  return any;
+  return any != 0;
 }
 
 // Keeps the compiler from moving anything across: groups of LDS reads stay a group of
@@ -446,8 +561,36 @@ __device__ __forceinline__ bool clear_odd(u32x4 *vs, int context) {
 // product, and a tile waits for 28 of them).
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
-// One key tile against a wave's rows. DRAFT: the tile has keys past len.
-template <class S, bool DRAFT>
+// Bit 4 t + i: whether row j of the draft sees position p0 + 16 t + i, t < KW, i < 4.
+template <class S>
+__device__ __forceinline__ uint32_t seen_bits(const TreeAttnArgs &a, const Work &w, int j, int p0) {
+  uint32_t seen = 0;
+  const uint32_t *row = a.mask ? a.mask + (w.b + j) * a.mask_stride : nullptr;
+#pragma unroll
+  for (int t = 0; t < S::KW; ++t) {
+    const int p = p0 + 16 * t, d = p - w.len;  // (d < 0: the context)
+    uint32_t bits;
+    if (row) {
+      // Bits d .. d + 3 of the row's mask; past its words they are clear.
+      const int wd = max(d, 0) >> 5;
+      uint64_t v = wd < a.mask_words && p < w.keys ? row[wd] : 0;
+      if (wd + 1 < a.mask_words && p < w.keys) v |= (uint64_t)row[wd + 1] << 32;
+      bits = d >= 0 ? (uint32_t)(v >> (d & 31)) : d > -4 ? (uint32_t)(v << -d) : 0;
+    } else {
+      const int n = j - d + 1;  // positions d .. j
+      bits = n >= 4 ? 15 : n > 0 ? (1u << n) - 1 : 0;
+    }
+    const int room = w.keys - p;
+    if (room < 4) bits &= room > 0 ? (1u << room) - 1 : 0;
+    if (d < 0) bits |= d > -4 ? (1u << -d) - 1 : 15;
+    seen |= (bits & 15) << (4 * t);
+  }
+  return seen;
+}
+
+// One key tile against NR groups of a wave's rows. DRAFT: the tile has keys that not all
+// rows see.
+template <class S, bool DRAFT, int NR>
 __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, int kb,
                                           const u32x4 *st, Rows<S> &R) {
   typedef typename S::T T;
@@ -455,7 +598,18 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
   const int lane = threadIdx.x & 63, g4 = lane >> 4, wk = (threadIdx.x >> 6) / S::WM;
   const u32x4 *ks = st, *vs = st + S::TILE;
   const int key0 = wk * S::KW * 16;
-  f32x4 x[S::RT][S::KW];
+  // What a lane's rows see of its keys, bit 4 t + i (worked out before the products, which
+  // need the registers).
+  [[maybe_unused]] uint32_t seen[NR];
+  if constexpr (DRAFT) {
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) {
+      in_order();
+      seen[rt] = seen_bits<S>(a, w, R.j[rt], kb + key0 + 4 * g4);
+    }
+    in_order();
+  }
+  f32x4 x[NR][S::KW];
   constexpr int KC = S::CH / 4;  // 16-byte chunks a lane reads of a key tile
   const int k_at = key_offset<S>(), v_at = value_offset<S>();
   const auto read_keys = [&](int t, u32x4 *kf) {
@@ -471,11 +625,11 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
     if (t + 1 < S::KW) read_keys(t + 1, kf[(t + 1) & 1]);
     in_order();
 #pragma unroll
-    for (int rt = 0; rt < S::RT; ++rt) x[rt][t] = f32x4{};
+    for (int rt = 0; rt < NR; ++rt) x[rt][t] = f32x4{};
 #pragma unroll
     for (int c = 0; c < KC; ++c)
 #pragma unroll
-      for (int rt = 0; rt < S::RT; ++rt) {
+      for (int rt = 0; rt < NR; ++rt) {
         if constexpr (S::F32) {
           const f32x4 kv = __builtin_bit_cast(f32x4, kf[t & 1][c]);
 #pragma unroll
@@ -494,32 +648,16 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
   if constexpr (!S::F32) vf[0].read(vs, v_at, key0, 0);
   if constexpr (DRAFT) {
 #pragma unroll
-    for (int rt = 0; rt < S::RT; ++rt) {
-      const uint32_t *row = a.mask ? a.mask + (w.b + R.j[rt]) * a.mask_stride : nullptr;
+    for (int rt = 0; rt < NR; ++rt)
 #pragma unroll
-      for (int t = 0; t < S::KW; ++t) {
-        // Bits d0 .. d0 + 3 of the row's mask (past its words: clear; d0 < 0: the context).
-        const int p0 = kb + key0 + t * 16 + 4 * g4, d0 = p0 - w.len;
-        uint32_t bits = 0;
-        if (row) {
-          const int wd = max(d0, 0) >> 5;
-          uint64_t v = wd < a.mask_words && p0 < w.keys ? row[wd] : 0;
-          if (wd + 1 < a.mask_words && p0 < w.keys) v |= (uint64_t)row[wd + 1] << 32;
-          bits = d0 >= 0 ? (uint32_t)(v >> (d0 & 31)) : d0 > -4 ? (uint32_t)(v << -d0) : 0;
-        }
+      for (int t = 0; t < S::KW; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int d = d0 + i;
-          const bool drafted = row ? (bits >> i) & 1 : d <= R.j[rt];
-          const bool vis = d < 0 || (drafted && p0 + i < w.keys);
-          x[rt][t][i] = vis ? x[rt][t][i] : -INFINITY;
-        }
-      }
-    }
+        for (int i = 0; i < 4; ++i)
+          x[rt][t][i] = seen[rt] >> (4 * t + i) & 1 ? x[rt][t][i] : -INFINITY;
   }
   const float c = a.scale_log2;
 #pragma unroll
-  for (int rt = 0; rt < S::RT; ++rt) {
+  for (int rt = 0; rt < NR; ++rt) {
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < S::KW; ++t)
@@ -576,15 +714,15 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
         for (int d = 0; d < S::HD / 16; ++d) {
           const float v = *reinterpret_cast<const float *>(row + (v_at ^ (d * 64 ^ i * 16)));
 #pragma unroll
-          for (int rt = 0; rt < S::RT; ++rt) R.o[rt][d] = M::mul(v, x[rt][t][i], R.o[rt][d]);
+          for (int rt = 0; rt < NR; ++rt) R.o[rt][d] = M::mul(v, x[rt][t][i], R.o[rt][d]);
         }
       }
   } else {
     typedef typename M::x4 x4;
     typedef typename M::x8 x8;
-    x4 p[S::RT][S::KW];
+    x4 p[NR][S::KW];
 #pragma unroll
-    for (int rt = 0; rt < S::RT; ++rt)
+    for (int rt = 0; rt < NR; ++rt)
 #pragma unroll
       for (int t = 0; t < S::KW; ++t)
 #pragma unroll
@@ -602,7 +740,7 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
 #pragma unroll
         for (int t = 0; t < S::KW; t += 2)
 #pragma unroll
-          for (int rt = 0; rt < S::RT; ++rt) {
+          for (int rt = 0; rt < NR; ++rt) {
             if constexpr (S::KW == 1) {
               R.o[rt][d] = M::mul(v[0], p[rt][0], R.o[rt][d]);
             } else {
@@ -659,9 +797,7 @@ __device__ __forceinline__ void put_row(const TreeAttnArgs &a, const Work &w, in
     if (c == 0) a.part_ml[which * S::BM + r] = make_float2(top, l);
     return;
   }
-  const int G = a.n_heads / a.n_kv;
-  const long gr = (long)tile * w.step + r;
-  const int j = (int)(gr / G), h = kvh * G + (int)(gr % G);
+  const int gr = tile * w.step + r, j = token_of(a, gr), h = kvh * a.group + gr - j * a.group;
   // (A row that saw nothing has l = 0 and y = 0; NaN stays.)
   const float inv = l == 0.f ? 1.f : 1.f / l;
   T *out = static_cast<T *>(a.out) + (w.b + j) * a.o_ts + h * a.o_hs + 4 * c;
@@ -680,71 +816,58 @@ __device__ __forceinline__ void put_row(const TreeAttnArgs &a, const Work &w, in
         l == 0.f ? -INFINITY : (top + __builtin_log2f(l)) * 0.69314718055994531f;
 }
 
-// An item's rows stored (put_row). Waves along the keys join their shares first, in the
-// ring's two stages.
+// An item's rows stored (put_row), a group of each wave after the other, through the ring's
+// two stages: there the waves along the keys join their shares, and a loop stores whole
+// rows (unrolled from registers, the stores were 60 KB of code, met once a block).
 template <class S>
 __device__ __forceinline__ void store_rows(const TreeAttnArgs &a, const Work &w, int kvh, int tile,
                                            Rows<S> &R, u32x4 *lds0, u32x4 *lds1, float2 *ml,
                                            long which, const int *met_odd, int from, int to) {
-  const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4;
+  constexpr int CF = S::HD / 4, LR = S::WM * 16;  // float chunks of a row, rows a pass
+  const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, l = lane & 15;
   const int wm = (tid >> 6) % S::WM, wk = (tid >> 6) / S::WM;
-  const int G = a.n_heads / a.n_kv;
-  const int rows = (int)min((long)w.step, (long)w.n * G - (long)tile * w.step);
-  const int last = min(to, w.keys);
-  __syncthreads();  // the ring is free, and met_odd what it will be
-  const bool odd = *met_odd;
+  const int rows = item_rows(a, w, tile), last = min(to, w.keys);
+  // Float chunk c of row r of the pass, wave k along the keys.
+  const auto at = [&](int k, int r, int c) -> f32x4 & {
+    const int i = (k * LR + r) * CF + (c ^ (r & 15));
+    u32x4 *p = i < 2 * S::TILE ? lds0 + i : lds1 + (i - 2 * S::TILE);
+    return *reinterpret_cast<f32x4 *>(p);
+  };
 #pragma unroll
-  for (int rt = 0; rt < S::RT; ++rt) R.l[rt] = over_groups_sum(R.l[rt]);
-  if constexpr (S::WK == 1) {
-#pragma unroll
-    for (int rt = 0; rt < S::RT; ++rt) {
-      const int r = (wm * S::RT + rt) * 16 + (lane & 15);
-      if (r >= rows) continue;
-#pragma unroll
-      for (int d = 0; d < S::HD / 16; ++d) {
-        f32x4 y = R.o[rt][d];
-        if (odd) y += odd_values<S>(a, w, kvh, R.j[rt], d * 4 + g4, from, last);
-        put_row<S>(a, w, kvh, tile, r, d * 4 + g4, y, R.l[rt], R.m[rt], which);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int rt = 0; rt < S::RT; ++rt)
-      if (g4 == 0)
-        ml[wk * S::BM + (wm * S::RT + rt) * 16 + lane] = make_float2(R.m[rt], R.l[rt]);
-    __syncthreads();
-    // Float chunk c (of HD / 4) of row r, wave k along the keys.
-    const auto at = [&](int k, int r, int c) -> f32x4 & {
-      const int i = (k * S::BM + r) * (S::HD / 4) + (c ^ (r & 15));
-      u32x4 *p = i < 2 * S::TILE ? lds0 + i : lds1 + (i - 2 * S::TILE);
-      return *reinterpret_cast<f32x4 *>(p);
-    };
-#pragma unroll
-    for (int rt = 0; rt < S::RT; ++rt) {
-      const int r = (wm * S::RT + rt) * 16 + (lane & 15);
+  for (int rt = 0; rt < S::RT; ++rt) {
+    __syncthreads();  // the ring is free, and met_odd what it will be
+    const float sum = over_groups_sum(R.l[rt]);
+    if (g4 == 0) ml[wk * LR + wm * 16 + l] = make_float2(R.m[rt], sum);
+    float f = 1.f;
+    if constexpr (S::WK > 1) {
+      __syncthreads();
       float top = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < S::WK; ++i) top = fmaxf(top, ml[i * S::BM + r].x);
-      const float f = R.m[rt] == -INFINITY ? (top == -INFINITY ? 1.f : 0.f)
-                                           : __builtin_amdgcn_exp2f(R.m[rt] - top);
-#pragma unroll
-      for (int d = 0; d < S::HD / 16; ++d) at(wk, r, d * 4 + g4) = R.o[rt][d] * f;
+      for (int k = 0; k < S::WK; ++k) top = fmaxf(top, ml[k * LR + wm * 16 + l].x);
+      f = R.m[rt] == -INFINITY ? (top == -INFINITY ? 1.f : 0.f)
+                               : __builtin_amdgcn_exp2f(R.m[rt] - top);
     }
-    __syncthreads();
-    for (int i = tid; i < rows * (S::HD / 4); i += S::NT) {
-      const int r = i / (S::HD / 4), c = i % (S::HD / 4);
-      float top = -INFINITY, l = 0.f;
 #pragma unroll
-      for (int k = 0; k < S::WK; ++k) top = fmaxf(top, ml[k * S::BM + r].x);
+    for (int d = 0; d < S::HD / 16; ++d) at(wk, wm * 16 + l, d * 4 + g4) = R.o[rt][d] * f;
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < LR * CF; i += S::NT) {
+      const int p = i / CF, c = i % CF;
+      const Groups g = groups_of<S>(rows, p / 16);
+      const int r = (g.first + rt) * 16 + p % 16;
+      if (rt >= g.n || r >= rows) continue;
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < S::WK; ++k) top = fmaxf(top, ml[k * LR + p].x);
       f32x4 y{};
 #pragma unroll
       for (int k = 0; k < S::WK; ++k) {
-        const float2 x = ml[k * S::BM + r];
-        l += x.x == -INFINITY ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - top);
-        y += at(k, r, c);
+        const float2 x = ml[k * LR + p];
+        sum += S::WK == 1 || x.x == -INFINITY ? x.y : x.y * __builtin_amdgcn_exp2f(x.x - top);
+        y += at(k, p, c);
       }
-      if (odd) y += odd_values<S>(a, w, kvh, (int)(((long)tile * w.step + r) / G), c, from, last);
-      put_row<S>(a, w, kvh, tile, r, c, y, l, top, which);
+      if (*met_odd) y += odd_values<S>(a, w, kvh, token_of(a, tile * w.step + r), c, from, last);
+      put_row<S>(a, w, kvh, tile, r, c, y, sum, top, which);
     }
   }
   __syncthreads();  // LDS may be filled again
@@ -753,45 +876,52 @@ __device__ __forceinline__ void store_rows(const TreeAttnArgs &a, const Work &w,
 template <class S, bool VEC>
 __global__ __launch_bounds__(S::NT, S::PER_CU) void k_tree_attn(TreeAttnArgs a) {
   __shared__ u32x4 ring0[2 * S::TILE], ring1[2 * S::TILE];
-  __shared__ float2 ml[S::WK * S::BM];
+  __shared__ float2 ml[S::NW * 16];
   __shared__ long sums[S::NT / 64], found[2];
   __shared__ int met_odd;
   if (threadIdx.x == 0) met_odd = 0;
-  long total;
-  const long first = block_scan<S::NT>(my_cost<S>(a), sums, total);
+  Plan<S> plan(a, sums);
+  const long total = plan.total;
   const int eff = blocks_used<S>(total, a.groups);
   const int g = logical_block(blockIdx.x, eff, a.groups);
-  if (total == 0 || g >= eff) {
+  const long per = max(1, __builtin_amdgcn_readfirstlane(quotient(total + eff - 1, eff)));
+  long at = g * per;
+  const long end = min(total, at + per);
+  if (at >= end) {
     if (threadIdx.x == 0) a.joins[g].last = -1;
     return;
   }
-  long at = total * g / eff;
-  const long end = total * (g + 1) / eff;
   Work w;
-  find_unit<S>(a, first, at, found, w);
-  const int G = a.n_heads / a.n_kv;
+  plan.find(a, at, found, w);
   Rows<S> R;
   for (;;) {
-    const long local = at - w.base, each = (long)w.nb * w.cost;
-    const int item = __builtin_amdgcn_readfirstlane((int)(local / each));
-    const long off = local - item * each, off_end = min(each, off + (end - at));
-    const int b0 = __builtin_amdgcn_readfirstlane((int)((off + w.cost - 1) / w.cost));
-    const int b1 = __builtin_amdgcn_readfirstlane((int)((off_end + w.cost - 1) / w.cost));
-    const int kvh = item / w.tiles, tile = item - kvh * w.tiles;
+    const long local = at - w.base;
+    const int each = w.nb * w.cost;
+    const int item = __builtin_amdgcn_readfirstlane(quotient(local, each));
+    const int off = __builtin_amdgcn_readfirstlane((int)(local - (long)item * each));
+    const int off_end = __builtin_amdgcn_readfirstlane((int)min((long)each, off + (end - at)));
+    const int b0 = __builtin_amdgcn_readfirstlane(quotient(off + w.cost - 1, w.cost));
+    const int b1 = __builtin_amdgcn_readfirstlane(quotient(off_end + w.cost - 1, w.cost));
+    const int kvh = __builtin_amdgcn_readfirstlane(quotient(item, w.tiles));
+    const int tile = item - kvh * w.tiles;
     // Without masks, key tiles past the last row's own position are seen by none.
-    const int last = (int)min((long)w.n - 1, ((long)(tile + 1) * w.step - 1) / G);
-    const long upto = a.mask ? w.keys : min((long)w.keys, (long)w.len + last + 1);
-    const int b2 = min(b1, (int)((upto + S::BK - 1) / S::BK));
+    const int last = min(w.n * a.group, (tile + 1) * w.step) - 1;
+    const int upto = a.mask ? w.keys : min(w.keys, w.len + token_of(a, last) + 1);
+    const int b2 = min(b1, (upto + S::BK - 1) / S::BK);
+    // Tiles before `plain` are seen whole by every row.
+    const int all = a.mask ? w.len : min(w.keys, w.len + token_of(a, tile * w.step) + 1);
+    const int plain = min(b2, all / S::BK);
+    int32_t page[S::NL];
+    if (b0 < b2) load_pages<S>(a, w, b0 * S::BK, page);
     if (b0 < b1) load_rows<S>(a, w, kvh, tile, R);
     if (b0 < b2) {
-      int32_t page[S::NL];
-      load_pages<S>(a, w, b0 * S::BK, page);
       load_tile<S, VEC>(a, w, kvh, b0 * S::BK, page, ring0);
       load_pages<S>(a, w, (b0 + 1) * S::BK, page);
-      // Tile b, in `cur`, against the rows, while tile b + 1 is on its way into `nxt`.
+      // Tile b, in `cur`, against NR row groups, while tile b + 1 is on its way into `nxt`.
       // The stages are arrays of their own so that the compiler knows that reads of one
       // need not wait for loads into the other.
-      const auto step = [&](auto draft, int b, u32x4 *cur, u32x4 *nxt) {
+      const auto step = [&](auto nr, auto draft, int b, u32x4 *cur,
+                            u32x4 *nxt) __attribute__((always_inline)) {
         __builtin_amdgcn_s_waitcnt(kAllLoads);
         __syncthreads();  // tile b is there for every wave, the other stage is free
         if (b + 1 < b2) {
@@ -802,35 +932,40 @@ __global__ __launch_bounds__(S::NT, S::PER_CU) void k_tree_attn(TreeAttnArgs a) 
           if (clear_odd<S>(cur + S::TILE, w.len - b * S::BK)) met_odd = 1;
           __syncthreads();
         }
-        if (R.any) tile_step<S, draft.value>(a, w, b * S::BK, cur, R);
+        if constexpr (nr.value > 0)
+          tile_step<S, draft.value, nr.value>(a, w, b * S::BK, cur, R);
       };
-      // Tiles of the context first, in a loop of their own: with one loop around both kinds
-      // the kernel spilled registers inside it, and a reload from scratch waits for
-      // every load before it, the next tile's among them.
-      const std::integral_constant<bool, false> context;
-      const std::integral_constant<bool, true> draft;
-      const int plain = min(b2, w.len / S::BK);
-      int b = b0;
-      bool second = false;
-      for (; b < plain; ++b) {
-        step(context, b, ring0, ring1);
-        if (++b >= plain) {
-          second = true;
-          break;
+      // Tiles that all rows see first, in a loop of their own, and waves by their number
+      // of row groups in loops of their own (they meet at the same barriers): with
+      // one loop around several kinds the kernel spilled registers inside it, and a reload
+      // from scratch waits for every load before it, the next tile's among them.
+      const auto walk = [&](auto nr) __attribute__((always_inline)) {
+        const std::integral_constant<bool, false> context;
+        const std::integral_constant<bool, true> draft;
+        int b = b0;
+        bool second = false;
+        for (; b < plain; ++b) {
+          step(nr, context, b, ring0, ring1);
+          if (++b >= plain) {
+            second = true;
+            break;
+          }
+          step(nr, context, b, ring1, ring0);
         }
-        step(context, b, ring1, ring0);
-      }
-      for (; b < b2; ++b, second = !second) {
-        if (second)
-          step(draft, b, ring1, ring0);
-        else
-          step(draft, b, ring0, ring1);
-      }
+        for (; b < b2; ++b, second = !second)
+          step(nr, draft, b, second ? ring1 : ring0, second ? ring0 : ring1);
+      };
+      if (R.n == S::RT)
+        walk(std::integral_constant<int, S::RT>());
+      else if (S::RT > 1 && R.n == 1)
+        walk(std::integral_constant<int, 1>());
+      else
+        walk(std::integral_constant<int, 0>());
     }
     if (b0 < b1) {
       const bool whole = b0 == 0 && b1 == w.nb;
       store_rows<S>(a, w, kvh, tile, R, ring0, ring1, ml, whole ? -1 : 2L * g + (b0 == 0),
-                    &met_odd, b0 * S::BK, b2 * S::BK);
+                    &met_odd, max(b0, plain) * S::BK, b2 * S::BK);
       if (threadIdx.x == 0) met_odd = 0;
     }
     at += off_end - off;
@@ -840,61 +975,146 @@ __global__ __launch_bounds__(S::NT, S::PER_CU) void k_tree_attn(TreeAttnArgs a) 
       if (threadIdx.x == 0) {
         int last = -1;
         if (b0 == 0 && b1 > 0 && b1 < w.nb) {
-          const long begins = w.base + (item + 1) * each - w.cost;
-          for (last = g + 1; total * (last + 1) / eff <= begins;) ++last;
+          const long begins = w.base + (item + 1L) * each - w.cost;
+          for (last = g + 1; (last + 1) * per <= begins;) ++last;
         }
         a.joins[g] = {w.b, w.n, kvh, tile, w.step, last};
       }
       return;
     }
-    while (at >= w.base + work_cost(a, w)) {
-      const long base = w.base + work_cost(a, w);
-      work_of<S>(a, w.s + 1, w);
-      w.base = base;
+    if (at >= w.base + work_cost(a, w)) plan.next(a, at, w);
+  }
+}
+
+constexpr int kTreeGroups = 512;  // the most blocks
+constexpr int kJoinThreads = 256, kJoinGrid = 2048;
+
+// Joins the items that more than one block has walked: block g's list entry names the item
+// that it begins and another ends (each has one at most). Blocks take groups of rows of all
+// items in turn (a grid over items and rows was mostly blocks with nothing to do: 8192
+// of them took 11 us). Few partial results a row are read by one thread a column at once;
+// many by SL threads in turn, whose sums are added in one order.
+template <class S>
+__global__ __launch_bounds__(kJoinThreads) void k_tree_join(TreeAttnArgs a) {
+  constexpr int CF = S::HD / 4, SL = 4, RB = kJoinThreads / (CF * SL), RF = RB * SL;
+  constexpr int FEW = 8;
+  static_assert(RB >= 1 && kTreeGroups <= 2 * kJoinThreads, "a block has a row, a thread two blocks");
+  __shared__ float2 ml[RB][kTreeGroups];  // of each partial result: reference, sum
+  __shared__ f32x4 part[SL][RB][CF];
+  __shared__ int first[kTreeGroups + 1], owner[kTreeGroups], sums[kJoinThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  // The items that have rows to join, and the first unit of each.
+  int units[2], n_items = 0;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int g = 2 * tid + k;
+    units[k] = 0;
+    if (g < a.groups) {
+      const TreeJoin i = a.joins[g];
+      const int rows = min(i.step, i.n * a.group - i.tile * i.step);
+      if (i.last >= 0)
+        units[k] = i.last - g < FEW ? (rows + RF - 1) / RF : (rows + RB - 1) / RB;
+    }
+    n_items += units[k] > 0;
+  }
+  // (Units are below 2^16 in all, items too: one scan counts both.)
+  int both = n_items << 20 | (units[0] + units[1]);
+  int upto = wave_scan(both);
+  if (lane == 63) sums[tid >> 6] = upto;
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / 64; ++i) {
+    if (i < tid >> 6) upto += sums[i];
+    total += sums[i];
+  }
+  int before = upto - both;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (units[k]) {
+      first[before >> 20] = before & 0xfffff;
+      owner[before >> 20] = 2 * tid + k;
+      before += 1 << 20 | units[k];
+    }
+  const int items = total >> 20, all = total & 0xfffff;
+  const int c = tid % CF, r = tid / CF % RB, sl = tid / (CF * RB);
+  __syncthreads();
+  for (int u = blockIdx.x; u < all; u += kJoinGrid) {
+    int lo = 0, hi = items;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= u)
+        lo = mid;
+      else
+        hi = mid;
+    }
+    const int g = owner[lo];
+    const TreeJoin i = a.joins[g];
+    const int rows = min(i.step, i.n * a.group - i.tile * i.step), n = i.last - g + 1;
+    const int r0 = (u - first[lo]) * (n <= FEW ? RF : RB);
+    Work w;
+    w.b = i.b;
+    w.step = i.step;
+    const auto at = [&](int b, int r) { return (2L * (g + b) + (b == 0)) * S::BM + r0 + r; };
+    if (n <= FEW) {
+      const int r = tid / CF;
+      if (r0 + r >= rows) continue;
+      float2 x[FEW];
+      f32x4 o[FEW];
+#pragma unroll
+      for (int b = 0; b < FEW; ++b) {
+        const long from = at(min(b, n - 1), r);
+        x[b] = a.part_ml[from];
+        o[b] = reinterpret_cast<const f32x4 *>(a.part)[from * CF + c];
+      }
+      float top = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int b = 0; b < FEW; ++b) top = fmaxf(top, x[b].x);
+      f32x4 y{};
+#pragma unroll
+      for (int b = 0; b < FEW; ++b) {
+        if (b >= n) break;
+        const float f = x[b].x == -INFINITY ? (top == -INFINITY ? 1.f : 0.f)
+                                            : __builtin_amdgcn_exp2f(x[b].x - top);
+        l += x[b].y * f;
+        y += o[b] * f;
+      }
+      put_row<S>(a, w, i.kvh, i.tile, r0 + r, c, y, l, top, -1);
+      continue;
+    }
+    __syncthreads();  // LDS is free
+    for (int k = tid; k < n * RB; k += kJoinThreads)
+      ml[k % RB][k / RB] = a.part_ml[at(k / RB, min(k % RB, rows - 1 - r0))];
+    const int rr = min(r, rows - 1 - r0);
+    f32x4 some[4];  // (on their way before the weights are known)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      some[k] = reinterpret_cast<const f32x4 *>(a.part)[at(min(sl + k * SL, n - 1), rr) * CF + c];
+    __syncthreads();
+    float top = -INFINITY;
+    for (int b = 0; b < n; ++b) top = fmaxf(top, ml[r][b].x);
+    const auto weight = [&](int b) {
+      const float x = ml[r][b].x;
+      return x == -INFINITY ? (top == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(x - top);
+    };
+    f32x4 y{};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (sl + k * SL < n) y += some[k] * weight(sl + k * SL);
+#pragma unroll 4
+    for (int b = sl + 4 * SL; b < n; b += SL)
+      y += reinterpret_cast<const f32x4 *>(a.part)[at(b, rr) * CF + c] * weight(b);
+    part[sl][r][c] = y;
+    __syncthreads();
+    if (sl == 0 && r0 + r < rows) {
+#pragma unroll
+      for (int k = 1; k < SL; ++k) y += part[k][r][c];
+      float l = 0.f;
+      for (int b = 0; b < n; ++b) l += ml[r][b].y * weight(b);
+      put_row<S>(a, w, i.kvh, i.tile, r0 + r, c, y, l, top, -1);
     }
   }
 }
-
-constexpr int kJoinThreads = 256;
-
-// Joins the items that more than one block has walked. Block (x, y): the item that
-// attention block x begins and another ends (each has one at most), rows y RB .. + RB.
-template <class S>
-__global__ __launch_bounds__(kJoinThreads) void k_tree_join(TreeAttnArgs a) {
-  typedef typename S::T T;
-  constexpr int CF = S::HD / 4, RB = kJoinThreads / CF;
-  const int g = blockIdx.x;
-  const TreeJoin i = a.joins[g];
-  if (i.last < 0) return;
-  const int G = a.n_heads / a.n_kv;
-  const int r = blockIdx.y * RB + threadIdx.x / CF, c = threadIdx.x % CF;
-  const long gr = (long)i.tile * i.step + r;
-  if (r >= i.step || gr >= (long)i.n * G) return;
-  const auto at = [&](int b) { return (2L * b + (b == g)) * S::BM + r; };
-  float top = -INFINITY, l = 0.f;
-  for (int b = g; b <= i.last; ++b) top = fmaxf(top, a.part_ml[at(b)].x);
-  f32x4 y{};
-#pragma unroll 4
-  for (int b = g; b <= i.last; ++b) {
-    const float2 x = a.part_ml[at(b)];
-    const f32x4 o = reinterpret_cast<const f32x4 *>(a.part)[at(b) * CF + c];
-    const float f = x.x == -INFINITY ? (top == -INFINITY ? 1.f : 0.f)
-                                     : __builtin_amdgcn_exp2f(x.x - top);
-    l += x.y * f;
-    y += o * f;
-  }
-  const int j = (int)(gr / G), h = i.kvh * G + (int)(gr % G);
-  const float inv = l == 0.f ? 1.f : 1.f / l;
-  T *out = static_cast<T *>(a.out) + (i.b + j) * a.o_ts + h * a.o_hs + 4 * c;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (4 * c + e < a.hd) out[e] = from_f32<T>(y[e] * inv);
-  if (c == 0 && a.lse)
-    a.lse[(long)(i.b + j) * a.n_heads + h] =
-        l == 0.f ? -INFINITY : (top + __builtin_log2f(l)) * 0.69314718055994531f;
-}
-
-constexpr int kTreeGroups = 512;
 
 // Whether keys and values can go straight into LDS, 16 bytes at a time.
 template <typename T>
@@ -916,8 +1136,7 @@ hipError_t launch_tree_shape(TreeAttnArgs a, void *ws, hipStream_t s) {
   k_tree_attn<S, VEC><<<a.groups, S::NT, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  constexpr int RB = kJoinThreads / (S::HD / 4);
-  k_tree_join<S><<<dim3(a.groups, (S::BM + RB - 1) / RB), kJoinThreads, 0, s>>>(a);
+  k_tree_join<S><<<kJoinGrid, kJoinThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -925,29 +1144,23 @@ inline int tree_rows_of(int T, int n_seqs, int n_heads, int n_kv) {
   return (int)std::min<long>(((long)T * (n_heads / n_kv) + n_seqs - 1) / n_seqs, 1 << 20);
 }
 
-// Rows of a block by the rows that a mean sequence has for a key head.
-inline int tree_block_rows(int rows) {
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-}
+// Rows of a block by the rows that a mean sequence has for a key head: four waves along
+// the keys, two blocks a CU, where 16 or 32 rows are enough; else eight waves along the
+// rows. (32 sequences of 8192 keys, 8 key heads: 64 rows 261 us on four waves, 247 on eight,
+// 128 rows 298 and 260; 16 rows 217 on four waves of 16 rows, 32 rows 236 and 247.)
+inline int tree_block_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 256; }
 
 template <typename T, int HD>
 hipError_t launch_tree_type(const TreeAttnArgs &a, void *ws, hipStream_t s) {
   constexpr bool wide = sizeof(T) == 4 && HD == 256;  // (its tiles of 32 keys feed two waves)
-  if (!tree_aligned<T>(a))
-    return launch_tree_shape<TreeShape<T, HD, 4, wide ? 1 : 2, wide ? 2 : 1>, false>(a, ws, s);
-  switch (tree_block_rows(tree_rows_of(a.T, a.pages.n_seqs, a.n_heads, a.n_kv))) {
-    case 16:
-      if constexpr (!wide) return launch_tree_shape<TreeShape<T, HD, 4, 1, 1>, true>(a, ws, s);
-      [[fallthrough]];
-    case 32:
-      return launch_tree_shape<TreeShape<T, HD, 4, wide ? 1 : 2, wide ? 2 : 1>, true>(a, ws, s);
-    case 64:
-      return launch_tree_shape<TreeShape<T, HD, 4, 2, 2>, true>(a, ws, s);
-    case 128:
-      return launch_tree_shape<TreeShape<T, HD, 4, 2, 4>, true>(a, ws, s);
-    default:
-      return launch_tree_shape<TreeShape<T, HD, 8, HD == 256 ? 1 : 2, 8>, true>(a, ws, s);
-  }
+  typedef TreeShape<T, HD, 4, wide ? 1 : 2, wide ? 2 : 1> Small;
+  if (!tree_aligned<T>(a)) return launch_tree_shape<Small, false>(a, ws, s);
+  const int rows = tree_block_rows(tree_rows_of(a.T, a.pages.n_seqs, a.n_heads, a.n_kv));
+  if (rows == 256)
+    return launch_tree_shape<TreeShape<T, HD, 8, HD == 256 ? 1 : 2, 8>, true>(a, ws, s);
+  if constexpr (!wide)
+    if (rows == 16) return launch_tree_shape<TreeShape<T, HD, 4, 1, 1>, true>(a, ws, s);
+  return launch_tree_shape<Small, true>(a, ws, s);
 }
 
 template <typename T>

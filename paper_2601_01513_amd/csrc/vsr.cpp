@@ -1967,6 +1967,7 @@ extern "C" int vsr_tree_attention(const vsr_pages *pages, int32_t dtype, int32_t
     if (q->n_heads != out->n_heads) return "q and out differ in n_heads";
     if (k->n_heads != v->n_heads || q->n_heads % k->n_heads)
       return "k and v need one n_heads that divides q's";
+    if ((int64_t)T * q->n_heads > INT32_MAX - 256) return "T * n_heads must be below 2^31 - 256";
     if (heads_clash(out, T, q, T, head_dim, esize)) return "out overlaps q";
     if (heads_clash(out, T, k, slots, head_dim, esize)) return "out overlaps k";
     if (heads_clash(out, T, v, slots, head_dim, esize)) return "out overlaps v";
