@@ -112,8 +112,10 @@ __device__ __forceinline__ int swz(int r) {
 
 // The walk of all blocks over all work. An item is (sequence, key head, tile of rows),
 // tiles innermost, the sequence's rows shared evenly by its tiles, a tile's 16-row groups
-// by the waves. Its key tiles cost what they take, about 1 / 4 + the most groups that a
-// SIMD has (2.33 us for 3, 3.09 for 4), here in quarters. Block g takes the key tiles that begin in [g per, (g + 1) per) of the summed costs.
+// by the waves. Its key tiles cost 6 + the row groups that take them: 16 x 48 rows behind
+// 16384 positions took 284 us so and at 9 +, 286 at 4 +, 290 at 2 +, 294 with the groups
+// rounded up to four. Block g takes the key tiles that begin in [g per, (g + 1) per) of
+// the summed costs.
 struct Work {
   int s, b, n;      // a sequence and its rows
   int len, keys;    // positions before the draft, and with it
@@ -136,7 +138,7 @@ __device__ __forceinline__ void work_of(const TreeAttnArgs &a, int s, Work &w) {
   w.step = w.tiles <= 1 ? max(16, (rows + 15) / 16 * 16)
                         : ((rows + w.tiles - 1) / w.tiles + 15) / 16 * 16;
   w.nb = max(1, (w.keys + S::BK - 1) / S::BK);
-  w.cost = 1 + (w.step / 16 * S::WK + 3) / 4 * 4;
+  w.cost = 6 + w.step / 16 * S::WK;
 }
 
 __device__ __forceinline__ long work_cost(const TreeAttnArgs &a, const Work &w) {
@@ -291,7 +293,7 @@ struct Plan {
 // first and last block then has one of its tiles).
 template <class S>
 __device__ __forceinline__ int blocks_used(long total, int groups) {
-  constexpr int least = 2 * (1 + S::RT * S::NW / 4 * 4);
+  constexpr int least = 2 * (6 + S::RT * S::NW);
   return (int)max(1L, min(total / least, (long)groups));
 }
 // Blocks of one XCD take neighbouring ranges (tiles that share keys), unless there are
