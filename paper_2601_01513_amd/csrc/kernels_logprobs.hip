@@ -7,12 +7,11 @@
 // The largest is left out of S' so that log1p keeps its relative accuracy where one token
 // has nearly all the mass.
 //
-// A block takes a segment of a row, each of its waves 1024 entries of every 4096. Lanes
-// keep (m, S', W) online and count the entries ahead of the token. For the alternatives a
-// wave keeps a list of candidates in LDS and a bound below which no entry can be one of
-// its best: at first the top-th largest of the tile's 64 lane maxima, later the top-th
-// largest of the list; tiles without an entry above it pass by one comparison of the lane
-// maxima. Segments are merged by a second kernel.
+// A block takes a segment of a row, each of its waves 1024 entries of every 4096. A wave
+// holds one reference, the largest value it has met; most tiles have none as large, and
+// pass without a word about the one left out. Of the alternatives a wave keeps candidates
+// in LDS: those above a bound that rises with the lanes' largest values so far, the top-th
+// largest of which `top` entries reach. Segments are merged by a second kernel.
 #include <algorithm>
 #include <type_traits>
 
@@ -26,8 +25,9 @@ constexpr int kLpThreads = 256, kLpWaves = kLpThreads / 64;
 constexpr int kLpLane = 16;                  // entries a lane and tile
 constexpr int kLpTile = kLpLane * 64;        // entries a wave and tile
 constexpr int kMaxTop = 64;
-constexpr int kList = kLpTile + kMaxTop;     // a full tile behind the best ones so far
-static_assert(kLpWaves * kList >= 64 * kMaxTop, "the lists hold 64 segments' best");
+constexpr int kLpFew = 8;                    // lanes with candidates that leave the bound
+constexpr int kList = kLpTile + kMaxTop + 8;  // a full tile behind the best ones, padded
+static_assert(kLpWaves * kLpTile >= 64 * kMaxTop, "the lists hold 64 segments' best");
 
 // An order of floats as unsigned numbers; 0: nothing (and NaN).
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -59,19 +59,17 @@ __device__ __forceinline__ Stats joined(const Stats &a, const Stats &b) {
   return r;
 }
 
-__device__ __forceinline__ Stats over_wave(Stats a) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1)
-    a = joined(a, {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.w, d), __shfl_xor(a.ahead, d)});
-  return a;
-}
-
-struct Entry {
-  uint32_t order;
-  int id;
-};
+// A candidate: its order above, the complement of its id below, so that the better of two
+// is the larger. 0: none.
+typedef uint64_t Key;
+__device__ __forceinline__ Key key_of(uint32_t order, int id) { return (Key)order << 32 | (uint32_t)~id; }
+__device__ __forceinline__ uint32_t order_in(Key k) { return (uint32_t)(k >> 32); }
+__device__ __forceinline__ int id_in(Key k) { return k ? (int)~(uint32_t)k : -1; }
 
 __device__ __forceinline__ int set_lanes(bool in) { return __popcll(__ballot(in)); }
+__device__ __forceinline__ int lanes_before(uint64_t who) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+}
 
 // The largest bound that at least `want` of the values reach which count(b) counts (the
 // same in every lane); the lowest candidate if there are fewer. The lowest LOW bits of an
@@ -88,83 +86,80 @@ __device__ __forceinline__ uint32_t wave_bound(int want, Count count) {
   return max(b, kNothing + 1);
 }
 
-// Leaves the `top` best of a wave's list of n (ties: the lowest ids), in the order they
-// were in; returns their number, and in `bound` the lowest order among them if they are
-// `top`.
+// Leaves the `top` best of a wave's list of n, in the order they were in; returns their
+// number.
 template <int LOW>
-__device__ __forceinline__ int wave_cut(Entry *list, int n, int top, uint32_t &bound) {
+__device__ __forceinline__ int wave_cut(Key *list, int n, int top) {
   const int lane = threadIdx.x & 63;
-  if (n < top) return n;
-  uint32_t b;
-  if (n <= 256) {
-    uint32_t o[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = i * 64 + lane < n ? list[i * 64 + lane].order : 0;
-    b = wave_bound<LOW>(top, [&](uint32_t t) {
-      int c = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c += set_lanes(o[i] >= t);
-      return c;
-    });
-  } else {
-    b = wave_bound<LOW>(top, [&](uint32_t t) {
-      int c = 0;
-      for (int i = 0; i < n; i += 64) c += set_lanes(i + lane < n && list[i + lane].order >= t);
-      return c;
-    });
-  }
-  bound = max(bound, b);
+  if (n <= top) return n;
+  const uint32_t b = wave_bound<LOW>(top, [&](uint32_t t) {
+    int c = 0;
+    for (int i = 0; i < n; i += 64) c += set_lanes(i + lane < n && order_in(list[i + lane]) >= t);
+    return c;
+  });
   int above = 0, ties = 0;
   for (int i = 0; i < n; i += 64) {
-    const uint32_t o = i + lane < n ? list[i + lane].order : 0;
+    const uint32_t o = i + lane < n ? order_in(list[i + lane]) : 0;
     above += set_lanes(o > b);
     ties += set_lanes(o == b);
   }
-  int upto = INT32_MAX;  // the largest id of a tie that stays
+  uint32_t least = 0;  // the lowest complement of an id among the ties that stay
   if (ties > top - above) {
-    ties = top - above;
-    upto = 0;
 #pragma unroll 1
-    for (int bit = 24; bit >= 0; --bit) {
-      const int t = upto | 1 << bit;
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t t = least | 1u << bit;
       int c = 0;
       for (int i = 0; i < n; i += 64) {
-        const Entry e = i + lane < n ? list[i + lane] : Entry{0, 0};
-        c += set_lanes(e.order == b && e.id < t);
+        const Key e = i + lane < n ? list[i + lane] : 0;
+        c += set_lanes(order_in(e) == b && (uint32_t)e >= t);
       }
-      if (c < ties) upto = t;
+      if (c >= top - above) least = t;
     }
   }
   int out = 0;
   for (int i = 0; i < n; i += 64) {
-    const Entry e = i + lane < n ? list[i + lane] : Entry{0, 0};
-    const bool in = e.order > b || (e.order == b && e.id <= upto);
+    const Key e = i + lane < n ? list[i + lane] : 0;
+    const bool in = e >= ((Key)b << 32 | least);
     const uint64_t who = __ballot(in);
-    if (in) list[out + __popcll(who & ((1ull << lane) - 1))] = e;
+    if (in) list[out + lanes_before(who)] = e;
     out += __popcll(who);
   }
   return out;
 }
 
-// The entries of the block's lists (n[w] of wave w) in order: put(rank, entry) for the
-// best `top`, Entry{0, -1} for ranks past their number.
+// The best `top` of the lists of a block's waves in order: put(rank, key), with key 0 for
+// ranks past their number. Wave w's list has n[w] <= 64 keys, 0 up to the next multiple of
+// 8. A thread counts the keys above its own.
 template <class Put>
-__device__ __forceinline__ void block_order(Entry (*lists)[kList], const int *n, int top, Put put) {
-  int all = 0;
-  for (int w = 0; w < kLpWaves; ++w) all += n[w];
-  for (int i = threadIdx.x; i < all; i += kLpThreads) {
-    int w = 0, j = i;
-    while (j >= n[w]) j -= n[w++];
-    const Entry e = lists[w][j];
-    int rank = 0;
-    for (int v = 0; v < kLpWaves; ++v)
-      for (int k = 0; k < n[v]; ++k) {
-        const Entry o = lists[v][k];
-        rank += o.order > e.order || (o.order == e.order && o.id < e.id);
-      }
-    if (rank < top) put(rank, e);
+__device__ __forceinline__ void block_order(const Key (*lists)[kList], const int *n, int top, Put put) {
+  typedef Pack<Key, 2> Two;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const Key e = lane < n[w] ? lists[w][lane] : 0;
+  int rank = 0, all = 0;
+#pragma unroll
+  for (int v = 0; v < kLpWaves; ++v) {
+    const int nv = n[v];
+    all += nv;
+#pragma unroll 1
+    for (int k = 0; k < nv; k += 8) {
+      Two o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = *reinterpret_cast<const Two *>(&lists[v][k + 2 * i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rank += (o[i].v[0] > e) + (o[i].v[1] > e);
+    }
   }
-  for (int r = all + threadIdx.x; r < top; r += kLpThreads) put(r, Entry{0, -1});
+  if (e && rank < top) put(rank, e);
+  if ((int)threadIdx.x >= all && (int)threadIdx.x < top) put(threadIdx.x, 0);
+}
+
+// A wave's list of n ready for block_order: its best if there are more than 64, and padded.
+template <int LOW>
+__device__ __forceinline__ int list_done(Key *list, int n, int top) {
+  const int lane = threadIdx.x & 63;
+  if (n > 64) n = wave_cut<LOW>(list, n, top);
+  if (lane < 8) list[n + lane] = 0;
+  return n;
 }
 
 // A row's token and its logit.
@@ -190,12 +185,12 @@ __device__ __forceinline__ void store_row(const LogprobArgs &a, int r, const Giv
     a.logprob[r] = s.s != s.s ? s.s : none || t.id < 0 ? -INFINITY : (t.x - s.m) - lse;
   if (a.rank) a.rank[r] = t.id < 0 || t.x != t.x ? -1 : s.ahead;
 }
-__device__ __forceinline__ void store_top(const LogprobArgs &a, int r, int rank, Entry e,
+__device__ __forceinline__ void store_top(const LogprobArgs &a, int r, int rank, Key k,
                                           const Stats &s) {
   const long at = (long)r * a.top + rank;
-  if (a.top_id) a.top_id[at] = e.id;
+  if (a.top_id) a.top_id[at] = id_in(k);
   if (a.top_logprob)
-    a.top_logprob[at] = s.s != s.s ? s.s : e.id < 0 ? -INFINITY : (value_of(e.order) - s.m) - log1pf(s.s);
+    a.top_logprob[at] = s.s != s.s ? s.s : k == 0 ? -INFINITY : (value_of(order_in(k)) - s.m) - log1pf(s.s);
 }
 
 // The next float up (NaN past infinity).
@@ -207,19 +202,20 @@ __device__ __forceinline__ float next_up(float x) {
 
 // Grid (segments, rows): `tiles` tiles of kLpWaves waves a segment.
 template <typename T, bool TOP>
-__global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tiles, Stats *part,
-                                                         Entry *best) {
+__global__ __launch_bounds__(kLpThreads, 4) void k_logprobs(LogprobArgs a, int tiles, Stats *part,
+                                                            Key *best) {
   constexpr int VEC = 16 / sizeof(T), NP = kLpLane / VEC, STEP = kLpWaves * kLpTile;
   constexpr int LOW = sizeof(T) == 4 ? 0 : std::is_same<T, bf16>::value ? 16 : 13;
   typedef Pack<T, VEC> P;
-  __shared__ Entry lists[TOP ? kLpWaves : 1][TOP ? kList : 1];
+  __shared__ __attribute__((aligned(16))) Key lists[TOP ? kLpWaves : 1][kList];
   __shared__ Stats stats[kLpWaves];
   __shared__ int sizes[kLpWaves];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r = blockIdx.y;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = blockIdx.y;
   const T *row = static_cast<const T *>(a.logits) + r * a.stride;
   const int beg = blockIdx.x * tiles * STEP + w * kLpTile;
   const int end = (int)min((long)a.vocab, (long)(blockIdx.x + 1) * tiles * STEP);
-  const auto load = [&](int v0, P *p) {
+  const auto load = [&](int v0, P *p) __attribute__((always_inline)) {
     if (v0 + kLpTile <= a.vocab) {
 #pragma unroll
       for (int k = 0; k < NP; ++k)
@@ -238,85 +234,113 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
   if (beg < end) load(beg, raw);
   const Given<T> t(a, r);
   const float after = next_up(t.x);
-  Stats s{-INFINITY, 0.f, 0.f, 0};
-  uint32_t bound = kNothing;
+  float m = -INFINITY;        // the wave's largest value
+  float sum = 0.f, wsum = 0.f;  // the lane's share of S' and W
+  int ahead = 0;              // the wave's
+  float peak = -INFINITY;     // the lane's largest value
+  float lim = next_up(-INFINITY);  // candidates reach it
   int n = 0;
-  for (int v0 = beg; v0 < end; v0 += STEP) {
-    if (v0 + STEP < end) load(v0 + STEP, next);
+  const auto tile = [&](int v0, const P *raw) __attribute__((always_inline)) {
     float x[kLpLane], top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kLpLane; ++i) {
       x[i] = to_f32(raw[i / VEC].v[i % VEC]);
       top = fmaxf(top, x[i]);
     }
-    float same = 0.f;  // entries that are the lane's largest, but for the one left out
-    if (__any(top > s.m)) {
-      if (top > s.m) {
-        if (s.m > -INFINITY) {
-          const float d = s.m - top, f = __expf(d), one = 1.f + s.s;
-          s.w = f == 0.f ? 0.f : f * (s.w + one * d);
-          s.s = f * one;
-        }
-        s.m = top;
-        same = -1.f;
-      }
-    }
-    const float m = s.m == -INFINITY ? 0.f : s.m;
-    const bool here = t.id >= v0 && t.id < v0 + kLpTile;
     const float least = v0 > t.id ? after : t.x;
+    if (!__any(top >= m)) {
 #pragma unroll
-    for (int i = 0; i < kLpLane; ++i) {
-      const float d = x[i] - m, e = __expf(d);
-      same += d == 0.f ? 1.f : 0.f;
-      s.s += d == 0.f ? 0.f : e;
-      s.w += e * fmaxf(d, -200.f);  // (e is 0 there, also for -inf)
-      s.ahead += x[i] >= least;
+      for (int i = 0; i < kLpLane; ++i) {
+        const float d = x[i] - m, e = __expf(d);
+        sum += e;
+        wsum += e * fmaxf(d, -200.f);  // (e is 0 there, also for -inf)
+        ahead += set_lanes(x[i] >= least);
+      }
+    } else {
+      float now = top;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) now = fmaxf(now, __shfl_xor(now, d));
+      if (now > m && m > -INFINITY) {
+        // Lane 0 takes in what was the largest so far.
+        const float d = m - now, f = __expf(d), one = (lane == 0 ? 1.f : 0.f) + sum;
+        wsum = f == 0.f ? 0.f : f * (wsum + one * d);
+        sum = f * one;
+      }
+      const bool out = now > m;
+      m = fmaxf(m, now);
+      const float z = m == -INFINITY ? 0.f : m;
+      int same = 0;
+#pragma unroll
+      for (int i = 0; i < kLpLane; ++i) {
+        const float d = x[i] - z, e = __expf(d);
+        same += d == 0.f;
+        sum += d == 0.f ? 0.f : e;
+        wsum += e * fmaxf(d, -200.f);
+        ahead += set_lanes(x[i] >= least);
+      }
+      const uint64_t who = __ballot(same > 0);
+      sum += (float)(same - (out && who && lane == __builtin_ctzll(who)));
     }
-    s.s += same;
-    if (here) {  // (counted by >= above: those after the token, and itself, only if larger)
+    if (t.id >= v0 && t.id < v0 + kLpTile) {
+      // (Counted by >= above: those after the token, and itself, only if larger.)
 #pragma unroll
       for (int i = 0; i < kLpLane; ++i) {
         const int v = v0 + (i / VEC * 64 + lane) * VEC + i % VEC;
-        s.ahead -= x[i] == t.x && v >= t.id;
+        ahead -= set_lanes(x[i] == t.x && v >= t.id);
       }
     }
     if constexpr (TOP) {
-      const uint32_t o = order_of(top);
-      if (__any(o > bound)) {
-        const uint32_t b = wave_bound<LOW>(a.top, [&](uint32_t u) { return set_lanes(o >= u); });
-        int more = 0;
+      peak = fmaxf(peak, top);
+      const int who = set_lanes(top >= lim);
+      if (who) {
+        bool raised = false;
+        if (who > kLpFew) {
+          const uint32_t o = order_of(peak);
+          const float b = value_of(wave_bound<LOW>(a.top, [&](uint32_t u) { return set_lanes(o >= u); }));
+          raised = b > lim;
+          lim = fmaxf(lim, b);
+        }
+        if (n > kMaxTop) {
+          int more = n;
+#pragma unroll
+          for (int i = 0; i < kLpLane; ++i) more += set_lanes(x[i] >= lim);
+          if (more > kList - 8) n = wave_cut<LOW>(lists[w], n, a.top);
+        }
 #pragma unroll
         for (int i = 0; i < kLpLane; ++i) {
-          const uint32_t u = order_of(x[i]);
-          more += set_lanes(u >= b && u > bound);
+          const bool in = x[i] >= lim;
+          const uint64_t which = __ballot(in);
+          if (which) {
+            if (in)
+              lists[w][n + lanes_before(which)] =
+                  key_of(order_of(x[i]), v0 + (i / VEC * 64 + lane) * VEC + i % VEC);
+            n += __popcll(which);
+          }
         }
-        if (n + more > kList) n = wave_cut<LOW>(lists[w], n, a.top, bound);
-#pragma unroll
-        for (int i = 0; i < kLpLane; ++i) {
-          const uint32_t u = order_of(x[i]);
-          const bool in = u >= b && u > bound;
-          const uint64_t who = __ballot(in);
-          if (in)
-            lists[w][n + __popcll(who & ((1ull << lane) - 1))] = {
-                u, v0 + (i / VEC * 64 + lane) * VEC + i % VEC};
-          n += __popcll(who);
-        }
-        // (The lanes that reach b are `top` at least, unless b is the lowest candidate.)
-        if (b > kNothing + 1) bound = max(bound, b);
-        if (n >= 2 * a.top + 64) n = wave_cut<LOW>(lists[w], n, a.top, bound);
+        // `top` entries up to here reach a bound that was raised: later ones must pass it.
+        if (raised) lim = next_up(lim);
       }
     }
-#pragma unroll
-    for (int k = 0; k < NP; ++k) raw[k] = next[k];
+  };
+  for (int v0 = beg; v0 < end; v0 += 2 * STEP) {
+    if (v0 + STEP < end) load(v0 + STEP, next);
+    tile(v0, raw);
+    if (v0 + STEP >= end) break;
+    if (v0 + 2 * STEP < end) load(v0 + 2 * STEP, raw);
+    tile(v0 + STEP, next);
   }
-  s = over_wave(s);
-  if constexpr (TOP) n = wave_cut<LOW>(lists[w], n, a.top, bound);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    sum += __shfl_xor(sum, d);
+    wsum += __shfl_xor(wsum, d);
+  }
+  if constexpr (TOP) n = list_done<LOW>(lists[w], n, a.top);
   if (lane == 0) {
-    stats[w] = s;
+    stats[w] = {m, sum, wsum, ahead};
     sizes[w] = n;
   }
   __syncthreads();
-  s = joined(joined(stats[0], stats[1]), joined(stats[2], stats[3]));
+  const Stats s = joined(joined(stats[0], stats[1]), joined(stats[2], stats[3]));
   const long at = (long)r * gridDim.x + blockIdx.x;
   if (threadIdx.x == 0) {
     if (gridDim.x == 1)
@@ -325,40 +349,45 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
       part[at] = s;
   }
   if constexpr (TOP)
-    block_order(lists, sizes, a.top, [&](int rank, Entry e) {
+    block_order(lists, sizes, a.top, [&](int rank, Key k) {
       if (gridDim.x == 1)
-        store_top(a, r, rank, e, s);
+        store_top(a, r, rank, k, s);
       else
-        best[at * a.top + rank] = e;
+        best[at * a.top + rank] = k;
     });
 }
 
 template <typename T, bool TOP>
 __global__ __launch_bounds__(kLpThreads) void k_logprobs_merge(LogprobArgs a, int segments,
-                                                               const Stats *part,
-                                                               const Entry *best) {
-  __shared__ Entry lists[TOP ? kLpWaves : 1][TOP ? kList : 1];
+                                                               const Stats *part, const Key *best) {
+  __shared__ __attribute__((aligned(16))) Key lists[TOP ? kLpWaves : 1][kList];
   __shared__ int sizes[kLpWaves];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r = blockIdx.x;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = blockIdx.x;
   const Given<T> t(a, r);
-  const Stats s = over_wave(lane < segments ? part[(long)r * segments + lane]
-                                            : Stats{-INFINITY, 0.f, 0.f, 0});
-  if (threadIdx.x == 0) store_row(a, r, t, s);
+  Stats s{-INFINITY, 0.f, 0.f, 0};
+  if (lane < segments) s = part[(long)r * segments + lane];
   if constexpr (TOP) {
     int n = 0;
-    const Entry *row = best + (long)r * segments * a.top;
+    const Key *row = best + (long)r * segments * a.top;
     const int all = segments * a.top;
     for (int i = w * 64; i < all; i += kLpThreads) {
-      const Entry e = i + lane < all ? row[i + lane] : Entry{0, -1};
-      const uint64_t who = __ballot(e.id >= 0);
-      if (e.id >= 0) lists[w][n + __popcll(who & ((1ull << lane) - 1))] = e;
+      const Key k = i + lane < all ? row[i + lane] : 0;
+      const uint64_t who = __ballot(k != 0);
+      if (k) lists[w][n + lanes_before(who)] = k;
       n += __popcll(who);
     }
-    uint32_t bound = 0;
-    n = wave_cut<0>(lists[w], n, a.top, bound);
+    n = list_done<0>(lists[w], n, a.top);
     if (lane == 0) sizes[w] = n;
+  }
+  for (int d = 1; d < segments; d <<= 1)
+    s = joined(s, {__shfl_xor(s.m, d), __shfl_xor(s.s, d), __shfl_xor(s.w, d), __shfl_xor(s.ahead, d)});
+  if (threadIdx.x == 0) store_row(a, r, t, s);
+  if constexpr (TOP) {
     __syncthreads();
-    block_order(lists, sizes, a.top, [&](int rank, Entry e) { store_top(a, r, rank, e, s); });
+    // (Lane 0 has the statistics; in the others the order of the sum differs.)
+    s.m = __shfl(s.m, 0), s.s = __shfl(s.s, 0);
+    block_order(lists, sizes, a.top, [&](int rank, Key k) { store_top(a, r, rank, k, s); });
   }
 }
 
@@ -376,7 +405,7 @@ template <typename T, bool TOP>
 hipError_t launch_logprobs_as(const LogprobArgs &a, void *ws, hipStream_t s) {
   const Segments g = segments_of(a.rows, a.vocab);
   Stats *part = static_cast<Stats *>(ws);
-  Entry *best = reinterpret_cast<Entry *>(part + (size_t)a.rows * g.n);
+  Key *best = reinterpret_cast<Key *>(part + (size_t)a.rows * g.n);
   k_logprobs<T, TOP><<<dim3(g.n, a.rows), kLpThreads, 0, s>>>(a, g.tiles, part, best);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.n == 1) return e;
@@ -392,7 +421,7 @@ hipError_t launch_logprobs_type(const LogprobArgs &a, void *ws, hipStream_t s) {
 }  // namespace
 
 size_t logprobs_workspace_bytes(int rows, int vocab, int top) {
-  return (size_t)rows * segments_of(rows, vocab).n * (sizeof(Stats) + top * sizeof(Entry));
+  return (size_t)rows * segments_of(rows, vocab).n * (sizeof(Stats) + top * sizeof(Key));
 }
 
 hipError_t launch_logprobs(const LogprobArgs &a, int dtype, void *ws, hipStream_t s) {
