@@ -9,9 +9,10 @@
 //
 // A block takes a segment of a row, each of its waves 1024 entries of every 4096. A wave
 // holds one reference, the largest value it has met; most tiles have none as large, and
-// pass without a word about the one left out. Of the alternatives a wave keeps candidates
-// in LDS: those above a bound that rises with the lanes' largest values so far, the top-th
-// largest of which `top` entries reach. Segments are merged by a second kernel.
+// pass without a word about the one left out. Lanes keep the largest of what they read.
+// The top-th largest of a block's 256 is a bound that `top` entries reach, and only lanes
+// whose largest does can have read such an entry: their columns (about `top` of 256) are
+// read again for the candidates. Segments are merged by a second kernel.
 #include <algorithm>
 #include <type_traits>
 
@@ -25,9 +26,8 @@ constexpr int kLpThreads = 256, kLpWaves = kLpThreads / 64;
 constexpr int kLpLane = 16;                  // entries a lane and tile
 constexpr int kLpTile = kLpLane * 64;        // entries a wave and tile
 constexpr int kMaxTop = 64;
-constexpr int kLpFew = 8;                    // lanes with candidates that leave the bound
-constexpr int kList = kLpTile + kMaxTop + 8;  // a full tile behind the best ones, padded
-static_assert(kLpWaves * kLpTile >= 64 * kMaxTop, "the lists hold 64 segments' best");
+constexpr int kPad = 8;                      // keys read at once
+constexpr int kMaxSegments = 64;
 
 // An order of floats as unsigned numbers; 0: nothing (and NaN).
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -86,12 +86,11 @@ __device__ __forceinline__ uint32_t wave_bound(int want, Count count) {
   return max(b, kNothing + 1);
 }
 
-// Leaves the `top` best of a wave's list of n, in the order they were in; returns their
-// number.
+// Leaves the `top` best of a wave's list of n > top, in the order they were in; returns
+// the lowest order among them.
 template <int LOW>
-__device__ __forceinline__ int wave_cut(Key *list, int n, int top) {
+__device__ __forceinline__ uint32_t wave_cut(Key *list, int n, int top) {
   const int lane = threadIdx.x & 63;
-  if (n <= top) return n;
   const uint32_t b = wave_bound<LOW>(top, [&](uint32_t t) {
     int c = 0;
     for (int i = 0; i < n; i += 64) c += set_lanes(i + lane < n && order_in(list[i + lane]) >= t);
@@ -124,14 +123,14 @@ __device__ __forceinline__ int wave_cut(Key *list, int n, int top) {
     if (in) list[out + lanes_before(who)] = e;
     out += __popcll(who);
   }
-  return out;
+  return b;
 }
 
 // The best `top` of the lists of a block's waves in order: put(rank, key), with key 0 for
 // ranks past their number. Wave w's list has n[w] <= 64 keys, 0 up to the next multiple of
-// 8. A thread counts the keys above its own.
-template <class Put>
-__device__ __forceinline__ void block_order(const Key (*lists)[kList], const int *n, int top, Put put) {
+// kPad. A thread counts the keys above its own.
+template <int LIST, class Put>
+__device__ __forceinline__ void block_order(const Key (*lists)[LIST], const int *n, int top, Put put) {
   typedef Pack<Key, 2> Two;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const Key e = lane < n[w] ? lists[w][lane] : 0;
@@ -141,12 +140,12 @@ __device__ __forceinline__ void block_order(const Key (*lists)[kList], const int
     const int nv = n[v];
     all += nv;
 #pragma unroll 1
-    for (int k = 0; k < nv; k += 8) {
-      Two o[4];
+    for (int k = 0; k < nv; k += kPad) {
+      Two o[kPad / 2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = *reinterpret_cast<const Two *>(&lists[v][k + 2 * i]);
+      for (int i = 0; i < kPad / 2; ++i) o[i] = *reinterpret_cast<const Two *>(&lists[v][k + 2 * i]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) rank += (o[i].v[0] > e) + (o[i].v[1] > e);
+      for (int i = 0; i < kPad / 2; ++i) rank += (o[i].v[0] > e) + (o[i].v[1] > e);
     }
   }
   if (e && rank < top) put(rank, e);
@@ -157,8 +156,11 @@ __device__ __forceinline__ void block_order(const Key (*lists)[kList], const int
 template <int LOW>
 __device__ __forceinline__ int list_done(Key *list, int n, int top) {
   const int lane = threadIdx.x & 63;
-  if (n > 64) n = wave_cut<LOW>(list, n, top);
-  if (lane < 8) list[n + lane] = 0;
+  if (n > 64) {
+    wave_cut<LOW>(list, n, top);
+    n = top;
+  }
+  if (lane < kPad) list[n + lane] = 0;
   return n;
 }
 
@@ -202,12 +204,14 @@ __device__ __forceinline__ float next_up(float x) {
 
 // Grid (segments, rows): `tiles` tiles of kLpWaves waves a segment.
 template <typename T, bool TOP>
-__global__ __launch_bounds__(kLpThreads, 4) void k_logprobs(LogprobArgs a, int tiles, Stats *part,
-                                                            Key *best) {
+__global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tiles, Stats *part,
+                                                         Key *best) {
   constexpr int VEC = 16 / sizeof(T), NP = kLpLane / VEC, STEP = kLpWaves * kLpTile;
   constexpr int LOW = sizeof(T) == 4 ? 0 : std::is_same<T, bf16>::value ? 16 : 13;
   typedef Pack<T, VEC> P;
-  __shared__ __attribute__((aligned(16))) Key lists[TOP ? kLpWaves : 1][kList];
+  constexpr int ROOM = kMaxTop + 64 * VEC;  // one more piece a lane behind the best ones
+  __shared__ __attribute__((aligned(16))) Key lists[TOP ? kLpWaves : 1][ROOM + kPad];
+  __shared__ uint32_t peaks[kLpThreads];
   __shared__ Stats stats[kLpWaves];
   __shared__ int sizes[kLpWaves];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -238,8 +242,6 @@ __global__ __launch_bounds__(kLpThreads, 4) void k_logprobs(LogprobArgs a, int t
   float sum = 0.f, wsum = 0.f;  // the lane's share of S' and W
   int ahead = 0;              // the wave's
   float peak = -INFINITY;     // the lane's largest value
-  float lim = next_up(-INFINITY);  // candidates reach it
-  int n = 0;
   const auto tile = [&](int v0, const P *raw) __attribute__((always_inline)) {
     float x[kLpLane], top = -INFINITY;
 #pragma unroll
@@ -289,38 +291,7 @@ __global__ __launch_bounds__(kLpThreads, 4) void k_logprobs(LogprobArgs a, int t
         ahead -= set_lanes(x[i] == t.x && v >= t.id);
       }
     }
-    if constexpr (TOP) {
-      peak = fmaxf(peak, top);
-      const int who = set_lanes(top >= lim);
-      if (who) {
-        bool raised = false;
-        if (who > kLpFew) {
-          const uint32_t o = order_of(peak);
-          const float b = value_of(wave_bound<LOW>(a.top, [&](uint32_t u) { return set_lanes(o >= u); }));
-          raised = b > lim;
-          lim = fmaxf(lim, b);
-        }
-        if (n > kMaxTop) {
-          int more = n;
-#pragma unroll
-          for (int i = 0; i < kLpLane; ++i) more += set_lanes(x[i] >= lim);
-          if (more > kList - 8) n = wave_cut<LOW>(lists[w], n, a.top);
-        }
-#pragma unroll
-        for (int i = 0; i < kLpLane; ++i) {
-          const bool in = x[i] >= lim;
-          const uint64_t which = __ballot(in);
-          if (which) {
-            if (in)
-              lists[w][n + lanes_before(which)] =
-                  key_of(order_of(x[i]), v0 + (i / VEC * 64 + lane) * VEC + i % VEC);
-            n += __popcll(which);
-          }
-        }
-        // `top` entries up to here reach a bound that was raised: later ones must pass it.
-        if (raised) lim = next_up(lim);
-      }
-    }
+    peak = fmaxf(peak, top);
   };
   for (int v0 = beg; v0 < end; v0 += 2 * STEP) {
     if (v0 + STEP < end) load(v0 + STEP, next);
@@ -334,10 +305,61 @@ __global__ __launch_bounds__(kLpThreads, 4) void k_logprobs(LogprobArgs a, int t
     sum += __shfl_xor(sum, d);
     wsum += __shfl_xor(wsum, d);
   }
-  if constexpr (TOP) n = list_done<LOW>(lists[w], n, a.top);
-  if (lane == 0) {
-    stats[w] = {m, sum, wsum, ahead};
-    sizes[w] = n;
+  if (lane == 0) stats[w] = {m, sum, wsum, ahead};
+  if constexpr (TOP) {
+    const uint32_t mine = order_of(peak);
+    peaks[threadIdx.x] = mine;
+    __syncthreads();
+    uint32_t o[kLpWaves];
+#pragma unroll
+    for (int i = 0; i < kLpWaves; ++i) o[i] = peaks[i * 64 + lane];
+    const uint32_t bound = wave_bound<LOW>(a.top, [&](uint32_t u) {
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < kLpWaves; ++i) c += set_lanes(o[i] >= u);
+      return c;
+    });
+    // The wave's lanes that reach the bound, in order; their columns in pieces of VEC,
+    // which lanes take in the order of the ids.
+    const bool in = mine >= bound;
+    const uint64_t who = __ballot(in);
+    const int cols = __popcll(who), turns = (end - beg + STEP - 1) / STEP;
+    if (in) peaks[w * 64 + lanes_before(who)] = lane;  // (the wave's own part)
+    float lim = value_of(bound);
+    int n = 0;
+    const int pieces = beg < end ? cols * NP * turns : 0;
+    for (int u0 = 0; u0 < pieces; u0 += 64) {
+      const int u = u0 + lane, row_of = u / max(cols, 1);  // (tile, piece of the lane)
+      const int v = beg + row_of / NP * STEP +
+                    (row_of % NP * 64 + (int)peaks[w * 64 + u - row_of * cols]) * VEC;
+      float x[VEC];
+      if (u < pieces && v + VEC <= a.vocab) {
+        const P p = *reinterpret_cast<const P *>(row + v);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[j] = to_f32(p.v[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          x[j] = u < pieces && v + j < a.vocab ? to_f32(row[v + j]) : -INFINITY;
+      }
+      int more = 0;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) more += set_lanes(x[j] >= lim);
+      if (n + more > ROOM) {
+        // What comes has higher ids: it has to pass the last of the best.
+        lim = next_up(value_of(wave_cut<LOW>(lists[w], n, a.top)));
+        n = a.top;
+      }
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const bool is = x[j] >= lim;
+        const uint64_t which = __ballot(is);
+        if (is) lists[w][n + lanes_before(which)] = key_of(order_of(x[j]), v + j);
+        n += __popcll(which);
+      }
+    }
+    n = list_done<LOW>(lists[w], n, a.top);
+    if (lane == 0) sizes[w] = n;
   }
   __syncthreads();
   const Stats s = joined(joined(stats[0], stats[1]), joined(stats[2], stats[3]));
@@ -360,7 +382,8 @@ __global__ __launch_bounds__(kLpThreads, 4) void k_logprobs(LogprobArgs a, int t
 template <typename T, bool TOP>
 __global__ __launch_bounds__(kLpThreads) void k_logprobs_merge(LogprobArgs a, int segments,
                                                                const Stats *part, const Key *best) {
-  __shared__ __attribute__((aligned(16))) Key lists[TOP ? kLpWaves : 1][kList];
+  constexpr int ROOM = kMaxTop * kMaxSegments / kLpWaves;
+  __shared__ __attribute__((aligned(16))) Key lists[TOP ? kLpWaves : 1][ROOM + kPad];
   __shared__ int sizes[kLpWaves];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x;
@@ -396,7 +419,7 @@ struct Segments {
 };
 Segments segments_of(int rows, int vocab) {
   const int step = kLpWaves * kLpTile, tiles = (vocab + step - 1) / step;
-  const int want = std::max(1, std::min({(1024 + rows - 1) / rows, 64, tiles}));
+  const int want = std::max(1, std::min({(1024 + rows - 1) / rows, kMaxSegments, tiles}));
   const int each = (tiles + want - 1) / want;
   return {(tiles + each - 1) / each, each};
 }
