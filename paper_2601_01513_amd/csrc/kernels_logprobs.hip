@@ -9,10 +9,11 @@
 //
 // A block takes a segment of a row, each of its waves 1024 entries of every 4096. A wave
 // holds one reference, the largest value it has met; most tiles have none as large, and
-// pass without a word about the one left out. Lanes keep the largest of what they read.
-// The top-th largest of a block's 256 is a bound that `top` entries reach, and only lanes
-// whose largest does can have read such an entry: their columns (about `top` of 256) are
-// read again for the candidates. Segments are merged by a second kernel.
+// pass without a word about the one left out. Lanes keep the largest of what they read,
+// and of each span of tiles. The top-th largest of a block's 256 is a bound that `top`
+// entries reach, and the entries that do are in spans of lanes whose largest does (little
+// more than `top` of them): these are read again for the candidates. Segments are merged
+// by a second kernel.
 #include <algorithm>
 #include <type_traits>
 
@@ -28,6 +29,7 @@ constexpr int kLpTile = kLpLane * 64;        // entries a wave and tile
 constexpr int kMaxTop = 64;
 constexpr int kPad = 8;                      // keys read at once
 constexpr int kMaxSegments = 64;
+constexpr int kSpans = 32;                   // spans of tiles in a segment
 
 // An order of floats as unsigned numbers; 0: nothing (and NaN).
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -71,9 +73,14 @@ __device__ __forceinline__ int lanes_before(uint64_t who) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
 }
 
+// The lowest bits of an order that follow from the others, with values of type T.
+template <typename T>
+constexpr int low_bits() {
+  return sizeof(T) == 4 ? 0 : std::is_same<T, bf16>::value ? 16 : 13;
+}
+
 // The largest bound that at least `want` of the values reach which count(b) counts (the
-// same in every lane); the lowest candidate if there are fewer. The lowest LOW bits of an
-// order follow from the others (those of a 16-bit type's values).
+// same in every lane); the lowest candidate if there are fewer.
 template <int LOW, class Count>
 __device__ __forceinline__ uint32_t wave_bound(int want, Count count) {
   uint32_t b = 0;
@@ -91,11 +98,19 @@ __device__ __forceinline__ uint32_t wave_bound(int want, Count count) {
 template <int LOW>
 __device__ __forceinline__ uint32_t wave_cut(Key *list, int n, int top) {
   const int lane = threadIdx.x & 63;
-  const uint32_t b = wave_bound<LOW>(top, [&](uint32_t t) {
-    int c = 0;
-    for (int i = 0; i < n; i += 64) c += set_lanes(i + lane < n && order_in(list[i + lane]) >= t);
-    return c;
-  });
+  uint32_t b;
+  if (n <= 128) {
+    const uint32_t o0 = order_in(list[lane]), o1 = 64 + lane < n ? order_in(list[64 + lane]) : 0;
+    b = wave_bound<LOW>(top, [&](uint32_t t) {
+      return set_lanes(o0 >= t && lane < n) + set_lanes(o1 >= t);
+    });
+  } else {
+    b = wave_bound<LOW>(top, [&](uint32_t t) {
+      int c = 0;
+      for (int i = 0; i < n; i += 64) c += set_lanes(i + lane < n && order_in(list[i + lane]) >= t);
+      return c;
+    });
+  }
   int above = 0, ties = 0;
   for (int i = 0; i < n; i += 64) {
     const uint32_t o = i + lane < n ? order_in(list[i + lane]) : 0;
@@ -207,11 +222,13 @@ template <typename T, bool TOP>
 __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tiles, Stats *part,
                                                          Key *best) {
   constexpr int VEC = 16 / sizeof(T), NP = kLpLane / VEC, STEP = kLpWaves * kLpTile;
-  constexpr int LOW = sizeof(T) == 4 ? 0 : std::is_same<T, bf16>::value ? 16 : 13;
+  constexpr int LOW = low_bits<T>();
   typedef Pack<T, VEC> P;
   constexpr int ROOM = kMaxTop + 64 * VEC;  // one more piece a lane behind the best ones
   __shared__ __attribute__((aligned(16))) Key lists[TOP ? kLpWaves : 1][ROOM + kPad];
   __shared__ uint32_t peaks[kLpThreads];
+  __shared__ uint16_t tops[TOP ? kSpans : 1][kLpThreads];  // upper half of a span's order
+  __shared__ uint16_t found[TOP ? kLpWaves : 1][128];      // spans to read: lane, span
   __shared__ Stats stats[kLpWaves];
   __shared__ int sizes[kLpWaves];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -242,6 +259,9 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
   float sum = 0.f, wsum = 0.f;  // the lane's share of S' and W
   int ahead = 0;              // the wave's
   float peak = -INFINITY;     // the lane's largest value
+  float high = -INFINITY;     // that of the span
+  const int span = (tiles + kSpans - 1) / kSpans;
+  int turn = 0, at_span = 0;
   const auto tile = [&](int v0, const P *raw) __attribute__((always_inline)) {
     float x[kLpLane], top = -INFINITY;
 #pragma unroll
@@ -291,7 +311,15 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
         ahead -= set_lanes(x[i] == t.x && v >= t.id);
       }
     }
-    peak = fmaxf(peak, top);
+    if constexpr (TOP) {
+      high = fmaxf(high, top);
+      if (++turn == span || v0 + STEP >= end) {
+        tops[at_span++][threadIdx.x] = (uint16_t)(order_of(high) >> 16);
+        peak = fmaxf(peak, high);
+        high = -INFINITY;
+        turn = 0;
+      }
+    }
   };
   for (int v0 = beg; v0 < end; v0 += 2 * STEP) {
     if (v0 + STEP < end) load(v0 + STEP, next);
@@ -319,45 +347,59 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
       for (int i = 0; i < kLpWaves; ++i) c += set_lanes(o[i] >= u);
       return c;
     });
-    // The wave's lanes that reach the bound, in order; their columns in pieces of VEC,
-    // which lanes take in the order of the ids.
-    const bool in = mine >= bound;
-    const uint64_t who = __ballot(in);
-    const int cols = __popcll(who), turns = (end - beg + STEP - 1) / STEP;
-    if (in) peaks[w * 64 + lanes_before(who)] = lane;  // (the wave's own part)
     float lim = value_of(bound);
     int n = 0;
-    const int pieces = beg < end ? cols * NP * turns : 0;
-    for (int u0 = 0; u0 < pieces; u0 += 64) {
-      const int u = u0 + lane, row_of = u / max(cols, 1);  // (tile, piece of the lane)
-      const int v = beg + row_of / NP * STEP +
-                    (row_of % NP * 64 + (int)peaks[w * 64 + u - row_of * cols]) * VEC;
-      float x[VEC];
-      if (u < pieces && v + VEC <= a.vocab) {
-        const P p = *reinterpret_cast<const P *>(row + v);
+    uint16_t *mine_found = found[w];
+    // Reads spans found[0..many): the pieces of a span's lane by tiles.
+    const auto collect = [&](int many) __attribute__((always_inline)) {
+      const int per = NP * span, pieces = many * per;
+      uint32_t cut = 0;
+#pragma unroll 1
+      for (int u0 = 0; u0 < pieces; u0 += 64) {
+        const int u = u0 + lane, f = mine_found[min(u / per, many - 1)], i = u % per;
+        const int v = beg + ((f >> 6) * span + i / NP) * STEP + (i % NP * 64 + (f & 63)) * VEC;
+        float x[VEC];
+        if (u < pieces && v + VEC <= min(end, a.vocab)) {
+          const P p = *reinterpret_cast<const P *>(row + v);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) x[j] = to_f32(p.v[j]);
-      } else {
+          for (int j = 0; j < VEC; ++j) x[j] = to_f32(p.v[j]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j)
-          x[j] = u < pieces && v + j < a.vocab ? to_f32(row[v + j]) : -INFINITY;
+          for (int j = 0; j < VEC; ++j)
+            x[j] = u < pieces && v + j < end ? to_f32(row[v + j]) : -INFINITY;
+        }
+        int more = 0;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) more += set_lanes(x[j] >= lim);
+        if (n + more > ROOM) {
+          cut = wave_cut<LOW>(lists[w], n, a.top);
+          lim = fmaxf(lim, value_of(cut));
+          n = a.top;
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const bool is = x[j] >= lim;
+          const uint64_t which = __ballot(is);
+          if (is) lists[w][n + lanes_before(which)] = key_of(order_of(x[j]), v + j);
+          n += __popcll(which);
+        }
       }
-      int more = 0;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) more += set_lanes(x[j] >= lim);
-      if (n + more > ROOM) {
-        // What comes has higher ids: it has to pass the last of the best.
-        lim = next_up(value_of(wave_cut<LOW>(lists[w], n, a.top)));
-        n = a.top;
-      }
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const bool is = x[j] >= lim;
-        const uint64_t which = __ballot(is);
-        if (is) lists[w][n + lanes_before(which)] = key_of(order_of(x[j]), v + j);
-        n += __popcll(which);
+      // What comes has higher ids: it has to pass the last of the best.
+      if (cut) lim = next_up(lim);
+    };
+    int many = 0;
+    for (int k = 0; k < at_span; ++k) {
+      // (lim rises when a list was cut)
+      const bool in = tops[k][threadIdx.x] >= (order_of(lim) >> 16);
+      const uint64_t who = __ballot(in);
+      if (in) mine_found[many + lanes_before(who)] = (uint16_t)(k << 6 | lane);
+      many += __popcll(who);
+      if (many > 64) {
+        collect(many);
+        many = 0;
       }
     }
+    if (many) collect(many);
     n = list_done<LOW>(lists[w], n, a.top);
     if (lane == 0) sizes[w] = n;
   }
@@ -400,7 +442,7 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs_merge(LogprobArgs a, in
       if (k) lists[w][n + lanes_before(who)] = k;
       n += __popcll(who);
     }
-    n = list_done<0>(lists[w], n, a.top);
+    n = list_done<low_bits<T>()>(lists[w], n, a.top);
     if (lane == 0) sizes[w] = n;
   }
   for (int d = 1; d < segments; d <<= 1)
