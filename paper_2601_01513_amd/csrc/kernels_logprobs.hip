@@ -29,7 +29,8 @@ constexpr int kLpTile = kLpLane * 64;        // entries a wave and tile
 constexpr int kMaxTop = 64;
 constexpr int kPad = 8;                      // keys read at once
 constexpr int kMaxSegments = 64;
-constexpr int kSpans = 32;                   // spans of tiles in a segment
+constexpr int kSpans = 16;                   // spans of tiles in a segment
+constexpr int kRoom = kMaxTop + 64;          // candidates of a wave
 
 // An order of floats as unsigned numbers; 0: nothing (and NaN).
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -91,6 +92,22 @@ __device__ __forceinline__ uint32_t wave_bound(int want, Count count) {
   }
   if (LOW && b < 0x80000000u) b |= (1u << LOW) - 1;
   return max(b, kNothing + 1);
+}
+
+// The same of the values of a block's threads, one each.
+template <int LOW>
+__device__ __forceinline__ uint32_t block_bound(int want, uint32_t mine, uint32_t *all) {
+  all[threadIdx.x] = mine;
+  __syncthreads();
+  uint32_t o[kLpWaves];
+#pragma unroll
+  for (int i = 0; i < kLpWaves; ++i) o[i] = all[i * 64 + (threadIdx.x & 63)];
+  return wave_bound<LOW>(want, [&](uint32_t u) {
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < kLpWaves; ++i) c += set_lanes(o[i] >= u);
+    return c;
+  });
 }
 
 // Leaves the `top` best of a wave's list of n > top, in the order they were in; returns
@@ -224,8 +241,7 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
   constexpr int VEC = 16 / sizeof(T), NP = kLpLane / VEC, STEP = kLpWaves * kLpTile;
   constexpr int LOW = low_bits<T>();
   typedef Pack<T, VEC> P;
-  constexpr int ROOM = kMaxTop + 64 * VEC;  // one more piece a lane behind the best ones
-  __shared__ __attribute__((aligned(16))) Key lists[TOP ? kLpWaves : 1][ROOM + kPad];
+  __shared__ __attribute__((aligned(16))) Key lists[TOP ? kLpWaves : 1][kRoom + kPad];
   __shared__ uint32_t peaks[kLpThreads];
   __shared__ uint16_t tops[TOP ? kSpans : 1][kLpThreads];  // upper half of a span's order
   __shared__ uint16_t found[TOP ? kLpWaves : 1][128];      // spans to read: lane, span
@@ -335,57 +351,58 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
   }
   if (lane == 0) stats[w] = {m, sum, wsum, ahead};
   if constexpr (TOP) {
-    const uint32_t mine = order_of(peak);
-    peaks[threadIdx.x] = mine;
-    __syncthreads();
-    uint32_t o[kLpWaves];
-#pragma unroll
-    for (int i = 0; i < kLpWaves; ++i) o[i] = peaks[i * 64 + lane];
-    const uint32_t bound = wave_bound<LOW>(a.top, [&](uint32_t u) {
-      int c = 0;
-#pragma unroll
-      for (int i = 0; i < kLpWaves; ++i) c += set_lanes(o[i] >= u);
-      return c;
-    });
+    const uint32_t bound = block_bound<LOW>(a.top, order_of(peak), peaks);
     float lim = value_of(bound);
     int n = 0;
     uint16_t *mine_found = found[w];
-    // Reads spans found[0..many): the pieces of a span's lane by tiles.
+    // Reads spans found[0..many): by lanes, or in the order of ids if all are one span.
     const auto collect = [&](int many) __attribute__((always_inline)) {
       const int per = NP * span, pieces = many * per;
+      const bool one = mine_found[0] >> 6 == mine_found[many - 1] >> 6;
       uint32_t cut = 0;
 #pragma unroll 1
       for (int u0 = 0; u0 < pieces; u0 += 64) {
-        const int u = u0 + lane, f = mine_found[min(u / per, many - 1)], i = u % per;
+        const int u = min(u0 + lane, pieces - 1), q = u / (one ? many : per);
+        const int rest = u - q * (one ? many : per), f = mine_found[one ? rest : q];
+        const int i = one ? q : rest;
         const int v = beg + ((f >> 6) * span + i / NP) * STEP + (i % NP * 64 + (f & 63)) * VEC;
         float x[VEC];
-        if (u < pieces && v + VEC <= min(end, a.vocab)) {
+        if (u0 + lane < pieces && v + VEC <= end) {
           const P p = *reinterpret_cast<const P *>(row + v);
 #pragma unroll
           for (int j = 0; j < VEC; ++j) x[j] = to_f32(p.v[j]);
         } else {
 #pragma unroll
           for (int j = 0; j < VEC; ++j)
-            x[j] = u < pieces && v + j < end ? to_f32(row[v + j]) : -INFINITY;
+            x[j] = u0 + lane < pieces && v + j < end ? to_f32(row[v + j]) : -INFINITY;
         }
         int more = 0;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) more += set_lanes(x[j] >= lim);
-        if (n + more > ROOM) {
-          cut = wave_cut<LOW>(lists[w], n, a.top);
-          lim = fmaxf(lim, value_of(cut));
-          n = a.top;
-        }
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const bool is = x[j] >= lim;
+        const auto append = [&](float y, int j) __attribute__((always_inline)) {
+          const bool is = y >= lim;
           const uint64_t which = __ballot(is);
-          if (is) lists[w][n + lanes_before(which)] = key_of(order_of(x[j]), v + j);
+          if (is) lists[w][n + lanes_before(which)] = key_of(order_of(y), v + j);
           n += __popcll(which);
+        };
+        if (n + more <= kRoom) {
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) append(x[j], j);
+        } else {
+#pragma unroll 1
+          for (int j = 0; j < VEC; ++j) {
+            if (n > kMaxTop) {
+              cut = wave_cut<LOW>(lists[w], n, a.top);
+              lim = fmaxf(lim, one && j == 0 ? next_up(value_of(cut)) : value_of(cut));
+              n = a.top;
+            }
+            append(u0 + lane < pieces && v + j < end ? to_f32(row[v + j]) : -INFINITY, j);
+          }
         }
       }
-      // What comes has higher ids: it has to pass the last of the best.
-      if (cut) lim = next_up(lim);
+      // What comes has higher ids (and within one span, from turn to turn): it has to pass
+      // the last of the best.
+      if (cut) lim = fmaxf(lim, next_up(value_of(cut)));
     };
     int many = 0;
     for (int k = 0; k < at_span; ++k) {
@@ -394,7 +411,7 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
       const uint64_t who = __ballot(in);
       if (in) mine_found[many + lanes_before(who)] = (uint16_t)(k << 6 | lane);
       many += __popcll(who);
-      if (many > 64) {
+      if (many >= 64) {
         collect(many);
         many = 0;
       }
@@ -424,8 +441,9 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
 template <typename T, bool TOP>
 __global__ __launch_bounds__(kLpThreads) void k_logprobs_merge(LogprobArgs a, int segments,
                                                                const Stats *part, const Key *best) {
-  constexpr int ROOM = kMaxTop * kMaxSegments / kLpWaves;
-  __shared__ __attribute__((aligned(16))) Key lists[TOP ? kLpWaves : 1][ROOM + kPad];
+  constexpr int MANY = kMaxTop * kMaxSegments / kLpThreads;
+  __shared__ __attribute__((aligned(16))) Key lists[TOP ? kLpWaves : 1][64 * MANY + kPad];
+  __shared__ uint32_t peaks[TOP ? kLpThreads : 1];
   __shared__ int sizes[kLpWaves];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x;
@@ -433,13 +451,28 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs_merge(LogprobArgs a, in
   Stats s{-INFINITY, 0.f, 0.f, 0};
   if (lane < segments) s = part[(long)r * segments + lane];
   if constexpr (TOP) {
-    int n = 0;
+    // As above: a thread holds up to MANY keys, of different ranks in their segments, and the
+    // top-th largest of the threads' best is a bound.
     const Key *row = best + (long)r * segments * a.top;
     const int all = segments * a.top;
-    for (int i = w * 64; i < all; i += kLpThreads) {
-      const Key k = i + lane < all ? row[i + lane] : 0;
-      const uint64_t who = __ballot(k != 0);
-      if (k) lists[w][n + lanes_before(who)] = k;
+    Key keys[MANY], high = 0;
+#pragma unroll
+    for (int j = 0; j < MANY; ++j) {
+      keys[j] = 0;
+      if (j * kLpThreads >= all) continue;
+      const int i = j * kLpThreads + ((threadIdx.x + 37 * j) & (kLpThreads - 1));
+      if (i < all) keys[j] = row[i];
+      high = max(high, keys[j]);
+    }
+    Key bound = 1;
+    if (all > kLpThreads)
+      bound = (Key)block_bound<low_bits<T>()>(a.top, order_in(high), peaks) << 32;
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < MANY; ++j) {
+      if (j * kLpThreads >= all) continue;
+      const uint64_t who = __ballot(keys[j] >= bound);
+      if (keys[j] >= bound) lists[w][n + lanes_before(who)] = keys[j];
       n += __popcll(who);
     }
     n = list_done<low_bits<T>()>(lists[w], n, a.top);
