@@ -33,57 +33,73 @@ __device__ __forceinline__ bool is_page(const PageTables &p, int page) {
   return (uint32_t)page < (uint32_t)p.n_pages;
 }
 
-// heir[s]: who goes on with source s's own last page: s if it stays, else the
-// lowest-numbered sequence that becomes s (INT32_MAX: nobody). In LDS.
+// What a block knows of the sequences, in LDS. heir[s]: who goes on with source s's own
+// last page: s if it stays, else the lowest-numbered sequence that becomes s (INT32_MAX:
+// nobody).
+struct Seqs {
+  int src[kMaxSeqs], held[kMaxSeqs], len[kMaxSeqs], heir[kMaxSeqs];
+};
+
 template <int NT>
-__device__ __forceinline__ void find_heirs(const PagesUpdateArgs &a, int *heir) {
+__device__ __forceinline__ void load_seqs(const PagesUpdateArgs &a, Seqs &q) {
   const int n = a.pages.n_seqs;
-  for (int s = threadIdx.x; s < n; s += NT)
-    heir[s] = source_of(a.source, n, s) == s ? s : INT32_MAX;
-  __syncthreads();
   for (int d = threadIdx.x; d < n; d += NT) {
-    const int s = source_of(a.source, n, d);
-    if (s >= 0 && s != d && source_of(a.source, n, s) != s) atomicMin(&heir[s], d);
+    const int s = source_of(a.source, n, d), held = held_of(a.pages, d);
+    q.src[d] = s;
+    q.held[d] = held;
+    q.len[d] = len_of(a.pages, d, held);
+    q.heir[d] = s == d ? d : INT32_MAX;
+  }
+  __syncthreads();
+  if (!a.source) return;
+  for (int d = threadIdx.x; d < n; d += NT) {
+    const int s = q.src[d];
+    if (s >= 0 && s != d && q.src[s] != s) atomicMin(&q.heir[s], d);
   }
   __syncthreads();
 }
 
-// Tables and counts of the sequences that change. A block takes a run of 2^shift columns
-// of the table for every sequence: it reads them all before it writes any, so that
-// sequences may change places. A page that stays partly filled is counted for its heir
-// alone; the entry of another names the page that is copied into its own below.
-constexpr int kForkThreads = 256, kForkEntries = 8192;
+// Tables and counts of the sequences that change, columns [c0, c0 + 2^shift) of all: all
+// are read before any is written, so that sequences may change places. A page that stays
+// partly filled is counted for its heir alone; the entry of another names the page that is
+// copied into its own below.
+constexpr int kForkThreads = 1024, kForkEntries = 8192;
 
-__global__ __launch_bounds__(kForkThreads) void k_fork_tables(PagesUpdateArgs a, int shift) {
-  __shared__ int heir[kMaxSeqs];
-  __shared__ int32_t fresh[kForkEntries];
+__device__ __forceinline__ void fork_tables(const PagesUpdateArgs &a, const Seqs &q, int32_t *fresh,
+                                            int c0, int shift) {
   const PageTables &p = a.pages;
-  const int n = p.n_seqs, c0 = blockIdx.x << shift, part = (1 << p.page_shift) - 1;
-  find_heirs<kForkThreads>(a, heir);
-  for (int i = threadIdx.x; i < n << shift; i += kForkThreads) {
-    const int d = i >> shift, c = c0 + (i & ((1 << shift) - 1)), s = source_of(a.source, n, d);
+  const int n = p.n_seqs << shift, part = (1 << p.page_shift) - 1;
+#pragma unroll 1
+  for (int i = threadIdx.x; i < n; i += kForkThreads) {
+    const int d = i >> shift, c = c0 + (i & ((1 << shift) - 1)), s = q.src[d];
     int page = -1;
-    if (s >= 0 && s != d && c < p.max_pages &&
-        c < pages_for(len_of(p, s, held_of(p, s)), p.page_shift))
+    if (s >= 0 && s != d && c < p.max_pages && c < pages_for(q.len[s], p.page_shift))
       page = p.table[s * p.table_stride + c];
     fresh[i] = page;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n << shift; i += kForkThreads) {
-    const int d = i >> shift, c = c0 + (i & ((1 << shift) - 1)), s = source_of(a.source, n, d);
+#pragma unroll 1
+  for (int i = threadIdx.x; i < n; i += kForkThreads) {
+    const int d = i >> shift, c = c0 + (i & ((1 << shift) - 1)), s = q.src[d];
     if (s == d || c >= p.max_pages) continue;
     int32_t *at = p.table + d * p.table_stride + c;
-    if (c < held_of(p, d)) {
+    if (c < q.held[d]) {
       const int old = *at;
       if (is_page(p, old)) atomicSub(&p.refs[old], 1);
     }
-    if (s < 0) continue;
-    const int len = len_of(p, s, held_of(p, s));
-    if (c >= pages_for(len, p.page_shift)) continue;
-    *at = fresh[i];
-    const bool full = c < len >> p.page_shift || !(len & part);
-    if ((full || heir[s] == d) && is_page(p, fresh[i])) atomicAdd(&p.refs[fresh[i]], 1);
+    if (s < 0 || c >= pages_for(q.len[s], p.page_shift)) continue;
+    const int page = fresh[i];
+    *at = page;
+    const bool full = c < q.len[s] >> p.page_shift || !(q.len[s] & part);
+    if ((full || q.heir[s] == d) && is_page(p, page)) atomicAdd(&p.refs[page], 1);
   }
+}
+
+__global__ __launch_bounds__(kForkThreads) void k_fork_tables(PagesUpdateArgs a, int shift) {
+  __shared__ Seqs q;
+  __shared__ int32_t fresh[kForkEntries];
+  load_seqs<kForkThreads>(a, q);
+  fork_tables(a, q, fresh, blockIdx.x << shift, shift);
 }
 
 // The first `rows` rows of page `from` go to the page at column `col` of sequence `seq`.
@@ -95,137 +111,157 @@ struct PageCopies {
   PageCopy at[kMaxSeqs];
 };
 
-// Exclusive prefix sum over the threads of a block, and the total.
-template <int NT>
-__device__ __forceinline__ long block_rank(long mine, long *sums, long &total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  long v = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const long o = __shfl_up(v, d);
-    if (lane >= d) v += o;
+__device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) {  // (at most 2^32 - 1)
+  return __builtin_elementwise_add_sat(a, b);
+}
+
+// Inclusive prefix sum over N lanes.
+template <int N>
+__device__ __forceinline__ uint32_t lane_sums(uint32_t v) {
+#pragma unroll 1
+  for (int d = 1; d < N; d <<= 1) {
+    const uint32_t o = __shfl_up(v, d);
+    if ((int)(threadIdx.x & 63) >= d) v = plus(v, o);
   }
+  return v;
+}
+
+// Exclusive prefix sum over the threads of a block, and the total; more than 2^32 - 1 is
+// 2^32 - 1.
+template <int NT>
+__device__ __forceinline__ uint32_t block_rank(uint32_t mine, uint32_t *sums, uint32_t &total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const uint32_t v = lane_sums<64>(mine);
   __syncthreads();
   if (lane == 63) sums[w] = v;
   __syncthreads();
-  long before = 0;
-  total = 0;
-#pragma unroll
-  for (int i = 0; i < NT / 64; ++i) {
-    if (i < w) before += sums[i];
-    total += sums[i];
-  }
-  return before + v - mine;
+  const uint32_t all = lane_sums<NT / 64>(lane < NT / 64 ? sums[lane] : 0);
+  total = __shfl(all, NT / 64 - 1);
+  const uint32_t before = __shfl(all, max(w - 1, 0)), own = __shfl_up(v, 1);
+  return plus(w ? before : 0, lane ? own : 0);
 }
 
 // The sequences' new sizes and their new pages. One block: a prefix sum of what each
-// sequence needs, then walks over the counts, one to count free pages as far as they are
-// needed, one to hand them out in order.
-constexpr int kRoomThreads = 1024, kRoomSeqs = kMaxSeqs / kRoomThreads, kRoomPages = 16;
+// sequence needs, then the free pages as far as they are needed, first counted, then
+// listed by their ranks and handed out, a thread a page.
+constexpr int kRoomThreads = 1024, kRoomPages = 16;
 
 // Bit i: page first + i is free.
 __device__ __forceinline__ uint32_t free_pages(const PageTables &p, int first) {
   typedef Pack<int32_t, 4> I4;
   uint32_t bits = 0;
   if (first + kRoomPages <= p.n_pages) {
+    I4 r[kRoomPages / 4];
 #pragma unroll
-    for (int i = 0; i < kRoomPages; i += 4) {
-      const I4 r = *reinterpret_cast<const I4 *>(p.refs + first + i);
+    for (int i = 0; i < kRoomPages / 4; ++i)
+      r[i] = *reinterpret_cast<const I4 *>(p.refs + first + 4 * i);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) bits |= (uint32_t)(r.v[j] == 0) << (i + j);
-    }
+    for (int i = 0; i < kRoomPages; ++i) bits |= (uint32_t)(r[i / 4].v[i % 4] == 0) << i;
   } else {
+#pragma unroll 1
     for (int i = 0; first + i < p.n_pages; ++i) bits |= (uint32_t)(p.refs[first + i] == 0) << i;
   }
   return bits;
 }
 
-__global__ __launch_bounds__(kRoomThreads) void k_room(PagesUpdateArgs a, PageCopies *copies) {
-  __shared__ int heir[kMaxSeqs];
-  __shared__ long first[kMaxSeqs + 1];  // rank of each sequence's first new page
-  __shared__ int kept[kMaxSeqs];        // pages it goes on with
-  __shared__ long sums[kRoomThreads / 64];
-  __shared__ int n_copies;
-  constexpr int STEP = kRoomThreads * kRoomPages;
+// What sequence d goes on with.
+struct Turn {
+  int len, kept, need;  // positions, pages, new pages
+  bool copy, fits;      // the last page is copied into the first new one; room is to be had
+};
+__device__ __forceinline__ Turn turn_of(const PagesUpdateArgs &a, const Seqs &q, int d) {
   const PageTables &p = a.pages;
-  const int n = p.n_seqs, tid = threadIdx.x, part = (1 << p.page_shift) - 1;
-  if (a.source) find_heirs<kRoomThreads>(a, heir);
+  const int s = q.src[d], part = (1 << p.page_shift) - 1;
+  Turn t;
+  t.len = s >= 0 ? q.len[s] : 0;
+  const int have = s == d ? q.held[d] : pages_for(t.len, p.page_shift);
+  t.copy = s >= 0 && s != d && (t.len & part) && q.heir[s] != d;
+  const long pages = ((long)t.len + (a.room ? max(a.room[d], 0) : 0) + part) >> p.page_shift;
+  t.fits = pages <= p.max_pages;
+  t.need = t.copy + (t.fits ? max(0, (int)pages - have) : 0);
+  t.kept = have - t.copy;
+  return t;
+}
+
+__global__ __launch_bounds__(kRoomThreads) void k_room(PagesUpdateArgs a, PageCopies *copies) {
+  constexpr int STEP = kRoomThreads * kRoomPages;
+  __shared__ Seqs q;
+  __shared__ uint32_t first[kMaxSeqs + 1];  // rank of each sequence's first new page
+  __shared__ int kept[kMaxSeqs];            // pages it goes on with
+  __shared__ uint16_t list[STEP];           // free pages by their ranks
+  __shared__ uint32_t sums[kRoomThreads / 64];
+  __shared__ int n_copies;
+  const PageTables &p = a.pages;
+  const int n = p.n_seqs, tid = threadIdx.x;
   if (tid == 0) n_copies = 0;
-  const int per = (n + kRoomThreads - 1) / kRoomThreads;
-  int need[kRoomSeqs], copy[kRoomSeqs], lens[kRoomSeqs];
-  bool fits[kRoomSeqs];
-  long mine = 0;
-#pragma unroll
-  for (int i = 0; i < kRoomSeqs; ++i) {
-    const int d = tid * per + i;
-    need[i] = copy[i] = lens[i] = 0;
-    fits[i] = true;
-    if (i >= per || d >= n) continue;
-    const int s = source_of(a.source, n, d);
-    int have = 0;
-    if (s >= 0) {
-      const int held = held_of(p, s);
-      lens[i] = len_of(p, s, held);
-      have = s == d ? held : pages_for(lens[i], p.page_shift);
-      copy[i] = s != d && (lens[i] & part) && heir[s] != d;
-    }
-    const long want = (long)lens[i] + (a.room ? max(a.room[d], 0) : 0);
-    const long pages = (want + part) >> p.page_shift;
-    fits[i] = pages <= p.max_pages;
-    need[i] = copy[i] + (fits[i] ? max(0, (int)pages - have) : 0);
-    kept[d] = have - copy[i];
-    mine += need[i];
-  }
-  long total, found = 0, rank = block_rank<kRoomThreads>(mine, sums, total);
-  for (long at = 0; at < p.n_pages && found < total; at += STEP) {
-    long all;
-    const long from = at + tid * kRoomPages;
-    block_rank<kRoomThreads>(from < p.n_pages ? __popc(free_pages(p, (int)from)) : 0, sums, all);
-    found += all;
-  }
-  // Served: all whose needs, with those before them, are met. Of a copy that is not, the
-  // full pages stay.
-#pragma unroll
-  for (int i = 0; i < kRoomSeqs; ++i) {
-    const int d = tid * per + i;
-    if (i >= per || d >= n) continue;
-    first[d] = rank;
-    rank += need[i];
-    const bool served = need[i] == 0 || rank <= found;
-    p.held[d] = kept[d] + (served ? need[i] : 0);
-    p.len[d] = copy[i] && !served ? lens[i] & ~part : lens[i];
-    if (a.ok) a.ok[d] = served && fits[i];
-    if (copy[i] && served) {  // (in any order: the copies are independent)
-      const int from = p.table[d * p.table_stride + kept[d]];
-      copies->at[atomicAdd(&n_copies, 1)] = {d, kept[d], from, lens[i] & part};
-    }
-  }
-  if (tid == 0) first[n] = total;
-  __syncthreads();
-  if (copies && tid == 0) copies->n = n_copies;
-  const long most = min(total, found);
-  for (long at = 0, before = 0; at < p.n_pages && before < most; at += STEP) {
-    long all;
-    const long from = at + tid * kRoomPages;
-    uint32_t bits = from < p.n_pages ? free_pages(p, (int)from) : 0;
-    long k = before + block_rank<kRoomThreads>(__popc(bits), sums, all);
-    for (; bits && k < most; ++k, bits &= bits - 1) {
-      // The k-th free page is the last sequence's whose first rank is not above k.
-      int lo = 0, hi = n;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (first[mid] <= k)
-          lo = mid;
-        else
-          hi = mid;
+  load_seqs<kRoomThreads>(a, q);
+  const int per = (n + kRoomThreads - 1) / kRoomThreads, d0 = tid * per, d1 = min(n, d0 + per);
+  uint32_t mine = 0, total, found, most = 0;
+#pragma unroll 1
+  for (int d = d0; d < d1; ++d) mine += turn_of(a, q, d).need;
+  uint32_t rank = block_rank<kRoomThreads>(mine, sums, total);
+  uint32_t bits = 0, k = 0, all = 0;
+#pragma unroll 1
+  for (int listing = 0; listing < 2; ++listing) {
+    uint32_t base = 0;
+    const uint32_t until = listing ? most : total;
+#pragma unroll 1
+    for (long at = 0; at < p.n_pages && base < until; at += STEP) {
+      if (!listing || at || found > all) {  // (else all that count are held here)
+        const long from = at + tid * kRoomPages;
+        bits = from < p.n_pages ? free_pages(p, (int)from) : 0;
+        k = block_rank<kRoomThreads>(__popc(bits), sums, all);
       }
-      if (first[lo + 1] > found) continue;  // not served
-      const int page = (int)from + __builtin_ctz(bits);
-      p.refs[page] = 1;
-      p.table[lo * p.table_stride + kept[lo] + (k - first[lo])] = page;
+      if (listing) {
+#pragma unroll 1
+        for (uint32_t i = k; bits && base + i < most; ++i, bits &= bits - 1)
+          list[i] = (uint16_t)(tid * kRoomPages + __builtin_ctz(bits));
+        __syncthreads();
+#pragma unroll 1
+        for (uint32_t i = tid; i < min(all, most - base); i += kRoomThreads) {
+          // The free page of that rank is the last sequence's whose first is not above it.
+          int lo = 0, hi = n;
+          while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (first[mid] <= base + i)
+              lo = mid;
+            else
+              hi = mid;
+          }
+          if (first[lo + 1] > found) continue;  // not served
+          const int page = (int)at + list[i];
+          p.refs[page] = 1;
+          p.table[lo * p.table_stride + kept[lo] + (base + i - first[lo])] = page;
+        }
+        __syncthreads();
+      }
+      base += all;
     }
-    before += all;
+    if (listing) break;
+    // Served: all whose needs, with those before them, are met. Of a copy that is not, the
+    // full pages stay.
+    found = base;
+    most = min(total, found);
+#pragma unroll 1
+    for (int d = d0; d < d1; ++d) {
+      const Turn t = turn_of(a, q, d);
+      first[d] = rank;
+      kept[d] = t.kept;
+      rank = plus(rank, t.need);
+      const bool served = t.need == 0 || rank <= found;
+      const int part = t.len & ((1 << p.page_shift) - 1);
+      p.held[d] = t.kept + (served ? t.need : 0);
+      p.len[d] = t.copy && !served ? t.len - part : t.len;
+      if (a.ok) a.ok[d] = served && t.fits;
+      if (t.copy && served) {  // (in any order: the copies are independent)
+        const int from = p.table[d * p.table_stride + t.kept];
+        copies->at[atomicAdd(&n_copies, 1)] = {d, t.kept, from, part};
+      }
+    }
+    if (tid == 0) first[n] = total;
+    __syncthreads();
   }
+  if (copies && tid == 0) copies->n = n_copies;
 }
 
 // Bytes [at, at + sizeof(U)) of row `slot` of one head.
@@ -234,22 +270,24 @@ __device__ __forceinline__ U *row_at(char *base, long slot_stride, long slot, lo
   return reinterpret_cast<U *>(base + slot * slot_stride + at);
 }
 
-// The copied rows in every layer: units (copy, layer, matrix, head) in turn.
+// The copied rows in every layer. Grid (layers, matrices and heads in turn; copies).
 template <typename U>
 __global__ __launch_bounds__(256) void k_copy_pages(PageTables p, CacheRows c,
                                                     const PageCopies *copies) {
-  const long per = 2L * c.n_layers * c.n_heads, units = copies->n * per;
+  const int per = 2 * c.n_layers * c.n_heads, n = copies->n;
   const int pieces = (int)(c.row / sizeof(U));
-  for (long u = blockIdx.x; u < units; u += gridDim.x) {
-    const PageCopy x = copies->at[u / per];
-    const int i = (int)(u % per), head = i % c.n_heads, layer = i / (2 * c.n_heads);
+  for (int u = blockIdx.y; u < n; u += gridDim.y) {
+    const PageCopy x = copies->at[u];
     const int to = p.table[x.seq * p.table_stride + x.col];
     if (!is_page(p, x.from) || !is_page(p, to)) continue;
-    char *base = (i / c.n_heads & 1 ? c.v : c.k) + layer * c.layer_stride + head * c.head_stride;
     const long a = (long)x.from << p.page_shift, b = (long)to << p.page_shift;
-    for (int k = threadIdx.x; k < x.rows * pieces; k += 256) {
-      const int r = k / pieces, at = (k % pieces) * (int)sizeof(U);
-      *row_at<U>(base, c.slot_stride, b + r, at) = *row_at<U>(base, c.slot_stride, a + r, at);
+    for (int i = blockIdx.x; i < per; i += gridDim.x) {
+      const int head = i % c.n_heads, layer = i / (2 * c.n_heads);
+      char *base = (i / c.n_heads & 1 ? c.v : c.k) + layer * c.layer_stride + head * c.head_stride;
+      for (int k = threadIdx.x; k < x.rows * pieces; k += 256) {
+        const int r = k / pieces, at = (k % pieces) * (int)sizeof(U);
+        *row_at<U>(base, c.slot_stride, b + r, at) = *row_at<U>(base, c.slot_stride, a + r, at);
+      }
     }
   }
 }
@@ -279,30 +317,26 @@ __device__ __forceinline__ void bounds_of(const PageTables &p, int s, int &len, 
   len = len_of(p, s, held);
 }
 
-// A wave moves a slice of 64 pieces of the rows of one (sequence, layer, matrix, head).
+// Grid ((layer, matrix, head, slice) / 4, sequence): a wave moves a slice of 64 pieces of
+// the rows.
 // Rows move to lower places only, and rise: eight are read, then written, then the next,
 // and no row is written that a later one is read from.
 template <typename U>
-__global__ __launch_bounds__(256) void k_keep_rows(PagesKeepArgs a, int slices, long units) {
+__global__ __launch_bounds__(256) void k_keep_rows(PagesKeepArgs a, int slices, int units) {
   const PageTables &p = a.pages;
   const CacheRows &c = a.cache;
   const int lane = threadIdx.x & 63;
-  const long u = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int u = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), s = blockIdx.y;
   if (u >= units) return;
-  const int slice = (int)(u % slices);
-  const long v = u / slices;
-  const int head = (int)(v % c.n_heads), kv = (int)(v / c.n_heads % 2);
-  const int layer = (int)(v / c.n_heads / 2 % c.n_layers);
-  const int s = (int)(v / c.n_heads / 2 / c.n_layers);
+  const int v = u / slices, slice = u - v * slices, vh = v / c.n_heads, head = v - vh * c.n_heads;
+  const int kv = vh & 1, layer = vh >> 1;
   int len, room;
   bounds_of(p, s, len, room);
   const int n = kept_of(a, s, len, room);
-  if (a.len_out != p.len && !a.release && v == (long)s * c.n_layers * 2 * c.n_heads &&
-      slice == 0 && lane == 0)
-    a.len_out[s] = len + n;
+  if (a.len_out != p.len && !a.release && u == 0 && lane == 0) a.len_out[s] = len + n;
   const int32_t *kept = a.kept + s * a.kept_stride, *table = p.table + s * p.table_stride;
   char *base = (kv ? c.v : c.k) + layer * c.layer_stride + head * c.head_stride;
-  const long piece = ((long)slice * 64 + lane) * sizeof(U);
+  const int piece = (slice * 64 + lane) * (int)sizeof(U);
   const bool in = piece < c.row;
   for (int k0 = 0; k0 < n; k0 += 64) {
     // Lane k: where row k0 + k comes from and goes to (-1: it stays).
@@ -371,8 +405,8 @@ CacheRows merged(CacheRows c) {
 template <typename U>
 hipError_t launch_keep_rows(const PagesKeepArgs &a, hipStream_t s) {
   const int slices = (int)((a.cache.row / (long)sizeof(U) + 63) / 64);
-  const long units = 2L * a.pages.n_seqs * a.cache.n_layers * a.cache.n_heads * slices;
-  k_keep_rows<U><<<(int)((units + 3) / 4), 256, 0, s>>>(a, slices, units);
+  const int units = 2 * a.cache.n_layers * a.cache.n_heads * slices;
+  k_keep_rows<U><<<dim3((units + 3) / 4, a.pages.n_seqs), 256, 0, s>>>(a, slices, units);
   return hipGetLastError();
 }
 
@@ -384,9 +418,10 @@ size_t pages_update_workspace_bytes(int n_seqs) {
 
 hipError_t launch_pages_update(const PagesUpdateArgs &a, void *ws, hipStream_t s) {
   PageCopies *copies = a.source ? static_cast<PageCopies *>(ws) : nullptr;
+  const int n = a.pages.n_seqs;
   if (a.source) {
-    int shift = 0;
-    while (shift < 4 && a.pages.n_seqs << (shift + 1) <= kForkEntries) ++shift;
+    int shift = 0;  // (16 columns are a line of the table.)
+    while (shift < 4 && n << (shift + 1) <= kForkEntries) ++shift;
     k_fork_tables<<<((a.pages.max_pages - 1) >> shift) + 1, kForkThreads, 0, s>>>(a, shift);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -395,8 +430,8 @@ hipError_t launch_pages_update(const PagesUpdateArgs &a, void *ws, hipStream_t s
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.source) return e;
   const CacheRows c = merged(a.cache);
-  const long units = 2L * a.pages.n_seqs * c.n_layers * c.n_heads;
-  const int grid = (int)std::min(units, 2048L);
+  const int across = std::min(2 * c.n_layers * c.n_heads, 1024);
+  const dim3 grid(across, std::min(n, std::max(1, 2048 / across)));
   switch (piece_bytes(c)) {
     case 16:
       k_copy_pages<u32x4><<<grid, 256, 0, s>>>(a.pages, c, copies);
