@@ -1,5 +1,6 @@
 """Refusals of the paged-cache operators: every check runs before the device is touched,
 so the pointers below are never dereferenced; calls that pass have nothing to do."""
+import contextlib
 import ctypes
 import os
 
@@ -222,6 +223,58 @@ def test_the_binding_refuses_what_the_library_cannot_see():
         with pytest.raises(B.VsrError) as e:
             f()
         assert e.value.code == B.VSR_EINVAL, i
+
+
+class _Fine:
+    """A library whose calls all succeed and whose sizes are 64."""
+
+    def __getattr__(self, name):
+        return lambda *a: 64 if name.endswith("size") else 0
+
+
+def test_calls_on_a_given_stream_hold_their_tensors(monkeypatch):
+    torch = pytest.importorskip("torch")
+    seen = []
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    monkeypatch.setattr(B, "_hold", lambda stream, *ts: seen.append((stream, ts)))
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    B._torch_names()
+    for name, value in (("_lib", _Fine()), ("_device_now", lambda: 0), ("_raw_stream", lambda d: 0)):
+        monkeypatch.setattr(B, name, value)
+    stream = type("Stream", (), {"device_index": 0, "cuda_stream": 0})()
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    p = B.pages(**_tables(torch), page_size=4)
+    tables = [p.table, p.len, p.held, p.refs]
+    q, k, v = torch.ones(6, 4, 8), torch.ones(80, 2, 8), torch.ones(80, 2, 8)
+    k4, v4 = torch.ones(2, 80, 2, 8), torch.ones(2, 80, 2, 8)
+    start, parent, shift, mask = i32(4), i32(6), i32(3), i32(6, 1)
+    rows, ws = (i32(6), i32(6), i32(6, 1)), torch.ones(64, dtype=torch.uint8)
+    out, lse, source, room, ok = torch.ones(6, 4, 8), torch.ones(6, 4), i32(3), i32(3), i32(3)
+    kept, n_kept, length = i32(3, 2), i32(3), i32(3)
+    x, ids = torch.ones(3, 100), i32(3)
+    lp = torch.ones(3), i32(3), torch.ones(3), i32(3, 2), torch.ones(3, 2)
+    calls = [(lambda s: B.tree_rows(p, start, parent, shift, out=rows, stream=s),
+              [*tables, start, parent, shift, *rows]),
+             (lambda s: B.tree_attention(p, q, k, v, 1.0, start, mask, out, lse, ws, s),
+              [*tables, q, k, v, start, mask, out, lse, ws]),
+             (lambda s: B.pages_update(p, source, room, k4, v4, ok, ws, s),
+              [*tables, source, room, k4, v4, ok, ws]),
+             (lambda s: B.pages_keep(p, kept, n_kept, k4, v4, length, stream=s),
+              [*tables, kept, n_kept, k4, v4, length]),
+             (lambda s: B.token_logprobs(x, ids, 2, lp, ws, s), [x, ids, *lp, ws]),
+             # What a call makes for itself is held too.
+             (lambda s: B.tree_attention(p, q, k, v, 1.0, start, mask, stream=s),
+              [*tables, q, k, v, start, mask])]
+    for i, (call, tensors) in enumerate(calls):
+        seen.clear()
+        call(None)  # (the current stream's own order holds them)
+        assert not seen, i
+        call(stream)
+        assert all(s is stream for s, _ in seen), i
+        held = [id(t) for _, ts in seen for t in ts if t is not None]
+        assert set(map(id, tensors)) <= set(held), i
+        if i == len(calls) - 1:
+            assert len(held) == len(tensors) + 2  # (the result and the workspace)
 
 
 def test_plain_forms_by_hand():
