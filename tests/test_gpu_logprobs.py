@@ -114,6 +114,23 @@ def test_orders_that_rise_fall_and_tie(dtype):
         _check(x[:27], t[:27], top, [o[:27] for o in got])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_segments(dtype):
+    """Whole rows of 18 tiles in one segment: spans of two tiles."""
+    torch = _torch()
+    V = 70001
+    x, t = _inputs(torch, 1030, V, dtype, 5)
+    i = torch.arange(V, device="cuda", dtype=torch.float32)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    few = torch.randint(0, 4, (V,), generator=g, device="cuda").float()
+    odd = [i / 7000, -i / 7000, 0 * i, few, (i % 8192 < 40).float(), (i % 4096 == 4095).float() - 1,
+           torch.where(i > V - 50, 3.0, few), torch.where(i % 2 == 0, -float("inf"), few)]
+    x[:len(odd)] = torch.stack(odd).to(x.dtype)
+    for top in (1, 20, 64):
+        got = _run(torch, x, t, top)
+        _check(x[:20], t[:20], top, [o[:20] for o in got])
+
+
 def test_nothing_nan_and_infinity():
     torch = _torch()
     inf, nan = float("inf"), float("nan")

@@ -353,6 +353,25 @@ def test_many_sequences_and_long_ones():
     c.check(*c.run())
 
 
+@pytest.mark.parametrize("dtype,hd", [("f16", 128), ("bf16", 64), ("f32", 80)])
+def test_many_sequences_of_many_rows(dtype, hd):
+    torch = _torch()
+    rng = np.random.default_rng(23)
+    rows = rng.integers(0, 40, 100)
+    rows[[0, 50, 99]] = 0, 140, 1
+    c = Case(torch, rng.integers(0, 300, 100), rows, 8, 2, hd, 16, dtype, True, seed=24)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+def test_scales(scale):
+    torch = _torch()
+    for rows in (1, 3, 60):
+        c = Case(torch, [300, 40], [rows, rows + 1], 4, 2, 64, 16, "bf16", True, seed=rows)
+        c.scale = scale
+        c.check(*c.run())
+
+
 def test_a_captured_call_follows_its_inputs():
     """One graph over changing lengths, starts and masks, with eager work between."""
     torch = _torch()
