@@ -568,11 +568,12 @@ def rotary(sections: Sequence[int], base: float, interleaved: bool = False) -> V
 _float_types = None  # torch float dtype -> VSR_*
 _raw_stream = None   # device index -> its current stream's handle
 _device_now = None   # -> the current device's index
+_int32 = None        # torch.int32
 
 
 def _torch_names():
     """torch (imported on first use), with the library and the names above set."""
-    global _float_types, _raw_stream, _device_now
+    global _float_types, _raw_stream, _device_now, _int32
     import torch
     if _float_types is None:
         load_library()
@@ -580,6 +581,7 @@ def _torch_names():
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
         _device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        _int32 = torch.int32
         # Set last: another thread that finds it set finds the rest set too.
         _float_types = {torch.float32: VSR_F32, torch.bfloat16: VSR_BF16, torch.float16: VSR_F16}
     return torch
@@ -871,28 +873,24 @@ class Pages:
     """A paged cache's tables (vsr_pages): the tensors and what they hold."""
 
     def __init__(self, table, len, held, refs, page_size: int):
-        torch = _torch_names()
-        i32, dev = torch.int32, table.get_device()
-        if table.dtype is not i32 or table.dim() != 2 or \
-                (table.shape[1] > 1 and table.stride(1) != 1):
+        i32, dev = _torch_names().int32, table.get_device()
+        if table.dtype is not i32 or table.dim() != 2:
             raise VsrError(VSR_EINVAL, "table: int32 [n_seqs][max_pages] rows expected")
         seqs, most = table.shape
-        for t in (len, held):
-            if t.dtype is not i32 or t.shape != (seqs,) or t.stride(0) != 1 and seqs > 1 or \
-                    t.get_device() != dev:
-                raise VsrError(VSR_EINVAL, "len, held: contiguous int32 [n_seqs] on the table's "
-                                           "device expected")
-        if refs.dtype is not i32 or refs.dim() != 1 or not refs.is_contiguous() or \
-                refs.get_device() != dev:
-            raise VsrError(VSR_EINVAL, "refs: contiguous int32 [n_pages] on the table's device "
-                                       "expected")
+        rows, step = table.stride()
+        if most > 1 and step != 1:
+            raise VsrError(VSR_EINVAL, "table: int32 [n_seqs][max_pages] rows expected")
+        n_pages = refs.numel()
+        at = [_int_rows(t, n, dev, what) for t, n, what in
+              ((len, seqs, "len"), (held, seqs, "held"), (refs, n_pages, "refs"))]
+        if not len.dim() == held.dim() == refs.dim() == 1:
+            raise VsrError(VSR_EINVAL, "len, held, refs: one dimension expected")
         self.table, self.len, self.held, self.refs = table, len, held, refs
-        self.n_seqs, self.max_pages, self.n_pages, self.page_size = seqs, most, refs.shape[0], \
+        self.n_seqs, self.max_pages, self.n_pages, self.page_size = seqs, most, n_pages, \
             int(page_size)
         self.device_index = dev
-        self.c = VsrPages(seqs, self.n_pages, self.page_size, most, table.data_ptr(),
-                          table.stride(0) if seqs > 1 else most, len.data_ptr(), held.data_ptr(),
-                          refs.data_ptr())
+        self.c = VsrPages(seqs, n_pages, self.page_size, most, table.data_ptr(),
+                          rows if seqs > 1 else most, *at)
 
     def tensors(self):
         return self.table, self.len, self.held, self.refs
@@ -911,8 +909,7 @@ def _int_rows(t, n, dev, what):
     """Pointer of a contiguous int32 [n] tensor, or None."""
     if t is None:
         return None
-    if t.dtype is _torch_names().int32 and t.numel() == n and t.is_contiguous() and \
-            t.get_device() == dev:
+    if t.dtype is _int32 and t.numel() == n and t.is_contiguous() and t.get_device() == dev:
         return t.data_ptr()
     raise VsrError(VSR_EINVAL, f"{what}: contiguous int32 [{n}] on the pages' device expected")
 
@@ -921,7 +918,7 @@ def _mask_rows(mask, T, dev):
     """(pointer, row stride, words) of int32 [T][words] rows."""
     if mask is None:
         return None, 0, 0
-    if mask.dim() == 2 and mask.dtype is _torch_names().int32 and mask.get_device() == dev:
+    if mask.dim() == 2 and mask.dtype is _int32 and mask.get_device() == dev:
         n, words = mask.shape
         stride, step = mask.stride()
         if n == T and (step == 1 or words == 1):
