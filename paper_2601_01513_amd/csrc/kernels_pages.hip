@@ -210,19 +210,21 @@ __global__ __launch_bounds__(kRoomThreads) void k_room(PagesUpdateArgs a, PageCo
   const int per = (n + kRoomThreads - 1) / kRoomThreads, d0 = tid * per, d1 = min(n, d0 + per);
   uint32_t mine = 0, total, found, most = 0;
 #pragma unroll 1
-  for (int d = d0; d < d1; ++d) mine += turn_of(a, q, d).need;
+  for (int d = d0; d < d1; ++d) mine = plus(mine, turn_of(a, q, d).need);
   uint32_t rank = block_rank<kRoomThreads>(mine, sums, total);
   uint32_t bits = 0, k = 0, all = 0;
+  int walked = 0;
 #pragma unroll 1
   for (int listing = 0; listing < 2; ++listing) {
     uint32_t base = 0;
     const uint32_t until = listing ? most : total;
 #pragma unroll 1
     for (long at = 0; at < p.n_pages && base < until; at += STEP) {
-      if (!listing || at || found > all) {  // (else all that count are held here)
+      if (!listing || walked > 1) {  // (else what was counted is held here)
         const long from = at + tid * kRoomPages;
         bits = from < p.n_pages ? free_pages(p, (int)from) : 0;
         k = block_rank<kRoomThreads>(__popc(bits), sums, all);
+        walked += !listing;
       }
       if (listing) {
 #pragma unroll 1

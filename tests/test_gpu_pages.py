@@ -161,6 +161,19 @@ def test_many_pages():
     c.update([1, 2, 0], [0, 0, 30000])
 
 
+@pytest.mark.parametrize("first", [0, 16383, 16384, 16385, 40000, 99990])
+def test_the_first_free_page_far_up(first):
+    """None free in a walk's first steps, a few in a later one."""
+    torch = _torch()
+    c = Cache(torch, 3, 8, 100000, 1, shape=(1, 1, 2))
+    c.refs[:first] = 1
+    c.to_device()
+    c.refs = c.refs.copy()
+    assert c.update(room=[2, 1, 3]).all()
+    assert c.table[0, 0] == first and c.table[2, 2] == first + 5
+    c.update([0, 0, 1], [1, 0, 0])
+
+
 def test_kept_rows():
     torch = _torch()
     for apart, release in ((False, True), (False, False), (True, False), (True, True)):
