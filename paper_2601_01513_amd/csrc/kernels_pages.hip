@@ -289,7 +289,9 @@ template <typename U>
 __global__ __launch_bounds__(256) void k_copy_pages(PageTables p, CacheRows c,
                                                     const PageCopies *copies) {
   const int per = 2 * c.n_layers * c.n_heads, n = copies->n;
-  const int pieces = (int)(c.row / sizeof(U));
+  // A row's pieces by `across` threads, as many rows at once as the block has room for.
+  const int pieces = (int)(c.row / sizeof(U)), across = min(pieces, 256), rows = 256 / across;
+  const int r0 = threadIdx.x / across, k0 = threadIdx.x - r0 * across;
   for (int u = blockIdx.y; u < n; u += gridDim.y) {
     const PageCopy x = copies->at[u];
     const int to = p.table[x.seq * p.table_stride + x.col];
@@ -298,10 +300,10 @@ __global__ __launch_bounds__(256) void k_copy_pages(PageTables p, CacheRows c,
     for (int i = blockIdx.x; i < per; i += gridDim.x) {
       const int head = i % c.n_heads, layer = i / (2 * c.n_heads);
       char *base = (i / c.n_heads & 1 ? c.v : c.k) + layer * c.layer_stride + head * c.head_stride;
-      for (int k = threadIdx.x; k < x.rows * pieces; k += 256) {
-        const int r = k / pieces, at = (k % pieces) * (int)sizeof(U);
-        *row_at<U>(base, c.slot_stride, b + r, at) = *row_at<U>(base, c.slot_stride, a + r, at);
-      }
+      for (int r = r0; r0 < rows && r < x.rows; r += rows)
+        for (int k = k0; k < pieces; k += across)
+          *row_at<U>(base, c.slot_stride, b + r, (long)k * sizeof(U)) =
+              *row_at<U>(base, c.slot_stride, a + r, (long)k * sizeof(U));
     }
   }
 }
