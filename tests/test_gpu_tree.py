@@ -175,6 +175,22 @@ def test_rows_of_trees(lens, rows, page, words, parents):
     assert none is None and torch.equal(pos, out[0]) and torch.equal(slot, out[1])
 
 
+@pytest.mark.parametrize("n,words,step", [(70001, 2, 1), (3000, 94, 1), (2500, 80, 300), (1100, 33, 7)])
+def test_long_paths_in_time(n, words, step):
+    """Paths of thousands of rows, through every group of rows or past most of them."""
+    torch = _torch()
+    from paper_2601_01513_amd import binding as B
+    i32 = lambda x: torch.tensor(np.asarray(x, np.int32), device="cuda")  # noqa: E731
+    table, start = np.zeros((2, 1), np.int32), np.array([0, 3, n + 3], np.int32)
+    parent = np.concatenate([[-1, 0, 1], np.arange(n) - step]).astype(np.int32)
+    p = B.pages(i32(table), i32([4, 5]), i32([1, 1]), i32([1]), 64)
+    pos, slot, mask = B.tree_rows(p, i32(start), i32(parent), words=words)
+    torch.cuda.synchronize()
+    want = PT.tree_rows(table, [4, 5], [1, 1], 64, start, parent, n + 3, words, n_pages=1)
+    for got, w in zip((pos, slot, mask), want):
+        assert np.array_equal(got.cpu().numpy(), w.view(np.int32))
+
+
 def test_rows_without_room_or_on_bad_pages():
     torch = _torch()
     c = Case(torch, [20, 30, 40], [10, 10, 10], 1, 1, 8, 8, "f32", False, seed=5)
