@@ -507,7 +507,8 @@ size_t vsr_tree_attention_workspace_size(int32_t dtype, int32_t head_dim, int32_
  *   workspace : device, >= vsr_tree_attention_workspace_size bytes, 256-byte
  *            aligned, caller-owned; calls that overlap in time need their own (two
  *            captured graphs that share one must not replay at once).
- * out must not overlap q, k, v or itself. n_heads % n_kv_heads == 0, n_heads <= 4096;
+ * out must not overlap q, k, v or itself, lse and the workspace no input and not each
+ * other. n_heads % n_kv_heads == 0, n_heads <= 4096;
  * 1 <= head_dim <= 256; 0 <= T <= 2^24, T n_heads < 2^31 - 256; scale finite.
  * pages->refs may be NULL.
  * Enqueued on hip_stream, whose device must be the current one; errors via

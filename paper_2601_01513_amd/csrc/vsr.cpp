@@ -1974,9 +1974,20 @@ extern "C" int vsr_tree_attention(const vsr_pages *pages, int32_t dtype, int32_t
     if (const char *m = mask_error(mask, mask_stride, mask_words)) return m;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))
       return "workspace must be non-NULL and 256-byte aligned";
-    if (ws_bytes < vsr_tree_attention_workspace_size(dtype, head_dim, T, pages->n_seqs, q->n_heads,
-                                                     k->n_heads))
-      return "workspace smaller than vsr_tree_attention_workspace_size";
+    const size_t need = vsr_tree_attention_workspace_size(dtype, head_dim, T, pages->n_seqs,
+                                                          q->n_heads, k->n_heads);
+    if (ws_bytes < need) return "workspace smaller than vsr_tree_attention_workspace_size";
+    const size_t seqs = pages->n_seqs, lse_bytes = (size_t)T * q->n_heads * 4;
+    const struct {
+      const void *p;
+      size_t n;
+    } ints[] = {{pages->table, ((seqs - 1) * pages->table_stride + pages->max_pages) * 4},
+                {pages->len, seqs * 4}, {pages->held, seqs * 4}, {start, seqs * 4 + 4},
+                {mask, mask ? mask_bytes(T, mask_stride, mask_words) : 0}};
+    for (const auto &x : ints)
+      if (ranges_meet(lse, lse_bytes, x.p, x.n) || ranges_meet(workspace, need, x.p, x.n))
+        return "lse or workspace overlaps an input";
+    if (ranges_meet(lse, lse_bytes, workspace, need)) return "lse overlaps the workspace";
     return nullptr;
   };
   if (const char *msg = check()) return refuse(VSR_EINVAL, "tree_attention", msg);

@@ -98,6 +98,8 @@ def _h(p, n=8, ts=512, hs=64):
     (dict(out=_h(6 * MB + 4096)), "overlaps v"), (dict(words=0), "mask_words"),
     (dict(stride=1), "mask_stride"), (dict(mask=8 * MB + 2), "mask"), (dict(lse=10 * MB + 2), "lse"),
     (dict(ws=None), "workspace"), (dict(ws=11 * MB + 128), "workspace"), (dict(wsb=4096), "smaller"),
+    (dict(lse=8 * MB + 64), "lse or workspace"), (dict(lse=2 * MB), "lse or workspace"),
+    (dict(ws=8 * MB), "lse or workspace"), (dict(lse=11 * MB + 512), "lse overlaps"),
 ])
 def test_tree_attention_refuses(kw, word):
     _message("tree_attention", _attend(**kw), word)
