@@ -410,10 +410,10 @@ size_t vsr_token_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t to
  *             (two captured graphs that share one must not replay at once).
  * A NaN or +inf in a row makes its log-probabilities and entropy NaN (NaN is never
  * among the likeliest). A row of -inf alone: log-probabilities -inf, entropy 0.
- * Statistics in fp32, those of the likeliest token to its relative accuracy. Outputs
- * must not overlap inputs or each other. 0 <= rows <= 65535 (0: nothing is done), 1 <=
- * vocab <= 2^24, 0 <= top <= VSR_MAX_TOP. Enqueued on hip_stream, whose device must be
- * the current one; errors via vsr_last_error(NULL). */
+ * Statistics in fp32, those of the likeliest token to its relative accuracy. Outputs and
+ * the workspace must not overlap inputs or each other. 0 <= rows <= 65535 (0: nothing
+ * is done), 1 <= vocab <= 2^24, 0 <= top <= VSR_MAX_TOP. Enqueued on hip_stream,
+ * whose device must be the current one; errors via vsr_last_error(NULL). */
 #define VSR_MAX_TOP 64
 int vsr_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,
                        int64_t stride, const int32_t *tokens, int32_t top, float *logprob,
@@ -552,8 +552,9 @@ size_t vsr_pages_update_workspace_size(int32_t n_seqs);
  *   workspace : device, >= vsr_pages_update_workspace_size(n_seqs) bytes, 16-byte
  *            aligned, caller-owned (used with source alone, else it may be NULL).
  * Table entries past held are left as they are. A table entry outside [0, n_pages)
- * is neither counted nor copied. Arrays must not overlap. Enqueued on hip_stream,
- * whose device must be the current one; errors via vsr_last_error(NULL). */
+ * is neither counted nor copied. Arrays must not overlap, nor the workspace any.
+ * Enqueued on hip_stream, whose device must be the current one; errors via
+ * vsr_last_error(NULL). */
 int vsr_pages_update(const vsr_pages *pages, const int32_t *source, const int32_t *room,
                      const vsr_cache *cache, int32_t *ok, void *workspace, size_t ws_bytes,
                      void *hip_stream);

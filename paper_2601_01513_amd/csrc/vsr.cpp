@@ -2102,8 +2102,13 @@ extern "C" int vsr_pages_update(const vsr_pages *pages, const int32_t *source,
     if (const char *m = cache_error(cache, (long)pages->n_pages * pages->page_size)) return m;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))
       return "workspace must be non-NULL and 16-byte aligned";
-    if (ws_bytes < pages_update_workspace_bytes(pages->n_seqs))
-      return "workspace smaller than vsr_pages_update_workspace_size";
+    const size_t need = pages_update_workspace_bytes(pages->n_seqs);
+    if (ws_bytes < need) return "workspace smaller than vsr_pages_update_workspace_size";
+    const IntArray mine[] = {{pages->table, (n - 1) * pages->table_stride + pages->max_pages},
+                             {pages->len, n}, {pages->held, n}, {pages->refs, (size_t)pages->n_pages},
+                             {source, n}, {room, n}, {ok, n}};
+    for (const IntArray &x : mine)
+      if (ranges_meet(workspace, need, x.p, x.n * 4)) return "the workspace overlaps another array";
     return nullptr;
   };
   if (const char *msg = check()) return refuse(VSR_EINVAL, "pages_update", msg);
@@ -2175,8 +2180,10 @@ extern "C" int vsr_token_logprobs(const void *logits, int32_t dtype, int32_t row
       for (int j = i + 1; j < 7; ++j)
         if (ranges_meet(all[i].p, all[i].n, all[j].p, all[j].n)) return "an output overlaps another array";
     if (reinterpret_cast<uintptr_t>(workspace) & 15) return "workspace must be 16-byte aligned";
-    if (ws_bytes < logprobs_workspace_bytes(rows, vocab, top))
-      return "workspace smaller than vsr_token_logprobs_workspace_size";
+    const size_t need = logprobs_workspace_bytes(rows, vocab, top);
+    if (ws_bytes < need) return "workspace smaller than vsr_token_logprobs_workspace_size";
+    for (const auto &x : all)
+      if (ranges_meet(workspace, need, x.p, x.n)) return "the workspace overlaps another array";
     return nullptr;
   };
   if (const char *msg = check()) return refuse(VSR_EINVAL, "token_logprobs", msg);

@@ -31,6 +31,7 @@ def _call(**kw):
     (dict(rank=3 * MB + 12), "overlaps"), (dict(top_logprob=3 * MB + 380), "overlaps"),
     (dict(entropy=2 * MB + 4), "overlaps"), (dict(logprob=MB + 7996), "overlaps"),
     (dict(ws=4 * MB + 8), "workspace"), (dict(wsb=64), "smaller"),
+    (dict(ws=MB + 4096), "workspace overlaps"), (dict(ws=3 * MB + 512), "workspace overlaps"),
 ])
 def test_refuses(kw, word):
     assert _call(**kw) == B.VSR_EINVAL

@@ -141,6 +141,7 @@ def _update(pages="own", cache="own", **kw):
     (dict(ok=2 * MB + 130), "aligned"), (dict(room=2 * MB), "overlap"), (dict(ok=MB + 4096), "overlap"),
     (dict(source=MB + 8), "overlap"), (dict(room=MB + 8192 + 396), "overlap"), (dict(len=MB + 156), "overlap"),
     (dict(ws=None), "workspace"), (dict(ws=3 * MB + 8), "workspace"), (dict(wsb=79), "smaller"),
+    (dict(ws=MB + 8192), "workspace overlaps"), (dict(ws=2 * MB), "workspace overlaps"),
 ])
 def test_pages_update_refuses(kw, word):
     _message("pages_update", _update(**kw), word)
