@@ -14,6 +14,10 @@
 // entries reach, and the entries that do are in spans of lanes whose largest does (little
 // more than `top` of them): these are read again for the candidates. Segments are merged
 // by a second kernel.
+//
+// 512 rows of 152064 bf16 (156 MB) with 20 alternatives: 44 + 5 us, 36 without (4.3 TB/s:
+// memory and the exponentials together); candidates kept inside the loop took 76 + 5. 3
+// rows of 151936 fp32: 8 + 7, a launch's way twice.
 #include <algorithm>
 #include <type_traits>
 
@@ -489,6 +493,8 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs_merge(LogprobArgs a, in
   }
 }
 
+// Segments to fill the chip four blocks a CU: for 512, 1024, 1280, 2048 blocks 48, 43, 51,
+// 50 us (512 rows of 152064 bf16, 20 alternatives), 117, 117, 127, 128 (1024 rows, fp32).
 struct Segments {
   int n, tiles;
 };
