@@ -498,7 +498,8 @@ size_t vsr_tree_attention_workspace_size(int32_t dtype, int32_t head_dim, int32_
  *   q, out : [T][n_heads][head_dim]; k, v : [n_pages page_size slots][n_kv_heads]
  *            [head_dim] of one layer, token_stride from slot to slot;
  *            all of dtype (VSR_F32, VSR_BF16, VSR_F16; 16-bit ones round the
- *            probabilities to it), element-aligned; 16-byte aligned keys and values
+ *            probabilities to it: to half a step, in fp16 below 2^-21 of the
+ *            row's largest to 2^-32 of that), element-aligned; 16-byte aligned keys and values
  *            with strides and head_dim to match are read faster;
  *   start  : as vsr_tree_rows; rows of no sequence are left as they are;
  *   mask   : device rows of mask_words words, mask_stride words apart, or NULL;

@@ -110,6 +110,11 @@ struct TreeShape {
   static constexpr int TILE = BK * CH;       // chunks of a K or V tile
   // Blocks a CU: by LDS, and two waves a SIMD.
   static constexpr int PER_CU = NW == 4 && 4 * TILE * 16 <= 72 << 10 ? 2 : 1;
+  // Probabilities are held 2^LIFT times as large: at most 2^(8 + LIFT), which fits an fp16,
+  // whose smallest numbers then reach 2^-31 of the likeliest key and full digits 2^-21. (At
+  // 2^0 a key below 2^-25 counted for nothing, and long contexts behind one strong key
+  // lost all their other keys.)
+  static constexpr float LIFT = std::is_same<T, f16>::value ? 7.f : 0.f;
   static_assert(KW >= 1 && NL >= 1, "each wave has keys, each thread a load");
   static_assert(NW * 16 * HD * 4 <= 4 * TILE * 16, "a row group of each wave fits the ring");
 };
@@ -714,14 +719,15 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float y = x[rt][t][i] * c;
-          x[rt][t][i] = y - ref;
+          x[rt][t][i] = (y - ref) + S::LIFT;
         }
       asm volatile("");  // (or the products are taken out of the branch)
     } else {
+      const float low = ref - S::LIFT;
 #pragma unroll
       for (int t = 0; t < S::KW; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[rt][t][i] = __builtin_fmaf(x[rt][t][i], c, -ref);
+        for (int i = 0; i < 4; ++i) x[rt][t][i] = __builtin_fmaf(x[rt][t][i], c, -low);
     }
     float sum = 0.f;
 #pragma unroll
@@ -843,7 +849,8 @@ __device__ __forceinline__ void put_row(const TreeAttnArgs &a, const Work &w, in
   }
   if (c == 0 && a.lse)
     a.lse[(long)(w.b + j) * a.n_heads + h] =
-        l == 0.f ? -INFINITY : (top + __builtin_log2f(l)) * 0.69314718055994531f;
+        l == 0.f ? -INFINITY
+                 : (top + (__builtin_log2f(l) - S::LIFT)) * 0.69314718055994531f;
 }
 
 // An item's rows stored (put_row), a group of each wave after the other, through the ring's
