@@ -1,5 +1,5 @@
 """What vsr_tree_attention's 16-bit probabilities hold: few strong keys before very many
-weak ones, and values that are all alike. Against the formula in 64 bits.
+weak ones, maxima that rise and fall. Against the formula in 64 bits.
 
 Bound of an output behind many keys, fp16, u = 2^-11 half a step, K keys, V the largest
 |v|: a probability is held relative to a reference that no score passes by more than 2^8,
