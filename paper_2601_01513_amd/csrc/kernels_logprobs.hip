@@ -8,12 +8,12 @@
 // has nearly all the mass.
 //
 // A block takes a segment of a row, each of its waves 1024 entries of every 4096. A wave
-// holds one reference, the largest value it has met; most tiles have none as large, and
-// pass without a word about the one left out. Lanes keep the largest of what they read,
-// and of each span of tiles. The top-th largest of a block's 256 is a bound that `top`
-// entries reach, and the entries that do are in spans of lanes whose largest does (little
-// more than `top` of them): these are read again for the candidates. Segments are merged
-// by a second kernel.
+// holds the largest value it has met, and a reference near it for the exponentials; most
+// tiles have none as large, and pass without a word about the one left out. Lanes keep the
+// largest of what they read, and of each span of tiles. The top-th largest of a block's 256
+// is a bound that `top` entries reach, and the entries that do are in spans of lanes whose
+// largest does (little more than `top` of them): these are read again for the candidates.
+// Segments are merged by a second kernel.
 //
 // 512 rows of 152064 bf16 (156 MB) with 20 alternatives: 44 + 5 us, 36 without (4.3 TB/s:
 // memory and the exponentials together); candidates kept inside the loop took 76 + 5. 3
@@ -231,6 +231,11 @@ __device__ __forceinline__ void store_top(const LogprobArgs &a, int r, int rank,
     a.top_logprob[at] = s.s != s.s ? s.s : k == 0 ? -INFINITY : (value_of(order_in(k)) - s.m) - log1pf(s.s);
 }
 
+// How far a wave's largest value may pass its reference: sums are scaled by less than
+// e^-kRefLag at a time, so that the roundings of earlier scalings fade, however often a
+// row rises.
+constexpr float kRefLag = 4.f;
+
 // The next float up (NaN past infinity).
 __device__ __forceinline__ float next_up(float x) {
   if (x == 0.f) return __uint_as_float(1);
@@ -276,7 +281,11 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
   const Given<T> t(a, r);
   const float after = next_up(t.x);
   float m = -INFINITY;        // the wave's largest value
-  float sum = 0.f, wsum = 0.f;  // the lane's share of S' and W
+  float ref = -INFINITY;      // what its exponentials are relative to
+  // The lane's share of S' and W relative to ref, a term a tile. (A term a column in 32 bits
+  // made chains of 16 roundings a tile: 4096 equal terms were off by 8e-6 of their sum. Here
+  // 32 bits take 6 roundings a tile and 64 the rest.)
+  double sum = 0., wsum = 0.;
   int ahead = 0;              // the wave's
   float peak = -INFINITY;     // the lane's largest value
   float high = -INFINITY;     // that of the span
@@ -290,39 +299,57 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
       top = fmaxf(top, x[i]);
     }
     const float least = v0 > t.id ? after : t.x;
+    float part[4] = {}, wpart[4] = {};
     if (!__any(top >= m)) {
 #pragma unroll
       for (int i = 0; i < kLpLane; ++i) {
-        const float d = x[i] - m, e = __expf(d);
-        sum += e;
-        wsum += e * fmaxf(d, -200.f);  // (e is 0 there, also for -inf)
+        const float d = x[i] - ref, e = __expf(d);
+        part[i % 4] += e;
+        wpart[i % 4] += e * fmaxf(d, -200.f);  // (e is 0 there, also for -inf)
         ahead += set_lanes(x[i] >= least);
       }
     } else {
       float now = top;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) now = fmaxf(now, __shfl_xor(now, d));
-      if (now > m && m > -INFINITY) {
-        // Lane 0 takes in what was the largest so far.
-        const float d = m - now, f = __expf(d), one = (lane == 0 ? 1.f : 0.f) + sum;
-        wsum = f == 0.f ? 0.f : f * (wsum + one * d);
-        sum = f * one;
-      }
       const bool out = now > m;
-      m = fmaxf(m, now);
-      const float z = m == -INFINITY ? 0.f : m;
+      if (out) {
+        if (m > -INFINITY) {
+          // Lane 0 takes in what was the largest so far.
+          const float d = m - ref, e = lane == 0 ? __expf(d) : 0.f;
+          sum += e;
+          wsum += e * d;
+        }
+        if (now > ref + kRefLag) {
+          // (From a reference of -inf there is nothing to carry over.)
+          const float d = ref - now, f = __expf(d);
+          wsum = f == 0.f ? 0. : f * (wsum + d * sum);
+          sum *= f;
+          ref = now;
+        }
+        m = now;
+      }
+      const float z = ref == -INFINITY ? 0.f : ref;
       int same = 0;
 #pragma unroll
       for (int i = 0; i < kLpLane; ++i) {
-        const float d = x[i] - z, e = __expf(d);
-        same += d == 0.f;
-        sum += d == 0.f ? 0.f : e;
-        wsum += e * fmaxf(d, -200.f);
+        const float d = x[i] - z, e = x[i] == m ? 0.f : __expf(d);
+        same += x[i] == m;
+        part[i % 4] += e;
+        wpart[i % 4] += e * fmaxf(d, -200.f);
         ahead += set_lanes(x[i] >= least);
       }
       const uint64_t who = __ballot(same > 0);
-      sum += (float)(same - (out && who && lane == __builtin_ctzll(who)));
+      if (m > -INFINITY) {
+        // (NaN where the largest is infinite.)
+        const bool left = out && who && lane == __builtin_ctzll(who);
+        const float d = m - ref, e = __expf(d) * (float)(same - left);
+        part[0] += e;
+        wpart[0] += e * d;
+      }
     }
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
+    wsum += (wpart[0] + wpart[1]) + (wpart[2] + wpart[3]);
     if (t.id >= v0 && t.id < v0 + kLpTile) {
       // (Counted by >= above: those after the token, and itself, only if larger.)
 #pragma unroll
@@ -348,12 +375,18 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a, int tile
     if (v0 + 2 * STEP < end) load(v0 + 2 * STEP, raw);
     tile(v0 + STEP, next);
   }
+  float S = (float)sum, W = (float)wsum;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    sum += __shfl_xor(sum, d);
-    wsum += __shfl_xor(wsum, d);
+    S += __shfl_xor(S, d);
+    W += __shfl_xor(W, d);
   }
-  if (lane == 0) stats[w] = {m, sum, wsum, ahead};
+  if (m > ref) {  // (both finite)
+    const float d = ref - m, f = __expf(d);
+    W = f * (W + d * S);
+    S *= f;
+  }
+  if (lane == 0) stats[w] = {m, S, W, ahead};
   if constexpr (TOP) {
     const uint32_t bound = block_bound<LOW>(a.top, order_of(peak), peaks);
     float lim = value_of(bound);
