@@ -508,8 +508,8 @@ size_t vsr_tree_attention_workspace_size(int32_t dtype, int32_t head_dim, int32_
  *   workspace : device, >= vsr_tree_attention_workspace_size bytes, 256-byte
  *            aligned, caller-owned; calls that overlap in time need their own (two
  *            captured graphs that share one must not replay at once).
- * out must not overlap q, k, v or itself, lse and the workspace no input and not each
- * other. n_heads % n_kv_heads == 0, n_heads <= 4096;
+ * out must not overlap an input or itself, lse and the workspace no input, nor out, nor
+ * each other. n_heads % n_kv_heads == 0, n_heads <= 4096;
  * 1 <= head_dim <= 256; 0 <= T <= 2^24, T n_heads < 2^31 - 256; scale finite.
  * pages->refs may be NULL.
  * Enqueued on hip_stream, whose device must be the current one; errors via
@@ -553,7 +553,8 @@ size_t vsr_pages_update_workspace_size(int32_t n_seqs);
  *   workspace : device, >= vsr_pages_update_workspace_size(n_seqs) bytes, 16-byte
  *            aligned, caller-owned (used with source alone, else it may be NULL).
  * Table entries past held are left as they are. A table entry outside [0, n_pages)
- * is neither counted nor copied. Arrays must not overlap, nor the workspace any.
+ * is neither counted nor copied. Arrays must not overlap, the cache's among them, nor
+ * the workspace any.
  * Enqueued on hip_stream, whose device must be the current one; errors via
  * vsr_last_error(NULL). */
 int vsr_pages_update(const vsr_pages *pages, const int32_t *source, const int32_t *room,
@@ -570,7 +571,8 @@ int vsr_pages_update(const vsr_pages *pages, const int32_t *source, const int32_
  *   len_out : device [n_seqs] out, the new lengths; pages->len, or an array of its own
  *            (pages->len then stays);
  *   release : nonzero: pages past the new length are given back (refs, held).
- * 0 <= max_kept <= 2^20. Arrays must not overlap, but for len_out as above.
+ * 0 <= max_kept <= 2^20. Arrays must not overlap, the cache's among them, but for len_out
+ * as above.
  * pages->refs may be NULL without release. Enqueued on hip_stream, whose device must
  * be the current one; errors via vsr_last_error(NULL). */
 int vsr_pages_keep(const vsr_pages *pages, const int32_t *kept, int64_t kept_stride,

@@ -1875,6 +1875,48 @@ bool ranges_meet(const void *a, size_t an, const void *b, size_t bn) {
   return a && b && an && bn && x < y + bn && y < x + an;
 }
 
+// Whether [p, p + n) bytes meet what lies at `base`: `width` bytes at every sum of i times
+// strides[l], i < counts[l]. Strides that do not nest count as if they filled their extent.
+struct Step {
+  size_t stride;
+  long count;
+};
+bool range_meets_steps(const void *p, size_t n, const void *base, std::initializer_list<Step> given,
+                       size_t width) {
+  size_t whole = width;
+  for (const Step &x : given) whole += (size_t)(x.count - 1) * x.stride;
+  if (!ranges_meet(p, n, base, whole)) return false;
+  Step steps[3];
+  int levels = 0;
+  for (const Step &x : given)
+    if (x.count > 1) steps[levels++] = x;
+  std::sort(steps, steps + levels, [](const Step &a, const Step &b) { return a.stride > b.stride; });
+  size_t extent[4];  // of one place at each level
+  extent[levels] = width;
+  for (int l = levels - 1; l >= 0; --l)
+    extent[l] = extent[l + 1] + (size_t)(steps[l].count - 1) * steps[l].stride;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(base);
+  if (a < b) return true;  // (it reaches the first byte)
+  size_t at = a - b;
+  for (int l = 0; l < levels; ++l) {
+    if (steps[l].stride < extent[l + 1]) return true;
+    at %= steps[l].stride;
+    // Behind one place, before the next (and it lies before the last one's end).
+    if (at >= extent[l + 1]) return at + n > steps[l].stride;
+    if (at + n > extent[l + 1]) return true;  // (it reaches that place's last byte)
+  }
+  return true;
+}
+
+// [p, p + n) bytes against `rows` rows of heads.
+bool range_meets_heads(const void *p, size_t n, const vsr_heads *h, long rows, int head_dim,
+                       size_t esize) {
+  return range_meets_steps(p, n, h->data,
+                           {{(size_t)h->token_stride * esize, rows},
+                            {(size_t)h->head_stride * esize, h->n_heads}},
+                           head_dim * esize);
+}
+
 const char *mask_error(const uint32_t *mask, int64_t stride, int32_t words) {
   if (!mask) return nullptr;
   if (reinterpret_cast<uintptr_t>(mask) & 3) return "mask must be 4-byte aligned";
@@ -1984,10 +2026,20 @@ extern "C" int vsr_tree_attention(const vsr_pages *pages, int32_t dtype, int32_t
     } ints[] = {{pages->table, ((seqs - 1) * pages->table_stride + pages->max_pages) * 4},
                 {pages->len, seqs * 4}, {pages->held, seqs * 4}, {start, seqs * 4 + 4},
                 {mask, mask ? mask_bytes(T, mask_stride, mask_words) : 0}};
-    for (const auto &x : ints)
+    for (const auto &x : ints) {
       if (ranges_meet(lse, lse_bytes, x.p, x.n) || ranges_meet(workspace, need, x.p, x.n))
         return "lse or workspace overlaps an input";
+      if (range_meets_heads(x.p, x.n, out, T, head_dim, esize)) return "out overlaps an input";
+    }
     if (ranges_meet(lse, lse_bytes, workspace, need)) return "lse overlaps the workspace";
+    const struct {
+      const vsr_heads *h;
+      long rows;
+    } heads[] = {{q, T}, {k, slots}, {v, slots}, {out, T}};
+    for (const auto &x : heads)
+      if (range_meets_heads(lse, lse_bytes, x.h, x.rows, head_dim, esize) ||
+          range_meets_heads(workspace, need, x.h, x.rows, head_dim, esize))
+        return x.h == out ? "out overlaps lse or the workspace" : "lse or workspace overlaps an input";
     return nullptr;
   };
   if (const char *msg = check()) return refuse(VSR_EINVAL, "tree_attention", msg);
@@ -2071,6 +2123,19 @@ const char *cache_error(const vsr_cache *c, long slots) {
   return nullptr;
 }
 
+// Whether [p, p + n) bytes meet a cache's keys or values.
+bool range_meets_cache(const void *p, size_t n, const vsr_cache *c, long slots) {
+  const size_t esize = c->dtype == VSR_F32 ? 4 : 2;
+  for (const void *base : {c->k, c->v})
+    if (range_meets_steps(p, n, base,
+                          {{(size_t)c->layer_stride * esize, c->n_layers},
+                           {(size_t)c->slot_stride * esize, slots},
+                           {(size_t)c->head_stride * esize, c->n_heads}},
+                          c->head_dim * esize))
+      return true;
+  return false;
+}
+
 CacheRows cache_rows(const vsr_cache *c) {
   const long esize = c->dtype == VSR_F32 ? 4 : 2;
   return {static_cast<char *>(c->k),
@@ -2107,8 +2172,12 @@ extern "C" int vsr_pages_update(const vsr_pages *pages, const int32_t *source,
     const IntArray mine[] = {{pages->table, (n - 1) * pages->table_stride + pages->max_pages},
                              {pages->len, n}, {pages->held, n}, {pages->refs, (size_t)pages->n_pages},
                              {source, n}, {room, n}, {ok, n}};
-    for (const IntArray &x : mine)
+    const long slots = (long)pages->n_pages * pages->page_size;
+    for (const IntArray &x : mine) {
       if (ranges_meet(workspace, need, x.p, x.n * 4)) return "the workspace overlaps another array";
+      if (range_meets_cache(x.p, x.n * 4, cache, slots)) return "the cache overlaps another array";
+    }
+    if (range_meets_cache(workspace, need, cache, slots)) return "the cache overlaps the workspace";
     return nullptr;
   };
   if (const char *msg = check()) return refuse(VSR_EINVAL, "pages_update", msg);
@@ -2134,7 +2203,14 @@ extern "C" int vsr_pages_keep(const vsr_pages *pages, const int32_t *kept, int64
     const size_t n = pages->n_seqs, list = max_kept ? (n - 1) * kept_stride + max_kept : 0;
     const int32_t *own_len = len_out == pages->len ? nullptr : len_out;
     if (const char *m = overlapping(pages, {{kept, list}, {n_kept, n}, {own_len, n}})) return m;
-    return cache_error(cache, (long)pages->n_pages * pages->page_size);
+    const long slots = (long)pages->n_pages * pages->page_size;
+    if (const char *m = cache_error(cache, slots)) return m;
+    const IntArray mine[] = {{pages->table, (n - 1) * pages->table_stride + pages->max_pages},
+                             {pages->len, n}, {pages->held, n}, {pages->refs, (size_t)pages->n_pages},
+                             {kept, list}, {n_kept, n}, {len_out, n}};
+    for (const IntArray &x : mine)
+      if (range_meets_cache(x.p, x.n * 4, cache, slots)) return "the cache overlaps another array";
+    return nullptr;
   };
   if (const char *msg = check()) return refuse(VSR_EINVAL, "pages_keep", msg);
   const PagesKeepArgs a{page_tables(pages), kept,    (long)kept_stride, n_kept, max_kept,
