@@ -161,8 +161,15 @@ __device__ __forceinline__ long work_cost(const TreeAttnArgs &a, const Work &w) 
   return (long)a.n_kv * w.tiles * (w.nb * w.cost);
 }
 
-// a / b, 0 <= a < 2^52, 0 < b < 2^31, by a reciprocal put right (a 64-bit division is 1 KB
-// of code, and a kernel's first steps wait for their code as well).
+// What a block takes of a call's cost. It passes 2^31 where a chain of 2^22 rows of 64 heads
+// meets all its keys.
+__host__ __device__ __forceinline__ long share_of(long total, int blocks) {
+  return std::max(1L, (total + blocks - 1) / blocks);
+}
+
+// a / b, 0 <= a < 2^57, 0 < b < 2^31, where that is below 2^31: by a reciprocal put right (a
+// 64-bit division is 1 KB of code, and a kernel's steps from item to item wait for their
+// code as well).
 __device__ __forceinline__ int quotient(long a, int b) {
   long q = (long)((double)a * __builtin_amdgcn_rcp((double)b));
   long r = a - q * b;
@@ -923,7 +930,7 @@ __global__ __launch_bounds__(S::NT, S::PER_CU) void k_tree_attn(TreeAttnArgs a) 
   const long total = plan.total;
   const int eff = blocks_used<S>(total, a.groups);
   const int g = logical_block(blockIdx.x, eff, a.groups);
-  const long per = max(1, __builtin_amdgcn_readfirstlane(quotient(total + eff - 1, eff)));
+  const long per = share_of(total, eff);
   long at = g * per;
   const long end = min(total, at + per);
   if (at >= end) {
