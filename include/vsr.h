@@ -552,9 +552,10 @@ size_t vsr_pages_update_workspace_size(int32_t n_seqs);
  *   cache  : HOST struct; may be NULL with source NULL;
  *   workspace : device, >= vsr_pages_update_workspace_size(n_seqs) bytes, 16-byte
  *            aligned, caller-owned (used with source alone, else it may be NULL).
- * Table entries past held are left as they are. A table entry outside [0, n_pages)
- * is neither counted nor copied. Arrays must not overlap, the cache's among them, nor
- * the workspace any.
+ * Table entries past held are left as they are, but for the one behind a copy that
+ * got no page: it names the source's last page, which is not counted for it. A table
+ * entry outside [0, n_pages) is neither counted nor copied. Arrays must not overlap,
+ * the cache's among them, nor the workspace any.
  * Enqueued on hip_stream, whose device must be the current one; errors via
  * vsr_last_error(NULL). */
 int vsr_pages_update(const vsr_pages *pages, const int32_t *source, const int32_t *room,
