@@ -706,8 +706,9 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, x[rt][t][i]);
     top = over_groups_max(top) * c;
-    // The reference of the exponents moves only where a score passes it by 2^8.
-    if (__any(top > R.m[rt] + 8.f)) {
+    // The reference of the exponents moves only where a score passes it by 2^8. (A difference:
+    // 8 above a reference past 2^27 is rounded to 16, and fp16's probabilities overflowed.)
+    if (__any(top - R.m[rt] > 8.f)) {
       const float m = fmaxf(R.m[rt], top);
       const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(R.m[rt] - m);
       R.m[rt] = m;

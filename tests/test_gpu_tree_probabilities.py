@@ -105,3 +105,36 @@ def test_maxima_that_rise_and_the_lowest_values(dtype):
             full = m + np.log(p.sum())
             assert (np.abs(lse[j].double().cpu().numpy() - full)
                     <= d + 2.0 ** -21 * (1 + abs(full)) + K * 2.0 ** -32).all(), (scale, j)
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("rows", [1, 20])
+def test_rises_by_the_last_digit_of_scores_past_2_27(dtype, rows):
+    """Scores whose fp32 neighbours lie 16 apart (in steps of log 2), one neighbour higher
+    from some tile on. Whatever their roundings make of the weights, an output lies between
+    the values it is a mean of, but for the roundings of test_gpu_tree.py's bound: u of itself
+    and 2 (u + K 2^-23 + 2^-20) of the largest."""
+    torch = _torch()
+    dt, page, hd, K, n = getattr(torch, dtype), 16, 64, 256, 16
+    u = torch.finfo(dt).eps / 2
+    # q . k = 49152^2 + 256 i: fp32 numbers of steps of 256, times c = 16 / 256. (Four key
+    # tiles a sequence: a block has its first two.)
+    k = torch.zeros((K + 2 * page, 1, hd), dtype=dt, device="cuda")
+    v = torch.ones_like(k)
+    k[:, 0, 0] = 49152.0
+    k[64:, 0, 1] = 256.0
+    v[64:] = 3.0
+    q = torch.zeros((n * rows, 1, hd), dtype=dt, device="cuda")
+    # (Both parities of the last digit: 256 j from the third column, j a sequence's number.)
+    q[:, 0, 0], q[:, 0, 1] = 49152.0, 1.0
+    k[:, 0, 2] = 256.0
+    q[:, 0, 2] = (torch.arange(n * rows, device="cuda") // rows).to(dt)
+    start = None if rows == 1 else np.arange(n + 1) * rows
+    table = np.tile(np.arange(K // page + 2), (n, 1))
+    lse = torch.empty(q.shape[:2], device="cuda")
+    scale = 16 / 256 / 1.4426950408889634
+    out = _attend(torch, table, [K // page + 2] * n, [K - rows] * n, page, q, k, v, scale, start,
+                  lse).float()
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    off = u * 3 + 2 * (u + (K + 32) * 2.0 ** -23 + 2.0 ** -20) * 3
+    assert float(out.min()) >= 1 - off and float(out.max()) <= 3 + off
