@@ -99,8 +99,8 @@ hipError_t launch_tree_rows(const TreeRowsArgs &a, hipStream_t s) {
 
 size_t tree_attention_workspace_bytes(int hd, int T, int n_seqs, int n_heads, int n_kv) {
   const int HD = hd <= 64 ? 64 : hd <= 128 ? 128 : 256;
-  const int rows = std::max(32, tree_block_rows(tree_rows_of(T, n_seqs, n_heads, n_kv)));
-  return (size_t)kTreeGroups * (2 * rows * (HD * sizeof(float) + sizeof(float2)) + sizeof(TreeJoin));
+  const size_t rows = tree_all_rows(tree_block_rows(tree_rows_of(T, n_seqs, n_heads, n_kv)), HD);
+  return 2 * rows * (HD * sizeof(float) + sizeof(float2)) + kTreeGroups * sizeof(TreeJoin);
 }
 
 hipError_t launch_tree_attention(const TreeAttnArgs &given, int dtype, void *ws, hipStream_t s) {

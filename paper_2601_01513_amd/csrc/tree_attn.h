@@ -1176,10 +1176,19 @@ bool tree_aligned(const TreeAttnArgs &a) {
   return a.hd * sizeof(T) % 16 == 0 && even(a.k, a.k_ts, a.k_hs) && even(a.v, a.v_ts, a.v_hs);
 }
 
+// Rows of all blocks together, by the rows of one (tree_block_rows) and head_dim's shape.
+constexpr int tree_all_rows(int block_rows, int HD) {
+  return block_rows <= 32 ? kTreeGroups * 32 : HD == 256 ? 256 * 128 : 256 * 256;
+}
+
 template <class S, bool VEC>
 hipError_t launch_tree_shape(TreeAttnArgs a, void *ws, hipStream_t s) {
   a.groups = 256 * S::PER_CU;
-  static_assert(256 * S::PER_CU <= kTreeGroups, "the workspace has room for each block");
+  // (Four waves also run in the place of eight, where rows do not lie on 16 bytes.)
+  static_assert(256 * S::PER_CU <= kTreeGroups &&
+                    256 * S::PER_CU * S::BM <= tree_all_rows(S::NW == 8 ? 256 : 32, S::HD) &&
+                    tree_all_rows(32, S::HD) <= tree_all_rows(256, S::HD),
+                "the workspace has room for each block");
   a.part = static_cast<float *>(ws);
   a.part_ml = reinterpret_cast<float2 *>(a.part + (size_t)2 * a.groups * S::BM * S::HD);
   a.joins = reinterpret_cast<TreeJoin *>(a.part_ml + (size_t)2 * a.groups * S::BM);

@@ -41,3 +41,18 @@ def test_shares_of_large_costs(share_of):
     for total in totals:
         for blocks in (1, 2, 255, 256, 512, rng.randrange(1, 512)):
             assert share_of(total, blocks) == -(-total // blocks)
+
+
+def test_workspaces_are_as_large_as_what_is_written():
+    """Two partial results of fp32 and their sums for each row of 512 blocks of 32 rows, or of
+    256 blocks of 256 (head_dim past 128: of 128) rows, and 512 lists of 24 bytes."""
+    from paper_2601_01513_amd import binding as B
+    if not os.path.exists(B.LIB_PATH):
+        pytest.skip("libvsr.so not built (python -m paper_2601_01513_amd.build)")
+    size = B.load_library().vsr_tree_attention_workspace_size
+    for hd, HD in ((1, 64), (64, 64), (65, 128), (128, 128), (129, 256), (256, 256)):
+        for T, rows in ((8, 512 * 32), (64, 512 * 32), (65, 256 * (128 if HD == 256 else 256)),
+                        (4096, 256 * (128 if HD == 256 else 256))):
+            for dtype in (B.VSR_F32, B.VSR_BF16, B.VSR_F16):
+                need = 2 * rows * (HD * 4 + 8) + 512 * 24
+                assert need <= size(dtype, hd, T, 8, 4, 1) <= need + 256, (hd, T)
