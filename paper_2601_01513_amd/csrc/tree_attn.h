@@ -115,6 +115,7 @@ struct TreeShape {
   // 2^0 a key below 2^-25 counted for nothing, and long contexts behind one strong key
   // lost all their other keys.)
   static constexpr float LIFT = std::is_same<T, f16>::value ? 7.f : 0.f;
+  static constexpr float DROP = LIFT > 0.f ? 0x1p-7f : 1.f;  // 2^-LIFT
   static_assert(KW >= 1 && NL >= 1, "each wave has keys, each thread a load");
   static_assert(NW * 16 * HD * 4 <= 4 * TILE * 16, "a row group of each wave fits the ring");
 };
@@ -766,6 +767,9 @@ __device__ __forceinline__ void tile_step(const TreeAttnArgs &a, const Work &w, 
   } else {
     typedef typename M::x4 x4;
     typedef typename M::x8 x8;
+    // Rounded to the values' type, as the matrix units take them: results are 2.3e-3 off for
+    // bf16, where their own rounding alone makes 1.7e-3, 2.9e-4 and 2.1e-4 for fp16. (A second
+    // product with what the rounding leaves would double the work with values.)
     x4 p[NR][S::KW];
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt)
@@ -860,7 +864,7 @@ __device__ __forceinline__ void put_row(const TreeAttnArgs &a, const Work &w, in
   if (c == 0 && a.lse)
     a.lse[(long)(w.b + j) * a.n_heads + h] =
         l == 0.f ? -INFINITY
-                 : (top + (__builtin_log2f(l) - S::LIFT)) * 0.69314718055994531f;
+                 : (top + __builtin_log2f(l * S::DROP)) * 0.69314718055994531f;
 }
 
 // An item's rows stored (put_row), a group of each wave after the other, through the ring's

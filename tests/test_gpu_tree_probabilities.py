@@ -138,3 +138,29 @@ def test_rises_by_the_last_digit_of_scores_past_2_27(dtype, rows):
     assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
     off = u * 3 + 2 * (u + (K + 32) * 2.0 ** -23 + 2.0 ** -20) * 3
     assert float(out.min()) >= 1 - off and float(out.max()) <= 3 + off
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+def test_log_sums_near_nothing(dtype):
+    """lse around 0 to its own digits: n equal scores of -log n, n <= 9. In steps of log 2,
+    where |x| and log2 n are below 3.17: log2 is off by 2^-22 of itself, 7.6e-7, the score by
+    2^-24 of itself for log2(e)'s rounding, 1.9e-7, and half a last digit, 1.2e-7, the
+    probabilities by 2^-24, 0.9e-7 there; the sum of n of them is exact. Times log 2: 8.1e-7,
+    with the last products' roundings below 2^-20."""
+    torch = _torch()
+    dt, page, hd = getattr(torch, dtype), 16, 64
+    k = torch.zeros((page, 1, hd), dtype=dt, device="cuda")
+    v = torch.ones_like(k)
+    q = torch.zeros((9, 1, hd), dtype=dt, device="cuda")
+    k[:, 0, :2] = 1
+    for i in range(9):
+        y = -np.log(i + 1.0)
+        hi = float(torch.tensor(y).to(dt))
+        q[i, 0, 0], q[i, 0, 1] = hi, float(torch.tensor(y - hi).to(dt))
+    lse = torch.empty((9, 1), device="cuda")
+    out = _attend(torch, [[0]], [1], [0], page, q, k, v, 1.0, [0, 9], lse)
+    x = q.double()[:, 0, :2].sum(1).cpu().numpy()
+    want = x + np.log(np.arange(1, 10))
+    assert np.abs(lse.double().cpu().numpy()[:, 0] - want).max() <= 2.0 ** -20
+    # (The sum over itself: a reciprocal and a product, 2^-24 each of it in fp32.)
+    assert float((out.double() - 1).abs().max()) <= 2.0 ** -22
