@@ -510,7 +510,7 @@ size_t vsr_tree_attention_workspace_size(int32_t dtype, int32_t head_dim, int32_
  *            captured graphs that share one must not replay at once).
  * out must not overlap an input or itself, lse and the workspace no input, nor out, nor
  * each other. n_heads % n_kv_heads == 0, n_heads <= 4096;
- * 1 <= head_dim <= 256; 0 <= T <= 2^24, T n_heads < 2^31 - 256; scale finite.
+ * 1 <= head_dim <= 256; 0 <= T <= 2^24, T n_heads < 2^31 - 256; |scale| <= 2^127.
  * pages->refs may be NULL.
  * Enqueued on hip_stream, whose device must be the current one; errors via
  * vsr_last_error(NULL). */

@@ -1997,7 +1997,8 @@ extern "C" int vsr_tree_attention(const vsr_pages *pages, int32_t dtype, int32_t
     if (head_dim < 1 || head_dim > 256) return "head_dim must lie in [1, 256]";
     if (T < 0 || T > kMaxTreeRows) return "T must lie in [0, 2^24]";
     if (!start && T != pages->n_seqs) return "T must be n_seqs without start";
-    if (!std::isfinite(scale)) return "scale must be finite";
+    // (Times log2(e) it stays a finite float.)
+    if (!(std::fabs(scale) <= 0x1p127f)) return "scale must be at most 2^127 either way";
     if (!q || !k || !v || !out) return "q, k, v and out must be non-NULL";
     if (T == 0) return nullptr;
     if (!aligned4({start, lse})) return "start and lse must be 4-byte aligned";
