@@ -152,7 +152,7 @@ constexpr int kRoomThreads = 1024, kRoomPages = 16;
 __device__ __forceinline__ uint32_t free_pages(const PageTables &p, int first) {
   typedef Pack<int32_t, 4> I4;
   uint32_t bits = 0;
-  if (first + kRoomPages <= p.n_pages) {
+  if (first <= p.n_pages - kRoomPages) {  // (first + kRoomPages may pass 2^31)
     I4 r[kRoomPages / 4];
 #pragma unroll
     for (int i = 0; i < kRoomPages / 4; ++i)
