@@ -99,7 +99,10 @@ __global__ __launch_bounds__(kForkThreads) void k_fork_tables(PagesUpdateArgs a,
   __shared__ Seqs q;
   __shared__ int32_t fresh[kForkEntries];
   load_seqs<kForkThreads>(a, q);
-  fork_tables(a, q, fresh, blockIdx.x << shift, shift);
+  for (int c0 = blockIdx.x << shift; c0 < a.pages.max_pages; c0 += gridDim.x << shift) {
+    fork_tables(a, q, fresh, c0, shift);
+    __syncthreads();  // (fresh is free)
+  }
 }
 
 // The first `rows` rows of page `from` go to the page at column `col` of sequence `seq`.
@@ -445,7 +448,9 @@ hipError_t launch_pages_update(const PagesUpdateArgs &a, void *ws, hipStream_t s
   } else {
     if (a.source) {
       shift = std::min(shift, 4);  // (16 columns are a line of the table.)
-      k_fork_tables<<<((a.pages.max_pages - 1) >> shift) + 1, kForkThreads, 0, s>>>(a, shift);
+      // (A launch has below 2^32 threads: wider tables in turns.)
+      const int blocks = std::min(((a.pages.max_pages - 1) >> shift) + 1, 1 << 16);
+      k_fork_tables<<<blocks, kForkThreads, 0, s>>>(a, shift);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
