@@ -15,7 +15,7 @@
 // largest does (little more than `top` of them): these are read again for the candidates.
 // Segments are merged by a second kernel.
 //
-// 512 rows of 152064 bf16 (156 MB) with 20 alternatives: 44 + 5 us, 36 without (4.3 TB/s:
+// 512 rows of 152064 bf16 (156 MB) with 20 alternatives: 46 + 5 us, 39 without (4.0 TB/s:
 // memory and the exponentials together); candidates kept inside the loop took 76 + 5. 3
 // rows of 151936 fp32: 8 + 7, a launch's way twice.
 #include <algorithm>

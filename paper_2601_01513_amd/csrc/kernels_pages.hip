@@ -337,7 +337,8 @@ __device__ __forceinline__ void bounds_of(const PageTables &p, int s, int &len, 
 }
 
 // Grid ((layer, matrix, head, slice) / 4, sequence): a wave moves a slice of 64 pieces of
-// the rows (64 sequences of 28 layers, 9 rows each: 10.2 us, memory's rate).
+// the rows (64 sequences of 28 layers, 33 MB read and written: 10.2 us, 3.2 TB/s; the list
+// and the table come before each wave's first load).
 // Rows move to lower places only, and rise: eight are read, then written, then the next,
 // and no row is written that a later one is read from.
 template <typename U>
