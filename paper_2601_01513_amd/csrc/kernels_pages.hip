@@ -188,6 +188,8 @@ __device__ __forceinline__ Turn turn_of(const PagesUpdateArgs &a, const Seqs &q,
   return t;
 }
 
+constexpr int kAllMemory = 0x0f70;  // s_waitcnt's word for "no load, store or atomic is on its way"
+
 template <bool FORK>
 __global__ __launch_bounds__(kRoomThreads) void k_room(PagesUpdateArgs a, PageCopies *copies,
                                                        int shift) {
@@ -205,8 +207,10 @@ __global__ __launch_bounds__(kRoomThreads) void k_room(PagesUpdateArgs a, PageCo
   if constexpr (FORK) {
     static_assert(sizeof(list) >= sizeof(int32_t) * kForkEntries, "");
     fork_tables(a, q, reinterpret_cast<int32_t *>(list), 0, shift);
-    // The block's own stores and counts lie in its L2: no older line of the L1 is read.
+    // Every wave's stores and counts lie in the L2 before the others read on (the barrier's
+    // own release does not wait for them), and no older line of the L1 is read.
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(kAllMemory);
     __syncthreads();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   }
